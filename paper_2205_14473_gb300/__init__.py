@@ -12,6 +12,9 @@ or cannot be loaded, the first call raises.
         for i in range(cfg.n): rnd.worker_compress(i, g[i])
         rnd.server_step()
         rnd.apply(x)
+
+Embedding, GradNorm, AdamW and TensorList, the operators around a round of a language model's training, are in
+lm.py (include/ea_lm.h).
 """
 from __future__ import annotations
 
@@ -20,6 +23,7 @@ import dataclasses
 import os
 import threading
 
+from . import lm_abi
 from .workloads import (ADAM_AT_SERVER, ADAM_AT_WORKER, Q_IDENTITY, Q_POW2, Q_SIGN_L1,  # noqa: F401
                         Q_UNIFORM_MAX, QuantSpec, Workload)
 
@@ -32,7 +36,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "_lib", "libea.so")
 EXPORTED = ["ea_workspace_bytes", "ea_init", "ea_worker_compress", "ea_server_step", "ea_worker_apply", "ea_round_step",
             "ea_bits_sent", "ea_round_index", "ea_round_launches", "ea_get_view", "ea_sync_status", "ea_last_error", "ea_destroy",
-            "ea_worker_compress_noalloc", "ea_set_hparams", "ea_selftest_bounded_wait"]
+            "ea_worker_compress_noalloc", "ea_set_hparams", "ea_selftest_bounded_wait", *lm_abi.EXPORTED]
 
 
 class EAError(RuntimeError):
@@ -85,6 +89,7 @@ def lib() -> ctypes.CDLL:
             L.ea_destroy.argtypes = [_P]
             L.ea_set_hparams.argtypes = [_P, ctypes.c_float, ctypes.c_float, ctypes.c_float]
             L.ea_worker_compress_noalloc.argtypes = [C, ctypes.c_int32, ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P]
+            lm_abi.declare(L)
             L.ea_selftest_bounded_wait.argtypes = [ctypes.c_int64, ctypes.c_int32, _P, ctypes.POINTER(ctypes.c_int32)]
             _lib = L
     return _lib
@@ -309,3 +314,13 @@ class EARound:
         off = ptr - self.workspace.data_ptr()
         dt = torch.int32 if which in (EA_VIEW_CODES_WORKER, EA_VIEW_CODES_SERVER) else torch.float32
         return self.workspace[off:off + n].view(dt)
+
+
+def __getattr__(name: str):
+    """The operators of lm.py (which, unlike this module, imports torch when it is loaded)."""
+    if name in ("Embedding", "GradNorm", "AdamW", "TensorList", "lm"):
+        import importlib
+
+        lm = importlib.import_module(".lm", __name__)
+        return lm if name == "lm" else getattr(lm, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,0 +1,228 @@
+// ea_norm.cu -- ea_grad_norm: the 2-norm of a list of gradients and the factor that clips them.
+#include "ea_lm.cuh"
+
+namespace ea {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormUnit = 1024;  // coordinates of a warp's unit of work
+
+struct NormArgs {
+    int64_t units;           // of this launch
+    int n_tensors;           // of this launch
+    const int64_t *first;    // n_tensors + 1: each tensor's first unit within the launch
+    const int64_t *sizes;
+    double *partials;        // one per CTA, of this launch
+    const double *all;       // of all launches, n_all of them
+    int n_all;
+    unsigned *ticket;
+    int last;                // whether this launch is the last one
+    float grad_scale, max_norm;
+    float *out;
+};
+
+template <class G>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a, const __grid_constant__ GradList list)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kNormThreads / 32);
+    double sum = 0.0;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kNormThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
+        int lo = 0, hi = a.n_tensors - 1;  // the last tensor whose first unit is <= u
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (a.first[mid] <= u) lo = mid;
+            else hi = mid - 1;
+        }
+        const int64_t base = (u - a.first[lo]) * kNormUnit;
+        const int64_t n = min(a.sizes[lo] - base, static_cast<int64_t>(kNormUnit));
+        const G *g = static_cast<const G *>(list.g[lo]) + base;
+        for (int64_t j = lane; j < n; j += 32) {
+            const double x = to_f32(g[j]);
+            sum += x * x;
+        }
+    }
+    __shared__ double red[kNormThreads];
+    __shared__ bool last;
+    auto block_sum = [&](double v) {
+        red[threadIdx.x] = v;
+        __syncthreads();
+        for (int o = kNormThreads / 2; o > 0; o >>= 1) {
+            if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+            __syncthreads();
+        }
+        return red[0];
+    };
+    const double total = block_sum(sum);
+    if (threadIdx.x == 0) {
+        a.partials[blockIdx.x] = total;
+        __threadfence();
+        last = a.last && atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    double v = 0.0;
+    for (int i = threadIdx.x; i < a.n_all; i += kNormThreads) v += __ldcg(a.all + i);
+    __syncthreads();
+    v = block_sum(v);
+    if (threadIdx.x == 0) {
+        *a.ticket = 0;
+        const float norm = static_cast<float>(fabs(static_cast<double>(a.grad_scale)) * sqrt(v));
+        float factor = a.grad_scale;
+        if (!isfinite(norm)) factor = __int_as_float(0x7fc00000);
+        else if (norm > a.max_norm)
+            factor = static_cast<float>(a.grad_scale * (a.max_norm / (fabs(static_cast<double>(a.grad_scale)) * sqrt(v))));
+        a.out[0] = norm;
+        a.out[1] = factor;
+    }
+}
+
+}  // namespace ea
+
+using namespace ea;
+
+struct ea_norm {
+    DeviceOf dev;
+    cudaStream_t stream = nullptr;
+    int32_t type = 0;
+    std::vector<int64_t> sizes;
+    struct Launch {
+        int first_tensor, n_tensors, grid;
+        int64_t units, first_at;  // first_at: of its unit offsets in the table
+    };
+    std::vector<Launch> launches;
+    std::vector<int64_t> table;  // every launch's unit offsets (kept until the upload is done)
+    int64_t *d_first = nullptr, *d_sizes = nullptr;
+    double *d_partials = nullptr;
+    unsigned *d_ticket = nullptr;
+    int n_partials = 0;
+};
+
+namespace {
+
+constexpr int kNormCtasPerSm = 8;
+
+int validate(const ea_grad_norm_config *cfg)
+{
+    if (!cfg) return lm_fail(EA_E_INVAL, "config is NULL");
+    if (cfg->n_tensors < 1 || cfg->n_tensors > (1 << 20)) return lm_fail(EA_E_INVAL, "n_tensors must be in [1, 2^20]");
+    if (!cfg->sizes) return lm_fail(EA_E_INVAL, "sizes is NULL");
+    if (!is_float_type(cfg->grad_type)) return lm_fail(EA_E_INVAL, "unknown gradient type %d", cfg->grad_type);
+    for (int32_t i = 0; i < cfg->n_tensors; ++i)
+        if (cfg->sizes[i] < 0 || cfg->sizes[i] > (int64_t{1} << 40))
+            return lm_fail(EA_E_INVAL, "the size of tensor %d is out of [0, 2^40]", i);
+    return EA_OK;
+}
+
+// Bytes of the pieces of the workspace, each a multiple of 256.
+struct NormLayout {
+    size_t first, sizes, partials, ticket;
+    size_t total() const { return first + sizes + partials + ticket; }
+};
+
+NormLayout norm_layout(const ea_grad_norm_config &cfg, int sms)
+{
+    const size_t n = cfg.n_tensors, launches = (n + kGradBatch - 1) / kGradBatch;
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    return {up((n + launches) * 8), up(n * 8), up(launches * sms * kNormCtasPerSm * 8), up(4)};
+}
+
+}  // namespace
+
+extern "C" {
+
+int ea_grad_norm_workspace_bytes(const ea_grad_norm_config *cfg, size_t *bytes)
+{
+    if (!bytes) return lm_fail(EA_E_INVAL, "bytes is NULL");
+    const int r = validate(cfg);
+    if (r != EA_OK) return r;
+    *bytes = norm_layout(*cfg, kMaxSms).total();
+    return EA_OK;
+}
+
+int ea_grad_norm_init(const ea_grad_norm_config *cfg, void *workspace, size_t workspace_bytes, void *stream, ea_norm **out)
+{
+    if (!out) return lm_fail(EA_E_INVAL, "out is NULL");
+    *out = nullptr;
+    int r = validate(cfg);
+    if (r != EA_OK) return r;
+    const NormLayout L = norm_layout(*cfg, kMaxSms);
+    if ((r = check_workspace(workspace, workspace_bytes, L.total())) != EA_OK) return r;
+    ea_norm *h = new (std::nothrow) ea_norm;
+    if (!h) return lm_fail(EA_E_INVAL, "out of host memory");
+    r = h->dev.query();
+    try {
+        h->stream = static_cast<cudaStream_t>(stream);
+        h->type = cfg->grad_type;
+        h->sizes.assign(cfg->sizes, cfg->sizes + cfg->n_tensors);
+        for (int i = 0; i < cfg->n_tensors; i += kGradBatch) {
+            ea_norm::Launch l{i, std::min(kGradBatch, cfg->n_tensors - i), 0, 0, static_cast<int64_t>(h->table.size())};
+            for (int k = 0; k < l.n_tensors; ++k) {
+                h->table.push_back(l.units);
+                l.units += (h->sizes[i + k] + kNormUnit - 1) / kNormUnit;
+            }
+            h->table.push_back(l.units);
+            const int64_t ctas = (l.units + kNormThreads / 32 - 1) / (kNormThreads / 32);
+            l.grid = static_cast<int>(std::clamp<int64_t>(ctas, 1, std::min(h->dev.sms, kMaxSms) * kNormCtasPerSm));
+            h->n_partials += l.grid;
+            h->launches.push_back(l);
+        }
+    } catch (const std::bad_alloc &) {
+        r = lm_fail(EA_E_INVAL, "out of host memory");
+    }
+    if (r == EA_OK) {
+        char *p = static_cast<char *>(workspace);
+        h->d_first = reinterpret_cast<int64_t *>(p);
+        h->d_sizes = reinterpret_cast<int64_t *>(p += L.first);
+        h->d_partials = reinterpret_cast<double *>(p += L.sizes);
+        h->d_ticket = reinterpret_cast<unsigned *>(p += L.partials);
+        r = lm_cuda(cudaMemsetAsync(h->d_ticket, 0, 4, h->stream), "ticket clear");
+    }
+    if (r == EA_OK)
+        r = lm_cuda(cudaMemcpyAsync(h->d_first, h->table.data(), h->table.size() * 8, cudaMemcpyHostToDevice, h->stream), "table upload");
+    if (r == EA_OK)
+        r = lm_cuda(cudaMemcpyAsync(h->d_sizes, h->sizes.data(), h->sizes.size() * 8, cudaMemcpyHostToDevice, h->stream), "table upload");
+    if (r != EA_OK) {
+        delete h;
+        return r;
+    }
+    *out = h;
+    return EA_OK;
+}
+
+int ea_grad_norm(ea_norm *h, const void *const *grads, float grad_scale, float max_norm, float *out)
+{
+    if (!h) return lm_fail(EA_E_INVAL, "handle is NULL");
+    if (!grads) return lm_fail(EA_E_INVAL, "grads is NULL");
+    if (!std::isfinite(grad_scale) || grad_scale == 0.0f) return lm_fail(EA_E_INVAL, "grad_scale must be finite and not 0");
+    if (!(max_norm >= 0.0f)) return lm_fail(EA_E_INVAL, "max_norm must be >= 0");
+    int r = check_address(out, EA_T_F32, "out");
+    for (size_t i = 0; r == EA_OK && i < h->sizes.size(); ++i)
+        if (h->sizes[i]) r = check_address(grads[i], h->type, "a gradient");
+    if (r == EA_OK) r = h->dev.check();
+    if (r != EA_OK) return r;
+    int at = 0;
+    for (size_t k = 0; k < h->launches.size(); ++k) {
+        const ea_norm::Launch &l = h->launches[k];
+        GradList list{};
+        std::copy(grads + l.first_tensor, grads + l.first_tensor + l.n_tensors, list.g);
+        const NormArgs a{l.units, l.n_tensors, h->d_first + l.first_at, h->d_sizes + l.first_tensor, h->d_partials + at,
+                         h->d_partials, h->n_partials, h->d_ticket, k + 1 == h->launches.size(), grad_scale, max_norm, out};
+        switch (h->type) {
+        case EA_T_F32: norm_kernel<float><<<l.grid, kNormThreads, 0, h->stream>>>(a, list); break;
+        case EA_T_BF16: norm_kernel<bf16><<<l.grid, kNormThreads, 0, h->stream>>>(a, list); break;
+        default: norm_kernel<f16><<<l.grid, kNormThreads, 0, h->stream>>>(a, list);
+        }
+        if ((r = lm_cuda(cudaGetLastError(), "launch")) != EA_OK) return r;
+        at += l.grid;
+    }
+    return EA_OK;
+}
+
+int ea_grad_norm_destroy(ea_norm *h)
+{
+    delete h;
+    return EA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,94 @@
+"""The operators of include/ea_lm.h without a GPU: what they refuse before any CUDA call, and the sizes of their
+workspaces."""
+import ctypes
+
+import pytest
+
+import paper_2205_14473_gb300 as ea
+from paper_2205_14473_gb300 import lm_abi as A
+
+
+def _embed(**kw):
+    c = dict(vocab=100, dim=8, max_tokens=64, padding=-1, scale=1.0)
+    c.update(kw)
+    return A.ea_embed_config(*[c[k] for k in ("vocab", "dim", "max_tokens", "padding", "scale")])
+
+
+def _norm(sizes=(5, 0, 7), n=None, kind=A.EA_T_F32):
+    arr = (ctypes.c_int64 * max(len(sizes), 1))(*sizes)
+    c = A.ea_grad_norm_config(len(sizes) if n is None else n, kind, ctypes.cast(arr, ctypes.POINTER(ctypes.c_int64)))
+    c.keep = arr
+    return c
+
+
+def _adamw(tensor=None, **kw):
+    t = dict(size=10, param=4096, m=4096, v=4096, m_scale=4096, v_scale=4096, copy=0, weight_decay=0.1, lr_scale=1.0)
+    t.update(tensor or {})
+    c = dict(n_tensors=1, param_type=A.EA_T_F32, grad_type=A.EA_T_F32, copy_type=A.EA_T_BF16, state_bits=32, beta1=0.9,
+             beta2=0.999, eps=1e-8, seed=0, step=0)
+    c.update(kw)
+    arr = (A.ea_adamw_tensor * 1)(A.ea_adamw_tensor(*[t[f] for f, _ in A.ea_adamw_tensor._fields_]))
+    out = A.ea_adamw_config(*[c[f] for f, _ in A.ea_adamw_config._fields_[:-1]],
+                            ctypes.cast(arr, ctypes.POINTER(A.ea_adamw_tensor)))
+    out.keep = arr
+    return out
+
+
+def _refused(L, kind, config, status):
+    n, h = ctypes.c_size_t(0), ctypes.c_void_p()
+    assert getattr(L, kind + "_workspace_bytes")(config, ctypes.byref(n)) == status
+    assert L.ea_last_error(None)
+    assert getattr(L, kind + "_init")(config, 4096, 1 << 30, None, ctypes.byref(h)) == status
+    assert not h.value
+
+
+@pytest.mark.parametrize("bad", [dict(vocab=0), dict(vocab=2 ** 31 - 1), dict(dim=0), dict(dim=2 ** 24 + 1),
+                                 dict(max_tokens=-1), dict(max_tokens=2 ** 30 + 1), dict(padding=-2), dict(padding=100),
+                                 dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_embedding_refusals(ea_lib, bad):
+    _refused(ea_lib, "ea_embed", _embed(**bad), ea.EA_E_INVAL)
+
+
+@pytest.mark.parametrize("bad", [dict(sizes=()), dict(sizes=(3, -1)), dict(kind=A.EA_T_I32), dict(n=2 ** 20 + 1),
+                                 dict(sizes=(2 ** 40 + 1,))])
+def test_norm_refusals(ea_lib, bad):
+    _refused(ea_lib, "ea_grad_norm", _norm(**bad), ea.EA_E_INVAL)
+
+
+@pytest.mark.parametrize("status,tensor,bad", [
+    (ea.EA_E_INVAL, {}, dict(n_tensors=0)), (ea.EA_E_INVAL, {}, dict(state_bits=16)),
+    (ea.EA_E_INVAL, {}, dict(beta1=1.0)), (ea.EA_E_INVAL, {}, dict(beta2=-0.1)), (ea.EA_E_INVAL, {}, dict(eps=0.0)),
+    (ea.EA_E_INVAL, {}, dict(step=-1)), (ea.EA_E_INVAL, {}, dict(step=2 ** 32)), (ea.EA_E_INVAL, {}, dict(grad_type=9)),
+    (ea.EA_E_UNSUPPORTED, {}, dict(param_type=A.EA_T_F16)), (ea.EA_E_INVAL, dict(size=-1), {}),
+    (ea.EA_E_INVAL, dict(param=0), {}), (ea.EA_E_ALIGN, dict(param=4098), {}), (ea.EA_E_ALIGN, dict(m=4097), {}),
+    (ea.EA_E_INVAL, dict(weight_decay=-1.0), {}), (ea.EA_E_INVAL, dict(weight_decay=float("nan")), {}),
+    (ea.EA_E_INVAL, dict(lr_scale=-1.0), {}), (ea.EA_E_INVAL, dict(v=0), dict(state_bits=8)),
+    (ea.EA_E_INVAL, dict(m_scale=0), dict(state_bits=8)), (ea.EA_E_ALIGN, dict(v_scale=4098), dict(state_bits=8)),
+    (ea.EA_E_INVAL, dict(copy=4096), dict(copy_type=A.EA_T_F32)), (ea.EA_E_ALIGN, dict(copy=4097), {}),
+])
+def test_adamw_refusals(ea_lib, status, tensor, bad):
+    _refused(ea_lib, "ea_adamw", _adamw(tensor, **bad), status)
+
+
+@pytest.mark.parametrize("kind,config", [("ea_embed", _embed()), ("ea_grad_norm", _norm()), ("ea_adamw", _adamw())])
+def test_workspace_checks_come_before_the_device(ea_lib, kind, config):
+    n, h = ctypes.c_size_t(0), ctypes.c_void_p()
+    assert getattr(ea_lib, kind + "_workspace_bytes")(config, ctypes.byref(n)) == ea.EA_OK and n.value >= 256
+    init = getattr(ea_lib, kind + "_init")
+    for ws, size in ((None, n.value), (4096 + 16, n.value), (4096, n.value - 1)):
+        assert init(config, ws, size, None, ctypes.byref(h)) == ea.EA_E_WORKSPACE
+    assert init(config, 4096, n.value, None, None) == ea.EA_E_INVAL
+    assert getattr(ea_lib, kind + "_workspace_bytes")(config, None) == ea.EA_E_INVAL
+    assert getattr(ea_lib, kind + "_workspace_bytes")(None, ctypes.byref(n)) == ea.EA_E_INVAL
+    assert getattr(ea_lib, kind + "_destroy")(None) == ea.EA_OK
+
+
+def test_null_handles(ea_lib):
+    one = (ctypes.c_void_p * 1)(4096)
+    call = A.ea_embed_call(1, 1, 1, 1, 8, 8, 8, A.EA_T_I64, A.EA_T_F32, A.EA_T_F32)
+    assert ea_lib.ea_embed_lookup(None, call, 4096, 4096, 4096) == ea.EA_E_INVAL
+    assert ea_lib.ea_embed_grad(None, call, 4096, 4096, 4096, 0) == ea.EA_E_INVAL
+    assert ea_lib.ea_embed_sync_status(None) == ea.EA_E_INVAL
+    assert ea_lib.ea_grad_norm(None, one, 1.0, 1.0, 4096) == ea.EA_E_INVAL
+    assert ea_lib.ea_adamw_step(None, one, 1e-3, None) == ea.EA_E_INVAL
+    assert ea_lib.ea_adamw_step_index(None, None) == ea.EA_E_INVAL
