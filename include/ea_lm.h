@@ -29,7 +29,7 @@ typedef enum { EA_T_F32 = 0, EA_T_BF16 = 1, EA_T_F16 = 2, EA_T_I32 = 3, EA_T_I64
 
 typedef struct ea_embed_config {
     int64_t vocab;       /* rows of the table, 1 .. 2^31 - 2 */
-    int64_t dim;         /* its columns, 1 .. 2^24 */
+    int64_t dim;         /* its columns, 1 .. 2^20 */
     int64_t max_tokens;  /* most tokens of one call, 0 .. 2^30 */
     int64_t padding;     /* a token that takes no gradient, or -1 */
     float scale;         /* finite; the output and the gradient are multiplied by it */

@@ -1,5 +1,9 @@
 // ea_embed.cu -- the lookup of tokens in an embedding table (ea_embed_lookup) and the gradient of the table
 // (ea_embed_grad).
+#include <cooperative_groups.h>
+#include <type_traits>
+
+#include "ea_async.cuh"
 #include "ea_lm.cuh"
 
 namespace ea {
@@ -8,7 +12,9 @@ constexpr uint32_t kStatusToken = 4u;  // a token outside the table
 constexpr int kEmbedThreads = 256;
 
 struct EmbedArgs {
-    int64_t n, inner;            // tokens; tokens per row of the batch
+    int64_t n;                   // tokens
+    uint32_t inner, magic;       // tokens per row of the batch (0: all in one row), and t / inner = t * magic >> 32 + shift
+    int shift;
     int64_t token_outer, token_inner, row_outer, row_inner, table_stride;
     int64_t vocab, dim, padding;
     float scale;
@@ -17,16 +23,25 @@ struct EmbedArgs {
     uint32_t *status;
 };
 
-__device__ __forceinline__ int64_t token_at(const EmbedArgs &a, int64_t t)
+// Token t of the call lies in row i = t / inner of the batch.  The division of t < 2^30 by the constant inner >= 2
+// is a multiplication (Granlund and Montgomery, "Division by invariant integers using multiplication"): with
+// s = ceil(log2 inner) and magic = floor(2^(31 + s) / inner) + 1 < 2^32 the error stays below 1 / inner.
+__device__ __forceinline__ uint32_t batch_row(const EmbedArgs &a, uint32_t t)
 {
-    const int64_t i = t / a.inner, at = i * a.token_outer + (t - i * a.inner) * a.token_inner;
+    return a.inner ? __umulhi(t, a.magic) >> a.shift : 0;
+}
+
+__device__ __forceinline__ int64_t token_at(const EmbedArgs &a, uint32_t t)
+{
+    const uint32_t i = batch_row(a, t);
+    const int64_t at = i * a.token_outer + static_cast<int64_t>(t - i * a.inner) * a.token_inner;
     return a.token64 ? static_cast<const int64_t *>(a.tokens)[at] : static_cast<const int32_t *>(a.tokens)[at];
 }
 
-__device__ __forceinline__ int64_t row_at(const EmbedArgs &a, int64_t t)
+__device__ __forceinline__ int64_t row_at(const EmbedArgs &a, uint32_t t)
 {
-    const int64_t i = t / a.inner;
-    return i * a.row_outer + (t - i * a.inner) * a.row_inner;
+    const uint32_t i = batch_row(a, t);
+    return i * a.row_outer + static_cast<int64_t>(t - i * a.inner) * a.row_inner;
 }
 
 // One CTA per token.
@@ -34,8 +49,8 @@ template <class W, class Y>
 __global__ void __launch_bounds__(kEmbedThreads) lookup_kernel(const EmbedArgs a, const W *w, Y *y)
 {
     for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-        const int64_t v = token_at(a, t);
-        Y *row = y + row_at(a, t);
+        const int64_t v = token_at(a, static_cast<uint32_t>(t));
+        Y *row = y + row_at(a, static_cast<uint32_t>(t));
         const bool inside = v >= 0 && v < a.vocab;
         if (!inside && threadIdx.x == 0) atomicOr(a.status, kStatusToken);
         for (int64_t j = threadIdx.x; j < a.dim; j += kEmbedThreads)
@@ -43,36 +58,504 @@ __global__ void __launch_bounds__(kEmbedThreads) lookup_kernel(const EmbedArgs a
     }
 }
 
-// One CTA per row of the table: it goes through all tokens.
-template <class Y, class W>
-__global__ void __launch_bounds__(kEmbedThreads) grad_kernel(const EmbedArgs a, const Y *dy, W *dw, int accumulate)
+// ------------------------------------------------------------------------------- the table's gradient
+//
+// dw[v] = scale * sum of dy[t] over the t with token v: a sum over equal keys.  Tokens are sorted with their
+// positions (stable, so that each sum runs in the order of the positions), the sorted list is cut into chunks
+// of equal length, and a CTA sums a chunk's rows, one accumulator per column in registers, and stores a row of
+// dw wherever the token changes.  A token whose run crosses a chunk's border leaves a binary32 partial sum per
+// chunk instead, and combine_kernel adds those in the chunks' order.  So every row of dy is read once, a long
+// run (the tokens of a natural text are a few thousand times more frequent at the top than at the bottom) is
+// split over as many CTAs as its length asks for, and the result is a function of the inputs alone.
+//
+//   up to kClusterTokens   order_kernel: one cluster of CTAs sorts in shared memory, exchanging digit counts and
+//                          keys through distributed shared memory, while the other CTAs write the zero rows of
+//                          the tokens that do not occur (those need no order, only the set of tokens);
+//   more                   hist, scan and scatter launches per digit, then zero_kernel;
+//   then                   sum_kernel, combine_kernel.
+
+constexpr int kSortThreads = 512;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kDigits = 256;                 // of one radix pass
+constexpr int kCluster = 8;                  // CTAs that sort together
+constexpr int kMaxItems = 16;                // keys per thread of a sorting CTA
+constexpr int kOneCtaTokens = kSortThreads * 4;
+constexpr int kClusterTokens = kSortThreads * kMaxItems * kCluster;
+constexpr int kTileItems = 8;                // keys per thread of a tile of the longer sorts
+constexpr int kTile1 = kSortThreads * kTileItems;
+
+struct SortArgs {
+    EmbedArgs e;
+    uint32_t *key, *pos;       // the sorted list
+    int passes, bits;          // radix passes of `bits` bits each; keys are 0 .. vocab
+};
+
+// Key of token t: the token, or vocab (which sorts last and is ignored) where it takes no gradient.
+__device__ __forceinline__ uint32_t key_at(const EmbedArgs &a, uint32_t t, bool report)
 {
-    for (int64_t v = blockIdx.x; v < a.vocab; v += gridDim.x) {
-        for (int64_t j0 = 0; j0 < a.dim; j0 += kEmbedThreads) {
-            const int64_t j = j0 + threadIdx.x;
-            float sum = 0.0f;
-            bool any = false;
-            if (v != a.padding)
-                for (int64_t t = 0; t < a.n; ++t)
-                    if (token_at(a, t) == v) {
-                        any = true;
-                        if (j < a.dim) sum = __fadd_rn(sum, to_f32(dy[row_at(a, t) + j]));
-                    }
-            if (j < a.dim && (any || !accumulate)) {
-                W &out = dw[v * a.table_stride + j];
-                sum = __fmul_rn(sum, a.scale);
-                out = from_f32<W>(accumulate ? __fadd_rn(to_f32(out), sum) : sum);
+    const int64_t v = token_at(a, t);
+    const bool inside = v >= 0 && v < a.vocab;
+    if (report && !inside) atomicOr(a.status, kStatusToken);
+    return static_cast<uint32_t>(inside && v != a.padding ? v : a.vocab);
+}
+
+// Ranks of a CTA's keys within their digit.  Warp w holds the kSortThreads / 32 * ITEMS slots from w * 32 * ITEMS
+// on, slot 32 i + lane in item i.  On return rank[i] counts the equal digits before it in its warp, and
+// hist[w][d] those of the warps before; total[d] is the CTA's count.  Both are complete after the next barrier.
+template <int ITEMS>
+__device__ __forceinline__ void rank_digits(const uint32_t (&digit)[ITEMS], uint32_t (&rank)[ITEMS], uint32_t (*hist)[kDigits],
+                                            uint32_t *total, int digits)
+{
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int d = lane; d < digits; d += 32) hist[w][d] = 0;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t peers = __match_any_sync(0xffffffffu, digit[i]);
+        const int leader = __ffs(peers) - 1;
+        uint32_t before = 0;
+        if (lane == leader) {
+            before = hist[w][digit[i]];
+            hist[w][digit[i]] = before + __popc(peers);
+        }
+        rank[i] = __shfl_sync(0xffffffffu, before, leader) + __popc(peers & ((1u << lane) - 1u));
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int k = 0; k < kSortWarps; ++k) {
+            const uint32_t n = hist[k][d];
+            hist[k][d] = sum;
+            sum += n;
+        }
+        total[d] = sum;
+    }
+}
+
+// base[d] <- the sum of count over the smaller digits + add, for threads d < kDigits (count 0 above `digits`).
+__device__ __forceinline__ void scan_digits(uint32_t count, uint32_t add, uint32_t *base, uint32_t *warp_sums)
+{
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    uint32_t sum = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+    }
+    if (threadIdx.x < kDigits && lane == 31) warp_sums[w] = sum;
+    __syncthreads();
+    if (threadIdx.x < kDigits) {
+        for (int k = 0; k < w; ++k) sum += warp_sums[k];
+        base[threadIdx.x] = sum - count + add;
+    }
+    __syncthreads();
+}
+
+// The table that zero rows are written to: all of its types have an all-zero 0.
+struct ZeroTable {
+    unsigned char *dw;
+    int elem;  // bytes
+};
+
+// A row of `bytes` zeros (elements of 2 or 4 bytes), by one warp.
+__device__ __forceinline__ void zero_row(unsigned char *p, int64_t bytes)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t head = min(bytes, static_cast<int64_t>(-reinterpret_cast<uintptr_t>(p) & 15)), body = (bytes - head) / 16;
+    uint4 *q = reinterpret_cast<uint4 *>(p + head);
+    for (int64_t j = lane; j < body; j += 32) q[j] = make_uint4(0, 0, 0, 0);
+    const int64_t tail = head + 16 * body;  // at most 15 bytes on either side
+    const int64_t at = lane < 8 ? lane * 2 : tail + (lane - 8) * 2, end = lane < 8 ? head : bytes;
+    if (lane < 16 && at < end) *reinterpret_cast<uint16_t *>(p + at) = 0;
+}
+
+// Zero rows of the tokens in [row0, row1) that do not occur.  mark(lo, hi, set) calls set(v) for every token v of
+// [lo, hi) that does.
+template <class Mark>
+__device__ __forceinline__ void zero_rows(const EmbedArgs &a, const ZeroTable &z, int64_t row0, int64_t row1, uint32_t *bits,
+                                          int64_t bit_words, Mark mark)
+{
+    const int w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    for (int64_t lo = row0; lo < row1; lo += bit_words * 32) {
+        const int64_t hi = min(row1, lo + bit_words * 32);
+        const int64_t words = (hi - lo + 31) / 32;
+        for (int64_t i = threadIdx.x; i < words; i += blockDim.x) bits[i] = 0;
+        __syncthreads();
+        mark(lo, hi, [&](int64_t v) {
+            const uint32_t bit = 1u << ((v - lo) & 31);
+            uint32_t &word = bits[(v - lo) >> 5];
+            if (!(*static_cast<volatile uint32_t *>(&word) & bit)) atomicOr(&word, bit);
+        });
+        __syncthreads();
+        for (int64_t v = lo + w; v < hi; v += warps)
+            if (!(bits[(v - lo) >> 5] >> ((v - lo) & 31) & 1u))
+                zero_row(z.dw + v * a.table_stride * z.elem, a.dim * z.elem);
+        __syncthreads();
+    }
+}
+
+// Shared memory of a sorting CTA: two buffers of its keys and positions, the warps' digit counts and the CTA's.
+template <int ITEMS>
+constexpr size_t kSortSmem = size_t{2} * ITEMS * kSortThreads * 8 + (kSortWarps * kDigits + 2 * kDigits + 32) * 4;
+
+template <int ITEMS>
+__global__ void __launch_bounds__(kSortThreads) order_kernel(const SortArgs a, const ZeroTable z, int64_t rows_per_cta)
+{
+    namespace cg = cooperative_groups;
+    pdl_trigger();
+    extern __shared__ __align__(16) unsigned char smem[];
+    cg::cluster_group cluster = cg::this_cluster();
+    const unsigned ctas = cluster.num_blocks();
+    const uint32_t n = static_cast<uint32_t>(a.e.n);
+    if (blockIdx.x >= ctas) {  // not the sorting cluster: zero rows
+        const int64_t row0 = static_cast<int64_t>(blockIdx.x - ctas) * rows_per_cta;
+        zero_rows(a.e, z, row0, min(a.e.vocab, row0 + rows_per_cta), reinterpret_cast<uint32_t *>(smem),
+                  static_cast<int64_t>(kSortSmem<ITEMS> / 4), [&](int64_t lo, int64_t hi, auto set) {
+#pragma unroll 4
+                      for (uint32_t t = threadIdx.x; t < n; t += kSortThreads) {
+                          const int64_t v = token_at(a.e, t);
+                          if (v >= lo && v < hi && v != a.e.padding) set(v);
+                      }
+                  });
+        return;
+    }
+    constexpr uint32_t kKeys = ITEMS * kSortThreads;  // of a CTA
+    uint2 *buf = reinterpret_cast<uint2 *>(smem);
+    auto hist = reinterpret_cast<uint32_t(*)[kDigits]>(smem + size_t{2} * kKeys * 8);
+    uint32_t *total = &hist[kSortWarps][0], *base = total + kDigits, *warp_sums = base + kDigits;
+    const uint32_t me = cluster.block_rank(), slot0 = (threadIdx.x >> 5) * 32 * ITEMS + (threadIdx.x & 31);
+    const int digits = 1 << a.bits;
+    uint2 item[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {  // slots beyond the tokens sort last
+        const uint32_t t = me * kKeys + slot0 + 32 * i;
+        item[i] = make_uint2(t < n ? key_at(a.e, t, true) : 0xffffffffu, t);
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        uint32_t digit[ITEMS], rank[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) digit[i] = (item[i].x >> (pass * a.bits)) & (digits - 1);
+        rank_digits(digit, rank, hist, total, digits);
+        cluster.sync();  // every CTA's total
+        uint32_t before = 0, all = 0;
+        if (threadIdx.x < digits)
+            for (unsigned c = 0; c < ctas; ++c) {
+                const uint32_t m = cluster.map_shared_rank(total, c)[threadIdx.x];
+                before += c < me ? m : 0;
+                all += m;
             }
+        scan_digits(all, before, base, warp_sums);
+        const bool last = pass + 1 == a.passes;
+        uint2 *to = buf + (pass & 1) * kKeys;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const uint32_t at = base[digit[i]] + hist[threadIdx.x >> 5][digit[i]] + rank[i];
+            if (!last) {
+                cluster.map_shared_rank(to, at / kKeys)[at % kKeys] = item[i];
+            } else if (at < n) {
+                a.key[at] = item[i].x;
+                a.pos[at] = item[i].y;
+            }
+        }
+        cluster.sync();  // every CTA's keys have arrived, and its total has been read
+        if (!last)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) item[i] = to[slot0 + 32 * i];
+    }
+}
+
+// The longer sorts.  hist is digit-major: hist[d * tiles + tile].
+struct TileSortArgs {
+    EmbedArgs e;
+    const uint32_t *key_in, *pos_in;  // null in the first pass, which forms them
+    uint32_t *key, *pos;
+    uint32_t *hist, *total;
+    uint32_t tiles;
+    int shift, bits;
+};
+
+template <int ITEMS>
+__device__ __forceinline__ void load_tile(const TileSortArgs &a, uint2 (&item)[ITEMS], uint32_t (&digit)[ITEMS], bool report)
+{
+    const uint32_t slot0 = blockIdx.x * kTile1 + (threadIdx.x >> 5) * 32 * ITEMS + (threadIdx.x & 31);
+    const uint32_t n = static_cast<uint32_t>(a.e.n);
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const uint32_t t = slot0 + 32 * i;
+        item[i] = make_uint2(0xffffffffu, t);
+        if (t < n) item[i] = a.key_in ? make_uint2(a.key_in[t], a.pos_in[t]) : make_uint2(key_at(a.e, t, report), t);
+        digit[i] = (item[i].x >> a.shift) & ((1u << a.bits) - 1);
+    }
+}
+
+__global__ void __launch_bounds__(kSortThreads) hist_kernel(const TileSortArgs a)
+{
+    __shared__ uint32_t count[kDigits];
+    pdl_trigger();
+    if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+    pdl_wait();
+    __syncthreads();
+    uint2 item[kTileItems];
+    uint32_t digit[kTileItems];
+    load_tile(a, item, digit, true);
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i) {
+        const uint32_t peers = __match_any_sync(0xffffffffu, digit[i]);
+        if ((threadIdx.x & 31) == __ffs(peers) - 1) atomicAdd(&count[digit[i]], static_cast<uint32_t>(__popc(peers)));
+    }
+    __syncthreads();
+    if (threadIdx.x < (1u << a.bits)) a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] = count[threadIdx.x];
+}
+
+// One CTA per digit: its counts become exclusive sums over the tiles, total[d] their sum.
+__global__ void __launch_bounds__(kSortThreads) scan_kernel(uint32_t *hist, uint32_t *total, uint32_t tiles)
+{
+    __shared__ uint32_t warp_sums[kSortWarps];
+    pdl_trigger();
+    pdl_wait();
+    uint32_t *row = hist + static_cast<size_t>(blockIdx.x) * tiles, carry = 0;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    for (uint32_t i0 = 0; i0 < tiles; i0 += kSortThreads) {
+        const uint32_t i = i0 + threadIdx.x, v = i < tiles ? row[i] : 0;
+        uint32_t sum = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        if (lane == 31) warp_sums[w] = sum;
+        __syncthreads();
+        uint32_t before = carry, all = 0;
+#pragma unroll
+        for (int k = 0; k < kSortWarps; ++k) {
+            before += k < w ? warp_sums[k] : 0;
+            all += warp_sums[k];
+        }
+        if (i < tiles) row[i] = before + sum - v;
+        carry += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) total[blockIdx.x] = carry;
+}
+
+__global__ void __launch_bounds__(kSortThreads) scatter_kernel(const TileSortArgs a)
+{
+    __shared__ uint32_t hist[kSortWarps][kDigits], total[kDigits], base[kDigits], warp_sums[kDigits / 32];
+    pdl_trigger();
+    pdl_wait();
+    uint2 item[kTileItems];
+    uint32_t digit[kTileItems], rank[kTileItems];
+    load_tile(a, item, digit, false);
+    const int digits = 1 << a.bits;
+    rank_digits(digit, rank, hist, total, digits);
+    const bool mine = threadIdx.x < digits;
+    scan_digits(mine ? a.total[threadIdx.x] : 0, mine ? a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] : 0, base,
+                warp_sums);
+    const uint32_t n = static_cast<uint32_t>(a.e.n);
+#pragma unroll
+    for (int i = 0; i < kTileItems; ++i) {
+        const uint32_t at = base[digit[i]] + hist[threadIdx.x >> 5][digit[i]] + rank[i];
+        if (at < n) {  // the last tile's empty slots come last
+            a.key[at] = item[i].x;
+            a.pos[at] = item[i].y;
         }
     }
 }
 
-__global__ void __launch_bounds__(kEmbedThreads) check_tokens_kernel(const EmbedArgs a)
+__device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t n, int64_t v)
 {
-    for (int64_t t = blockIdx.x * static_cast<int64_t>(kEmbedThreads) + threadIdx.x; t < a.n;
-         t += static_cast<int64_t>(gridDim.x) * kEmbedThreads) {
-        const int64_t v = token_at(a, t);
-        if (v < 0 || v >= a.vocab) atomicOr(a.status, kStatusToken);
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (key[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+constexpr int kZeroWords = 8192;
+
+// The zero rows, from a sorted list of the tokens.
+__global__ void __launch_bounds__(kSortThreads) zero_kernel(const EmbedArgs a, const uint32_t *key, const ZeroTable z, int64_t rows_per_cta)
+{
+    __shared__ uint32_t bits[kZeroWords];
+    pdl_trigger();
+    pdl_wait();
+    const int64_t row0 = blockIdx.x * rows_per_cta;
+    zero_rows(a, z, row0, min(a.vocab, row0 + rows_per_cta), bits, kZeroWords, [&](int64_t lo, int64_t hi, auto set) {
+        const int64_t end = lower_bound(key, a.n, hi);
+        for (int64_t i = lower_bound(key, a.n, lo) + threadIdx.x; i < end; i += kSortThreads) set(key[i]);
+    });
+}
+
+struct SumArgs {
+    EmbedArgs e;
+    const uint32_t *key, *pos;
+    float *partial;       // chunk c's head at 2 c * pad, its tail at (2 c + 1) * pad
+    int64_t pad;          // columns of a partial sum, a multiple of 8
+    int64_t chunk;        // entries of the list per chunk
+    int accumulate;
+};
+
+template <class Y, int VEC>
+struct alignas(VEC > 1 ? 16 : sizeof(Y)) Pack {
+    Y y[VEC];
+};
+template <class Y, int VEC>
+__device__ __forceinline__ void load_pack(const Y *p, Pack<Y, VEC> &out)
+{
+    if constexpr (VEC > 1) *reinterpret_cast<uint4 *>(&out) = *reinterpret_cast<const uint4 *>(p);
+    else out.y[0] = *p;
+}
+
+template <class W, int VEC>
+__device__ __forceinline__ void store_sums(W *p, const float (&sum)[VEC], float scale, int accumulate)
+{
+    if constexpr (VEC == 1) {
+        const float x = __fmul_rn(sum[0], scale);
+        *p = from_f32<W>(accumulate ? __fadd_rn(to_f32(*p), x) : x);
+    } else {
+        constexpr int kBytes = VEC * sizeof(W), kWord = kBytes >= 16 ? 16 : 8;
+        constexpr int kPer = kWord / sizeof(W);
+#pragma unroll
+        for (int k = 0; k < VEC; k += kPer) {
+            using Word = typename std::conditional<kWord == 16, uint4, uint2>::type;
+            alignas(16) Word word;
+            W *x = reinterpret_cast<W *>(&word);
+            if (accumulate) word = *reinterpret_cast<const Word *>(p + k);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float s = __fmul_rn(sum[k + i], scale);
+                x[i] = from_f32<W>(accumulate ? __fadd_rn(to_f32(x[i]), s) : s);
+            }
+            *reinterpret_cast<Word *>(p + k) = word;
+        }
+    }
+}
+
+constexpr int kSumThreads = 256;
+constexpr int kSumRows = 128;   // entries of the list that a CTA holds in shared memory at a time
+constexpr int kSumUnroll = 8;   // rows in flight per thread
+
+template <class Y, class W, int VEC>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const Y *dy, W *dw)
+{
+    __shared__ uint32_t keys[kSumRows];
+    __shared__ int64_t rows[kSumRows];
+    pdl_trigger();
+    pdl_wait();
+    const int64_t begin = blockIdx.x * a.chunk, end = min(a.e.n, begin + a.chunk);
+    const int64_t j = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * VEC;
+    const uint32_t none = static_cast<uint32_t>(a.e.vocab);
+    const bool in = j < a.e.dim;
+    const uint32_t first = a.key[begin];
+    if (first == none) return;  // nothing but tokens without a gradient from here on
+    const bool head = begin > 0 && a.key[begin - 1] == first;
+    const uint32_t after = end < a.e.n ? a.key[end] : none;  // the token that the chunk's last run may go on with
+    float *part = a.partial + 2 * blockIdx.x * a.pad + j;
+    float sum[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) sum[k] = 0.0f;
+    uint32_t cur = first;
+    bool from_head = head;
+    auto flush = [&](bool goes_on) {
+        if (in) {
+            if (from_head || goes_on) {
+                float *p = part + (from_head ? 0 : a.pad);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) p[k] = sum[k];
+            } else {
+                store_sums<W, VEC>(dw + cur * a.e.table_stride + j, sum, a.e.scale, a.accumulate);
+            }
+        }
+    };
+    for (int64_t b = begin; b < end; b += kSumRows) {
+        const int n = static_cast<int>(min(end - b, static_cast<int64_t>(kSumRows)));
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            keys[i] = a.key[b + i];
+            rows[i] = row_at(a.e, a.pos[b + i]);
+        }
+        __syncthreads();
+        for (int i = 0; i < n; i += kSumUnroll) {
+            Pack<Y, VEC> x[kSumUnroll];
+#pragma unroll
+            for (int u = 0; u < kSumUnroll; ++u)
+                if (in && i + u < n && keys[i + u] != none) load_pack<Y, VEC>(dy + rows[i + u] + j, x[u]);
+#pragma unroll
+            for (int u = 0; u < kSumUnroll; ++u) {
+                if (i + u >= n) break;
+                const uint32_t k = keys[i + u];
+                if (k != cur) {
+                    flush(false);
+                    cur = k;
+                    from_head = false;
+#pragma unroll
+                    for (int v = 0; v < VEC; ++v) sum[v] = 0.0f;
+                    if (k == none) return;
+                }
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) sum[v] = __fadd_rn(sum[v], to_f32(x[u].y[v]));
+            }
+        }
+    }
+    flush(after == cur);
+}
+
+constexpr int kCombineThreads = 256, kCombineSplit = 4;
+
+// The rows of the tokens whose runs cross chunks.  CTA (c, y) takes the run that starts in chunk c and goes on in
+// the next, if there is one -- the tail of c and the heads of the chunks after it, as far as the run goes -- and
+// every kCombineSplit-th piece of its columns.  A long run is split over up to eight groups of
+// threads, which take its chunks in turn and are added in order.
+template <class W>
+__global__ void __launch_bounds__(kCombineThreads) combine_kernel(const SumArgs a, W *dw)
+{
+    __shared__ float4 red[kCombineThreads];
+    pdl_wait();
+    const int64_t c = blockIdx.x, begin = c * a.chunk, next = begin + a.chunk;  // c is not the last chunk
+    const uint32_t v = a.key[next];
+    const bool starts = a.key[begin] != v || begin == 0 || a.key[begin - 1] != v;
+    if (v == static_cast<uint32_t>(a.e.vocab) || a.key[next - 1] != v || !starts) return;
+    int64_t last = c + 1;  // the chunks whose first entry is v: c + 1 .. last
+    for (int64_t k = c + 2;; k += 32) {
+        const int64_t at = (k + (threadIdx.x & 31)) * a.chunk;
+        const uint32_t same = __ballot_sync(0xffffffffu, at < a.e.n && a.key[at] == v);
+        const int run = same == 0xffffffffu ? 32 : __ffs(~same) - 1;
+        last += run;
+        if (run < 32) break;
+    }
+    const int64_t parts = last - c;
+    const int groups = parts >= 16 ? 8 : parts >= 8 ? 4 : parts >= 4 ? 2 : 1, width = kCombineThreads / groups;
+    const int group = threadIdx.x / width, lane = threadIdx.x % width;
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * width * 4; j0 < a.e.dim; j0 += static_cast<int64_t>(kCombineSplit) * width * 4) {
+        const int64_t j = j0 + lane * 4;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (j < a.e.dim) {
+            if (group == 0) sum = *reinterpret_cast<const float4 *>(a.partial + (2 * c + 1) * a.pad + j);
+#pragma unroll 4
+            for (int64_t k = c + 1 + group; k <= last; k += groups) {
+                const float4 x = *reinterpret_cast<const float4 *>(a.partial + 2 * k * a.pad + j);
+                sum = make_float4(__fadd_rn(sum.x, x.x), __fadd_rn(sum.y, x.y), __fadd_rn(sum.z, x.z), __fadd_rn(sum.w, x.w));
+            }
+        }
+        if (groups > 1) {
+            __syncthreads();
+            red[threadIdx.x] = sum;
+            __syncthreads();
+        }
+        if (group == 0) {
+            for (int g = 1; g < groups; ++g) {
+                const float4 x = red[g * width + lane];
+                sum = make_float4(__fadd_rn(sum.x, x.x), __fadd_rn(sum.y, x.y), __fadd_rn(sum.z, x.z), __fadd_rn(sum.w, x.w));
+            }
+            const float s[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (j + i < a.e.dim) store_sums<W, 1>(dw + v * a.e.table_stride + j + i, {s[i]}, a.e.scale, a.accumulate);
+        }
     }
 }
 
@@ -85,6 +568,9 @@ struct ea_embed {
     cudaStream_t stream = nullptr;
     ea_embed_config cfg{};
     uint32_t *status = nullptr;
+    uint32_t *key[2] = {}, *pos[2] = {};  // the sorted list; the second pair, hist and total: longer sorts only
+    uint32_t *hist = nullptr, *total = nullptr;
+    float *partial = nullptr;
 };
 
 namespace {
@@ -93,14 +579,62 @@ int validate(const ea_embed_config *cfg)
 {
     if (!cfg) return lm_fail(EA_E_INVAL, "config is NULL");
     if (cfg->vocab < 1 || cfg->vocab > 0x7ffffffeLL) return lm_fail(EA_E_INVAL, "vocab must be in [1, 2^31 - 2]");
-    if (cfg->dim < 1 || cfg->dim > (1 << 24)) return lm_fail(EA_E_INVAL, "dim must be in [1, 2^24]");
+    if (cfg->dim < 1 || cfg->dim > (1 << 20)) return lm_fail(EA_E_INVAL, "dim must be in [1, 2^20]");
     if (cfg->max_tokens < 0 || cfg->max_tokens > (1 << 30)) return lm_fail(EA_E_INVAL, "max_tokens must be in [0, 2^30]");
     if (cfg->padding < -1 || cfg->padding >= cfg->vocab) return lm_fail(EA_E_INVAL, "padding must be a token or -1");
     if (!std::isfinite(cfg->scale)) return lm_fail(EA_E_INVAL, "scale must be finite");
     return EA_OK;
 }
 
-size_t embed_bytes(const ea_embed_config &) { return 256; }
+constexpr int kMaxVec = 8;
+constexpr int kMinChunk = 8;
+
+int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+int64_t over(int64_t x, int64_t a) { return (x + a - 1) / a; }
+
+// How sum_kernel's CTAs share the columns: `slabs` of them side by side, of `threads` threads.
+struct SumShape {
+    int64_t slabs;
+    int threads;
+    SumShape(int64_t dim, int vec)
+    {
+        const int64_t packs = over(dim, vec);
+        slabs = over(packs, kSumThreads);
+        threads = static_cast<int>(up(over(packs, slabs), 32));
+    }
+};
+
+// Entries of the sorted list per chunk: about 16 CTAs' worth of chunks per SM, slabs counted, and no fewer than
+// kMinChunk rows (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
+int64_t chunk_length(int64_t n, int64_t slabs, int sms)
+{
+    const int64_t most = std::max<int64_t>(1, sms * 16 / slabs);
+    return std::max<int64_t>(kMinChunk, over(n, most));
+}
+
+struct EmbedLayout {
+    size_t status, list, hist, total_, partial;
+    int lists;
+    size_t total() const { return status + 2 * lists * list + hist + total_ + partial; }
+};
+
+EmbedLayout embed_layout(const ea_embed_config &cfg)
+{
+    const int64_t n = cfg.max_tokens;
+    EmbedLayout l{};
+    l.status = 256;
+    l.list = up(n * 4, 256);
+    l.lists = n > kClusterTokens ? 2 : 1;
+    if (n > kClusterTokens) {
+        l.hist = up(over(n, kTile1) * kDigits * 4, 256);
+        l.total_ = kDigits * 4;
+    }
+    // the most chunks that chunk_length allows at any number of tokens
+    const int64_t slabs = SumShape(cfg.dim, kMaxVec).slabs;
+    const int64_t chunks = std::min(over(n, kMinChunk), std::max<int64_t>(1, kMaxSms * 16 / slabs));
+    l.partial = 2 * chunks * up(cfg.dim, kMaxVec) * 4;
+    return l;
+}
 
 // Checks a call and fills in the kernels' arguments.
 int embed_args(const ea_embed *h, const ea_embed_call *c, const void *tokens, const void *rows, const void *table,
@@ -122,8 +656,30 @@ int embed_args(const ea_embed *h, const ea_embed_call *c, const void *tokens, co
     }
     if (r == EA_OK) r = h->dev.check();
     if (r != EA_OK) return r;
-    a = EmbedArgs{c->outer * c->inner, c->inner, c->token_outer, c->token_inner, c->row_outer, c->row_inner, c->table_stride,
-                  h->cfg.vocab, h->cfg.dim, h->cfg.padding, h->cfg.scale, c->token_type == EA_T_I64, tokens, h->status};
+    a = EmbedArgs{};
+    a.n = c->outer * c->inner;
+    a.token_outer = c->token_outer;
+    a.token_inner = c->token_inner;
+    a.row_outer = c->row_outer;
+    a.row_inner = c->row_inner;
+    if (c->inner == 1) {  // a column of the batch is a row of it
+        a.token_inner = c->token_outer;
+        a.row_inner = c->row_outer;
+    } else if (c->outer > 1 && (c->token_outer != c->inner * c->token_inner || c->row_outer != c->inner * c->row_inner)) {
+        int s = 0;
+        while ((int64_t{1} << s) < c->inner) ++s;
+        a.inner = static_cast<uint32_t>(c->inner);
+        a.magic = static_cast<uint32_t>((uint64_t{1} << (31 + s)) / static_cast<uint64_t>(c->inner) + 1);
+        a.shift = s - 1;
+    }
+    a.table_stride = c->table_stride;
+    a.vocab = h->cfg.vocab;
+    a.dim = h->cfg.dim;
+    a.padding = h->cfg.padding;
+    a.scale = h->cfg.scale;
+    a.token64 = c->token_type == EA_T_I64;
+    a.tokens = tokens;
+    a.status = h->status;
     return EA_OK;
 }
 
@@ -138,6 +694,71 @@ void with_type(int32_t type, F f)
     }
 }
 
+// Whether every row of a tensor starts on a 16-byte boundary and is whole vectors of it.
+bool rows_aligned(const void *p, int32_t type, int64_t dim, int64_t outer, int64_t inner)
+{
+    const int64_t vec = 16 / static_cast<int64_t>(type_bytes(type));
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && dim % vec == 0 && outer % vec == 0 && inner % vec == 0;
+}
+
+// f(std::integral_constant<int, ITEMS>) for the keys per thread that n tokens take in a cluster of `ctas`.
+template <class F>
+void with_items(int64_t n, int ctas, F f)
+{
+    const int64_t items = over(n, int64_t{kSortThreads} * ctas);
+    if (items <= 1) f(std::integral_constant<int, 1>());
+    else if (items <= 2) f(std::integral_constant<int, 2>());
+    else if (items <= 4) f(std::integral_constant<int, 4>());
+    else if (items <= 8) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, kMaxItems>());
+}
+
+int allow_sort_smem()
+{
+    auto allow = [](auto *kernel, size_t bytes) {
+        return lm_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)), "shared memory");
+    };
+    int r = allow(order_kernel<4>, kSortSmem<4>);
+    if (r == EA_OK) r = allow(order_kernel<8>, kSortSmem<8>);
+    if (r == EA_OK) r = allow(order_kernel<kMaxItems>, kSortSmem<kMaxItems>);
+    return r;
+}
+
+// The sorted list of the tokens into h.key[0], h.pos[0]; with `zero`, the rows of dw whose token does not occur.
+cudaError_t order_tokens(ea_embed &h, const EmbedArgs &a, const ZeroTable &z, bool zero)
+{
+    int key_bits = 1;
+    while ((a.vocab >> key_bits) != 0) ++key_bits;  // keys are 0 .. vocab
+    const int passes = static_cast<int>(over(key_bits, 8)), bits = static_cast<int>(over(key_bits, passes));
+    cudaError_t e = cudaSuccess;
+    if (a.n <= kClusterTokens) {
+        const int ctas = a.n <= kOneCtaTokens ? 1 : kCluster;
+        const int64_t rows = over(a.vocab, h.dev.sms), zero_ctas = zero ? up(over(a.vocab, rows), ctas) : 0;
+        with_items(a.n, ctas, [&](auto items) {
+            constexpr int kItems = decltype(items)::value;
+            const SortArgs s{a, h.key[0], h.pos[0], passes, bits};
+            e = launch_lm(order_kernel<kItems>, dim3(static_cast<unsigned>(ctas + zero_ctas)), kSortThreads, kSortSmem<kItems>, h.stream,
+                          false, ctas, s, z, rows);
+        });
+        return e;
+    }
+    const unsigned tiles = static_cast<unsigned>(over(a.n, kTile1));
+    for (int pass = 0; pass < passes && e == cudaSuccess; ++pass) {
+        const int to = (passes - 1 - pass) & 1;  // the last pass writes the first pair
+        TileSortArgs s{a, pass ? h.key[to ^ 1] : nullptr, pass ? h.pos[to ^ 1] : nullptr, h.key[to], h.pos[to], h.hist, h.total, tiles,
+                       pass * bits, bits};
+        e = launch_lm(hist_kernel, dim3(tiles), kSortThreads, 0, h.stream, pass > 0, 1, s);
+        if (e == cudaSuccess) e = launch_lm(scan_kernel, dim3(1u << bits), kSortThreads, 0, h.stream, true, 1, h.hist, h.total, tiles);
+        if (e == cudaSuccess) e = launch_lm(scatter_kernel, dim3(tiles), kSortThreads, 0, h.stream, true, 1, s);
+    }
+    if (e == cudaSuccess && zero) {
+        const int64_t rows = over(a.vocab, h.dev.sms * 4);
+        e = launch_lm(zero_kernel, dim3(static_cast<unsigned>(over(a.vocab, rows))), kSortThreads, 0, h.stream, true, 1, a,
+                      static_cast<const uint32_t *>(h.key[0]), z, rows);
+    }
+    return e;
+}
+
 }  // namespace
 
 extern "C" {
@@ -147,7 +768,7 @@ int ea_embed_workspace_bytes(const ea_embed_config *cfg, size_t *bytes)
     if (!bytes) return lm_fail(EA_E_INVAL, "bytes is NULL");
     const int r = validate(cfg);
     if (r != EA_OK) return r;
-    *bytes = embed_bytes(*cfg);
+    *bytes = embed_layout(*cfg).total();
     return EA_OK;
 }
 
@@ -157,13 +778,29 @@ int ea_embed_init(const ea_embed_config *cfg, void *workspace, size_t workspace_
     *out = nullptr;
     int r = validate(cfg);
     if (r != EA_OK) return r;
-    if ((r = check_workspace(workspace, workspace_bytes, embed_bytes(*cfg))) != EA_OK) return r;
+    if ((r = check_workspace(workspace, workspace_bytes, embed_layout(*cfg).total())) != EA_OK) return r;
     ea_embed *h = new (std::nothrow) ea_embed;
     if (!h) return lm_fail(EA_E_INVAL, "out of host memory");
     h->cfg = *cfg;
     h->stream = static_cast<cudaStream_t>(stream);
-    h->status = static_cast<uint32_t *>(workspace);
+    const EmbedLayout l = embed_layout(*cfg);
+    unsigned char *p = static_cast<unsigned char *>(workspace);
+    auto take = [&p](size_t bytes) {
+        unsigned char *q = p;
+        p += bytes;
+        return q;
+    };
+    h->status = reinterpret_cast<uint32_t *>(take(l.status));
+    for (int i = 0; i < l.lists; ++i) {
+        h->key[i] = reinterpret_cast<uint32_t *>(take(l.list));
+        h->pos[i] = reinterpret_cast<uint32_t *>(take(l.list));
+    }
+    h->hist = reinterpret_cast<uint32_t *>(take(l.hist));
+    h->total = reinterpret_cast<uint32_t *>(take(l.total_));
+    h->partial = reinterpret_cast<float *>(take(l.partial));
     r = h->dev.query();
+    h->dev.sms = std::min(h->dev.sms, kMaxSms);
+    if (r == EA_OK) r = allow_sort_smem();
     if (r == EA_OK) r = lm_cuda(cudaMemsetAsync(h->status, 0, 4, h->stream), "status clear");
     if (r != EA_OK) {
         delete h;
@@ -193,14 +830,30 @@ int ea_embed_grad(ea_embed *h, const ea_embed_call *c, const void *tokens, const
     EmbedArgs a;
     const int r = embed_args(h, c, tokens, dy, dw, a);
     if (r != EA_OK) return r;
+    if (a.n == 0 && accumulate) return EA_OK;
+    const int wb = static_cast<int>(type_bytes(c->table_type));
+    const ZeroTable z{static_cast<unsigned char *>(dw), wb};
+    cudaError_t e = order_tokens(*h, a, z, !accumulate);
+    if (e != cudaSuccess || a.n == 0) return lm_cuda(e, "launch");
+    const int vec = rows_aligned(dy, c->row_type, a.dim, c->outer > 1 ? c->row_outer : 0, c->inner > 1 ? c->row_inner : 0) &&
+                            rows_aligned(dw, c->table_type, a.dim, a.table_stride, 0)
+                        ? 16 / static_cast<int>(type_bytes(c->row_type)) : 1;
+    const SumShape shape(a.dim, vec);
+    SumArgs s{a, h->key[0], h->pos[0], h->partial, up(a.dim, kMaxVec), chunk_length(a.n, shape.slabs, h->dev.sms), accumulate};
+    const unsigned chunks = static_cast<unsigned>(over(a.n, s.chunk));
     with_type(c->row_type, [&](auto *yt) {
+        using Y = std::remove_reference_t<decltype(*yt)>;
         with_type(c->table_type, [&](auto *wt) {
-            grad_kernel<<<static_cast<unsigned>(std::min<int64_t>(a.vocab, 1 << 20)), kEmbedThreads, 0, h->stream>>>(
-                a, static_cast<decltype(yt)>(const_cast<void *>(dy)), static_cast<decltype(wt)>(dw), accumulate);
+            using W = std::remove_reference_t<decltype(*wt)>;
+            const dim3 grid(chunks, static_cast<unsigned>(shape.slabs));
+            auto kernel = vec > 1 ? sum_kernel<Y, W, 16 / sizeof(Y)> : sum_kernel<Y, W, 1>;
+            e = launch_lm(kernel, grid, shape.threads, 0, h->stream, true, 1, s, static_cast<const Y *>(dy), static_cast<W *>(dw));
+            if (e == cudaSuccess && chunks > 1)
+                e = launch_lm(combine_kernel<W>, dim3(chunks - 1, kCombineSplit), kCombineThreads, 0, h->stream, true, 1, s,
+                              static_cast<W *>(dw));
         });
     });
-    if (a.n) check_tokens_kernel<<<static_cast<unsigned>(std::min<int64_t>((a.n + 255) / 256, 1024)), kEmbedThreads, 0, h->stream>>>(a);
-    return lm_cuda(cudaGetLastError(), "launch");
+    return lm_cuda(e, "launch");
 }
 
 int ea_embed_sync_status(ea_embed *h)

@@ -11,6 +11,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "ea_internal.h"
@@ -92,6 +93,33 @@ struct DeviceOf {
 
 // SMs that a workspace is sized for (a handle uses no more of them).
 constexpr int kMaxSms = 160;
+
+// Launch `kernel` in clusters of `cluster` CTAs; with `overlap`, it may begin before its predecessor has finished
+// (programmatic dependent launch; see pdl_wait).
+template <class... KArgs, class... Args>
+cudaError_t launch_lm(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t s, bool overlap, int cluster, Args &&...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(block));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    unsigned n = 0;
+    if (overlap) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = static_cast<unsigned>(cluster);
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
 
 // Tensors whose gradients one launch carries as a parameter.
 constexpr int kGradBatch = 448;
