@@ -9,6 +9,7 @@
 namespace ea {
 
 constexpr int kAdamThreads = 256;
+constexpr int kAdamCtasPerSm = 3;  // 85 registers per thread; a persistent grid of them
 constexpr int kBlock = EA_ADAMW_BLOCK;  // a warp's unit of work: eight coordinates per lane
 
 // What a step needs to know of the steps before it.  The last CTA of a step that is not skipped advances it.
@@ -45,9 +46,55 @@ __device__ __forceinline__ uint32_t e4m3_code(float x, float inv, uint32_t r16, 
     return code | (__float_as_uint(x) >> 31 << 7);
 }
 
-__device__ __forceinline__ float e4m3_value(uint32_t code)
+// The values of four e4m3 codes, exact.
+__device__ __forceinline__ void e4m3_values(uint32_t codes, float (&x)[4])
 {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(code), __NV_E4M3)));
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes & 0xffffu), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes >> 16), __NV_E4M3);
+    const float2 lo = __half22float2(__half2(a)), hi = __half22float2(__half2(b));
+    x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
+}
+
+// Four elements from p on, where `whole`, else those below n (the others are 0).
+template <class T>
+__device__ __forceinline__ void load_some(const T *p, int n, bool whole, float (&x)[4])
+{
+    if (whole) {
+        load4(p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < n ? to_f32(p[i]) : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_some(T *p, int n, bool whole, const float (&x)[4])
+{
+    if (whole) {
+        store4(p, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = from_f32<T>(x[i]);
+    }
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t *p, int n, bool whole)
+{
+    if (whole) return *reinterpret_cast<const uint32_t *>(p);
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) v |= static_cast<uint32_t>(p[i]) << (8 * i);
+    return v;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, bool whole, uint32_t v)
+{
+    if (whole) {
+        *reinterpret_cast<uint32_t *>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = static_cast<uint8_t>(v >> (8 * i));
+    }
 }
 
 // The exponent k of the smallest power of two >= 2^-126 with amax / 2^k <= 448 = 1.75 * 2^8.
@@ -62,68 +109,88 @@ __device__ __forceinline__ uint32_t finite_magnitude(float x)
     return b < 0x7f800000u ? b : 0u;
 }
 
+// A warp takes blocks of 256 coordinates: four consecutive ones per lane in each half, so that every access of the
+// warp is one contiguous piece, and the block's scale is one warp reduction.  All loads of a block are issued before
+// the first is used.
 template <class P, class G, class C, int BITS>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamArgs a, const __grid_constant__ GradList list)
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const AdamArgs a, const __grid_constant__ GradList list)
 {
     const int lane = threadIdx.x & 31;
     const float factor = a.clip ? a.clip[1] : 1.0f;
     const AdamState st = *a.state;
     if (!isnan(factor)) {
         const int64_t warps = static_cast<int64_t>(gridDim.x) * (kAdamThreads / 32);
+        int t = 0;
         for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kAdamThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
-            int lo = 0, hi = a.n_tensors - 1;  // the last tensor whose first block is <= u
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (a.first[mid] <= u) lo = mid;
-                else hi = mid - 1;
-            }
-            const ea_adamw_tensor &T = a.tensors[lo];
-            const int64_t block = u - a.first[lo], base = block * kBlock;
+            t = tensor_of(a.first, a.n_tensors, u, t);
+            const ea_adamw_tensor &T = a.tensors[t];
+            const int64_t block = u - a.first[t], base = block * kBlock;
             const int n = static_cast<int>(min(T.size - base, static_cast<int64_t>(kBlock)));
-            const float lr = __fmul_rn(a.lr, T.lr_scale), step = __fmul_rn(lr, st.a), rate = __fmul_rn(lr, T.weight_decay);
             P *p = static_cast<P *>(T.param) + base;
             C *copy = T.copy ? static_cast<C *>(T.copy) + base : nullptr;
-            const G *g = static_cast<const G *>(list.g[lo]) + base;
-            float m[8], v[8], root[8];
-            float ms = 1.0f, vs = 1.0f;
-            if (BITS == 8) {
+            const G *g = static_cast<const G *>(list.g[t]) + base;
+            float *m32 = static_cast<float *>(T.m) + base, *v32 = static_cast<float *>(T.v) + base;
+            uint8_t *m8 = static_cast<uint8_t *>(T.m) + base, *v8 = static_cast<uint8_t *>(T.v) + base;
+            const uintptr_t state = reinterpret_cast<uintptr_t>(T.m) | reinterpret_cast<uintptr_t>(T.v);
+            const bool vec = n == kBlock && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(P)) == 0 &&
+                             reinterpret_cast<uintptr_t>(g) % (4 * sizeof(G)) == 0 &&
+                             reinterpret_cast<uintptr_t>(copy) % (4 * sizeof(C)) == 0 && state % (BITS == 32 ? 16 : 4) == 0;
+            float pk[2][4], gk[2][4], m[2][4], v[2][4];
+            uint32_t mc[2], vc[2];
+            float ms = 0.0f, vs = 0.0f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = h * 128 + lane * 4;
+                load_some(p + j, n - j, vec, pk[h]);
+                load_some(g + j, n - j, vec, gk[h]);
+                if constexpr (BITS == 32) {
+                    load_some(m32 + j, n - j, vec, m[h]);
+                    load_some(v32 + j, n - j, vec, v[h]);
+                } else {
+                    mc[h] = load_codes(m8 + j, n - j, vec);
+                    vc[h] = load_codes(v8 + j, n - j, vec);
+                }
+            }
+            if constexpr (BITS == 8) {
                 ms = T.m_scale[block];
                 vs = T.v_scale[block];
             }
+            const float lr = __fmul_rn(a.lr, T.lr_scale), step = __fmul_rn(lr, st.a), rate = __fmul_rn(lr, T.weight_decay);
+            uint32_t am = 0, av = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int j = (k >> 2) * 128 + lane * 4 + (k & 3);
-                m[k] = v[k] = root[k] = 0.0f;
-                if (j >= n) continue;
-                const float gk = __fmul_rn(to_f32(g[j]), factor);
-                if (BITS == 32) {
-                    m[k] = static_cast<const float *>(T.m)[base + j];
-                    v[k] = static_cast<const float *>(T.v)[base + j];
-                } else {
-                    m[k] = __fmul_rn(e4m3_value(static_cast<const uint8_t *>(T.m)[base + j]), ms);
-                    const float r = __fmul_rn(e4m3_value(static_cast<const uint8_t *>(T.v)[base + j]), vs);
-                    v[k] = __fmul_rn(r, r);
+            for (int h = 0; h < 2; ++h) {
+                const int j = h * 128 + lane * 4;
+                if constexpr (BITS == 8) {
+                    e4m3_values(mc[h], m[h]);
+                    e4m3_values(vc[h], v[h]);
                 }
-                m[k] = __fadd_rn(__fmul_rn(m[k], a.beta1), __fmul_rn(gk, a.c1));
-                v[k] = __fadd_rn(__fmul_rn(v[k], a.beta2), __fmul_rn(__fmul_rn(gk, gk), a.c2));
-                root[k] = __fsqrt_rn(v[k]);
-                const float pk = to_f32(p[j]);
-                const float d = __fadd_rn(__fmul_rn(pk, rate), __fmul_rn(__fdiv_rn(m[k], __fadd_rn(root[k], st.e)), step));
-                const float q = __fsub_rn(pk, d);
-                p[j] = from_f32<P>(q);
-                if (copy) copy[j] = from_f32<C>(q);
-                if (BITS == 32) {
-                    static_cast<float *>(T.m)[base + j] = m[k];
-                    static_cast<float *>(T.v)[base + j] = v[k];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float &mi = m[h][i], &vi = v[h][i];
+                    if constexpr (BITS == 8) {
+                        mi = __fmul_rn(mi, ms);
+                        vi = __fmul_rn(vi, vs);
+                        vi = __fmul_rn(vi, vi);
+                    }
+                    const float gi = __fmul_rn(gk[h][i], factor);
+                    mi = __fadd_rn(__fmul_rn(mi, a.beta1), __fmul_rn(gi, a.c1));
+                    vi = __fadd_rn(__fmul_rn(vi, a.beta2), __fmul_rn(__fmul_rn(gi, gi), a.c2));
+                    const float root = __fsqrt_rn(vi), x = pk[h][i];
+                    pk[h][i] = __fsub_rn(x, __fadd_rn(__fmul_rn(x, rate), __fmul_rn(__fdiv_rn(mi, __fadd_rn(root, st.e)), step)));
+                    if constexpr (BITS == 8) {
+                        vi = root;
+                        am = max(am, finite_magnitude(mi));
+                        av = max(av, finite_magnitude(root));
+                    }
+                }
+                store_some(p + j, n - j, vec, pk[h]);
+                if (copy) store_some(copy + j, n - j, vec, pk[h]);
+                if constexpr (BITS == 32) {
+                    store_some(m32 + j, n - j, vec, m[h]);
+                    store_some(v32 + j, n - j, vec, v[h]);
                 }
             }
-            if (BITS == 8) {
-                uint32_t am = 0, av = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    am = max(am, finite_magnitude(m[k]));
-                    av = max(av, finite_magnitude(root[k]));
-                }
+            if constexpr (BITS == 8) {
                 const int km = scale_exponent(__reduce_max_sync(0xffffffffu, am));
                 const int kv = scale_exponent(__reduce_max_sync(0xffffffffu, av));
                 const float im = __uint_as_float(static_cast<uint32_t>(127 - km) << 23);
@@ -134,19 +201,20 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamArgs a, c
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int j0 = h * 128 + lane * 4;
-                    if (j0 >= n) continue;
-                    const uint64_t quad = static_cast<uint64_t>(base + j0) >> 2;
+                    const int j = h * 128 + lane * 4;
+                    const uint64_t quad = static_cast<uint64_t>(base + j) >> 2;
                     const uint4 w = philox4x32_10(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
-                                                             static_cast<uint32_t>(a.tensor0 + lo), static_cast<uint32_t>(st.t)),
+                                                             static_cast<uint32_t>(a.tensor0 + t), static_cast<uint32_t>(st.t)),
                                                   make_uint2(static_cast<uint32_t>(a.seed), static_cast<uint32_t>(a.seed >> 32)));
                     const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+                    uint32_t cm = 0, cv = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (j0 + i >= n) continue;
-                        static_cast<uint8_t *>(T.m)[base + j0 + i] = static_cast<uint8_t>(e4m3_code(m[4 * h + i], im, word[i] & 0xffffu, false));
-                        static_cast<uint8_t *>(T.v)[base + j0 + i] = static_cast<uint8_t>(e4m3_code(root[4 * h + i], iv, word[i] >> 16, true));
+                        cm |= e4m3_code(m[h][i], im, word[i] & 0xffffu, false) << (8 * i);
+                        cv |= e4m3_code(v[h][i], iv, word[i] >> 16, true) << (8 * i);
                     }
+                    store_codes(m8 + j, n - j, vec, cm);
+                    store_codes(v8 + j, n - j, vec, cv);
                 }
             }
         }
@@ -191,8 +259,6 @@ struct ea_adamw {
 };
 
 namespace {
-
-constexpr int kAdamCtasPerSm = 4;
 
 int validate(const ea_adamw_config *cfg)
 {

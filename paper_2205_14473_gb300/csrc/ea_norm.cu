@@ -4,7 +4,9 @@
 namespace ea {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormUnit = 1024;  // coordinates of a warp's unit of work
+constexpr int kNormCtasPerSm = 6;
+constexpr int kNormWarps = kNormThreads / 32;
+constexpr int kNormUnit = 512;  // coordinates of a warp's unit of work
 
 struct NormArgs {
     int64_t units;           // of this launch
@@ -21,38 +23,90 @@ struct NormArgs {
 };
 
 template <class G>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a, const __grid_constant__ GradList list)
+struct alignas(16) NormPack {
+    G x[16 / sizeof(G)];
+};
+
+// Sum of the squares of N values.  Squares are formed and added in binary32, at most 16 of them, where the largest
+// magnitude lies in [2^-40, 2^60]: none overflows, and one that underflows is below 2^-69 of the largest.  Other
+// values -- tiny, huge, infinite or NaN ones -- are squared in binary64.
+template <int N>
+__device__ __forceinline__ double squares(const float (&x)[N])
 {
+    static_assert(N <= 16);
+    uint32_t most = 0;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+        sum = __fmaf_rn(x[i], x[i], sum);
+    }
+    if (most == 0) return 0.0;
+    if (most - (87u << 23) <= (100u << 23)) return sum;
+    double wide = 0.0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) wide += static_cast<double>(x[i]) * x[i];
+    return wide;
+}
+
+// The CTA's sum, in a fixed order, valid in thread 0.  One barrier before `red` may be reused.
+__device__ __forceinline__ double norm_block_sum(double v, double *red)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_down_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int w = 0; w < kNormWarps; ++w) v += red[w];
+    return v;
+}
+
+// A read-only pass: a warp takes units of kNormUnit coordinates of one tensor, its loads 16 bytes wide and all in
+// flight at once (a tensor that starts off a 16-byte boundary gives its first elements to its first unit).  Each
+// CTA leaves one binary64 partial sum, and the last one to finish adds those in order.
+template <class G>
+__global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(const NormArgs a, const __grid_constant__ GradList list)
+{
+    constexpr int kVec = 16 / sizeof(G), kPacks = kNormUnit / (32 * kVec);
+    __shared__ double red[kNormWarps];
+    __shared__ bool last;
     const int lane = threadIdx.x & 31;
-    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kNormThreads / 32);
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * kNormWarps;
     double sum = 0.0;
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kNormThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
-        int lo = 0, hi = a.n_tensors - 1;  // the last tensor whose first unit is <= u
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.first[mid] <= u) lo = mid;
-            else hi = mid - 1;
+    int t = 0;
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * kNormWarps + (threadIdx.x >> 5); u < a.units; u += warps) {
+        t = tensor_of(a.first, a.n_tensors, u, t);
+        const G *g = static_cast<const G *>(list.g[t]);
+        const int64_t size = a.sizes[t], unit = u - a.first[t];
+        const int64_t off = (reinterpret_cast<uintptr_t>(g) & 15) / sizeof(G);  // elements after the boundary before g
+        const int64_t begin = unit == 0 ? 0 : unit * kNormUnit - off;
+        const int64_t end = u + 1 == a.first[t + 1] ? size : (unit + 1) * kNormUnit - off;
+        const int64_t body = unit == 0 ? min(size, off ? kVec - off : 0) : begin;  // the first whole pack
+        float x[kVec];
+        NormPack<G> pack[kPacks];
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int64_t j = body + (k * 32 + lane) * kVec;
+            if (j + kVec <= end) pack[k] = *reinterpret_cast<const NormPack<G> *>(g + j);
+            else pack[k] = NormPack<G>{};
         }
-        const int64_t base = (u - a.first[lo]) * kNormUnit;
-        const int64_t n = min(a.sizes[lo] - base, static_cast<int64_t>(kNormUnit));
-        const G *g = static_cast<const G *>(list.g[lo]) + base;
-        for (int64_t j = lane; j < n; j += 32) {
-            const double x = to_f32(g[j]);
-            sum += x * x;
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) x[i] = to_f32(pack[k].x[i]);
+            sum += squares(x);
+        }
+        // what is left on either side: fewer than kVec elements before, fewer than 2 kVec after (in the last unit)
+        const int64_t packs = min((end - body) / kVec, static_cast<int64_t>(32 * kPacks)), tail = body + packs * kVec;
+        const int64_t edge = lane < kVec ? begin + lane : tail + lane - kVec;
+        if (lane < kVec ? edge < body : edge < end) {
+            const float one[1] = {to_f32(g[edge])};
+            sum += squares(one);
         }
     }
-    __shared__ double red[kNormThreads];
-    __shared__ bool last;
-    auto block_sum = [&](double v) {
-        red[threadIdx.x] = v;
-        __syncthreads();
-        for (int o = kNormThreads / 2; o > 0; o >>= 1) {
-            if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-            __syncthreads();
-        }
-        return red[0];
-    };
-    const double total = block_sum(sum);
+    const double total = norm_block_sum(sum, red);
     if (threadIdx.x == 0) {
         a.partials[blockIdx.x] = total;
         __threadfence();
@@ -63,15 +117,14 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const NormArgs a, co
     if (!last) return;
     double v = 0.0;
     for (int i = threadIdx.x; i < a.n_all; i += kNormThreads) v += __ldcg(a.all + i);
-    __syncthreads();
-    v = block_sum(v);
+    v = norm_block_sum(v, red);
     if (threadIdx.x == 0) {
         *a.ticket = 0;
-        const float norm = static_cast<float>(fabs(static_cast<double>(a.grad_scale)) * sqrt(v));
+        const double wide = fabs(static_cast<double>(a.grad_scale)) * sqrt(v);
+        const float norm = static_cast<float>(wide);
         float factor = a.grad_scale;
         if (!isfinite(norm)) factor = __int_as_float(0x7fc00000);
-        else if (norm > a.max_norm)
-            factor = static_cast<float>(a.grad_scale * (a.max_norm / (fabs(static_cast<double>(a.grad_scale)) * sqrt(v))));
+        else if (norm > a.max_norm) factor = static_cast<float>(a.grad_scale * (a.max_norm / wide));
         a.out[0] = norm;
         a.out[1] = factor;
     }
@@ -99,8 +152,6 @@ struct ea_norm {
 };
 
 namespace {
-
-constexpr int kNormCtasPerSm = 8;
 
 int validate(const ea_grad_norm_config *cfg)
 {
