@@ -124,7 +124,7 @@ typedef struct ea_adamw_config {
     int32_t copy_type;              /* EA_T_BF16 or EA_T_F16 (of the copies, where there are any) */
     int32_t state_bits;             /* 32 or 8 */
     float beta1, beta2;             /* in [0, 1) */
-    float eps;                      /* > 0 */
+    float eps;                      /* >= 1e-30 */
     uint64_t seed;                  /* Philox key of the 8-bit states' rounding */
     int64_t step;                   /* steps taken before (0 for a new run; a checkpoint's otherwise), < 2^32 */
     const ea_adamw_tensor *tensors; /* host memory, n_tensors of them; copied */
@@ -140,7 +140,7 @@ int ea_adamw_init(const ea_adamw_config *cfg, void *workspace, size_t workspace_
  *   p <- p - (l weight_decay p + a m / (sqrt(v) + e)),  l = lr lr_scale,
  *   a = l sqrt(1 - beta2^t) / (1 - beta1^t),  e = eps sqrt(1 - beta2^t)
  * which is lr_scale lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p), in binary32
- * with one rounding per operation.  p is rounded to the parameters' type, and the unrounded binary32 p to the
+ * with one rounding per operation (the quotient to within two units in the last place).  p is rounded to the parameters' type, and the unrounded binary32 p to the
  * copy's.  With 8-bit states the step uses m and v as just formed; then each is scaled by the smallest power
  * of two (>= 2^-126) that brings its block's largest finite magnitude to at most 448 and rounded to e4m3
  * stochastically (up with the probability of the remainder, in 2^-16): coordinate j of tensor i draws word

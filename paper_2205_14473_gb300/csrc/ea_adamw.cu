@@ -3,7 +3,6 @@
 // moments in binary32 or in 8 bits.
 #include <cuda_fp8.h>
 
-#include "ea_device.cuh"
 #include "ea_lm.cuh"
 
 namespace ea {
@@ -30,20 +29,79 @@ struct AdamArgs {
     int last;                      // whether this launch is the step's last
     float lr, beta1, beta2, c1, c2;
     double beta1d, beta2d, eps;
-    uint64_t seed;
     const float *clip;
+    uint2 keys[10];                // Philox's key of every round
+    float minus_zero;              // -0 (see mul2)
 };
 
-__device__ __forceinline__ uint32_t e4m3_code(float x, float inv, uint32_t r16, bool keep_nonzero)
+// Two binary32 values in one 64-bit register: one instruction slot for two operations, each rounded by itself.
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 pack2(float a, float b)
 {
-    const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
-    if (bits >= 0x7f800000u) return 0x7fu;  // not finite: NaN
-    const float y = __fmul_rn(__uint_as_float(bits), inv);
-    uint32_t code;
-    if (y >= 0x1p-6f) code = ((__float_as_uint(y) + (r16 << 4)) >> 20) - ((127u - 7u) << 3);
-    else code = static_cast<uint32_t>(floorf(__fadd_rn(__fmul_rn(y, 512.0f), __fmul_rn(static_cast<float>(r16), 0x1p-16f))));
-    if (keep_nonzero && bits != 0 && code == 0) code = 1;
-    return code | (__float_as_uint(x) >> 31 << 7);
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(F2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
+// a b as a b + (-0), the same value, with a -0 that the compiler does not know: a packed product and the packed sum
+// after it would be merged into one rounding, whatever their PTX says.
+__device__ __forceinline__ F2 mul2(F2 a, F2 b, F2 minus_zero) { return fma2(a, b, minus_zero); }
+
+__device__ __forceinline__ F2 negate2(F2 a) { return F2{a.v ^ 0x8000000080000000ull}; }
+
+// Within 2^-23 relative of the reciprocal of a normal number.
+__device__ __forceinline__ float recip_normal(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// The square roots of two numbers, zero or normal, rounded to nearest: from y ~ 1 / sqrt(x), g = x y and h = y / 2
+// are refined together (Goldschmidt), g <- g + g (1/2 - g h), h <- h + h (1/2 - g h), and the remainder x - g^2,
+// exact in a fused operation, corrects g's last bit (Markstein, "Computation of elementary functions on the IBM
+// RISC System/6000 processor", 1990).  Equal to sqrtf for every number above 2^-100.  It is half the
+// instructions of two calls, and no branch stands between the eight coordinates of a lane.
+__device__ __forceinline__ void sqrt_pair(float &a, float &b)
+{
+    float ya, yb;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(fmaxf(a, 0x1p-126f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(fmaxf(b, 0x1p-126f)));
+    const F2 x = pack2(a, b), y = pack2(ya, yb);
+    const F2 none = both(-0.0f);  // nothing here may be merged to another effect: every sum is a fused one already
+    F2 g = fma2(x, y, none), h = fma2(y, both(0.5f), none);
+    const F2 e = fma2(negate2(g), h, both(0.5f));
+    g = fma2(g, e, g);
+    h = fma2(h, e, h);
+    g = fma2(fma2(negate2(g), g, x), h, g);
+    unpack2(g, a, b);
+}
+
+// Philox4x32-10 with the round keys formed once on the host.
+__device__ __forceinline__ uint4 philox_words(uint4 c, const uint2 (&keys)[10])
+{
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = static_cast<uint64_t>(0xD2511F53u) * c.x, p1 = static_cast<uint64_t>(0xCD9E8D57u) * c.z;
+        c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ keys[r].x, static_cast<uint32_t>(p1),
+                       static_cast<uint32_t>(p0 >> 32) ^ c.w ^ keys[r].y, static_cast<uint32_t>(p0));
+    }
+    return c;
 }
 
 // The values of four e4m3 codes, exact.
@@ -98,28 +156,100 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int n, bool whole, uint3
 }
 
 // The exponent k of the smallest power of two >= 2^-126 with amax / 2^k <= 448 = 1.75 * 2^8.
-__device__ __forceinline__ int scale_exponent(uint32_t amax_bits)
+__device__ __forceinline__ int scale_exponent(float amax)
 {
-    return max(static_cast<int>((amax_bits + 0x1fffffu) >> 23) - 127 - 8, -126);
+    return max(static_cast<int>((__float_as_uint(amax) + 0x1fffffu) >> 23) - 127 - 8, -126);
+}
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float(static_cast<uint32_t>(127 + k) << 23); }
+
+__device__ __forceinline__ float finite_magnitude(float x)
+{
+    const float m = fabsf(x);
+    return m < __int_as_float(0x7f800000) ? m : 0.0f;
 }
 
-__device__ __forceinline__ uint32_t finite_magnitude(float x)
+// The largest of the warp's non-negative values.
+__device__ __forceinline__ float warp_max(float x) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x))); }
+
+// What a step does to four coordinates is written in two forms that give the same bits: AdamStep::pairs on packed
+// pairs and, in the 8-bit states, the quantizer below.
+struct AdamStep {
+    float factor, beta1, beta2, c1, c2, e, step, rate;
+    F2 z;  // (-0, -0)
+
+    // The new parameters, from the moments and the second one's root (times `unit`, a power of two).
+    __device__ __forceinline__ void params(float (&p)[4], const float (&m)[4], const float (&root)[4], float unit) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            float d0, d1;
+            unpack2(fma2(pack2(root[i], root[i + 1]), both(unit), both(e)), d0, d1);
+            const F2 q = mul2(pack2(m[i], m[i + 1]), pack2(recip_normal(d0), recip_normal(d1)), z);
+            const F2 x = pack2(p[i], p[i + 1]), d = add2(mul2(x, both(rate), z), mul2(q, both(step), z));
+            unpack2(fma2(d, both(-1.0f), x), p[i], p[i + 1]);
+        }
+    }
+
+    // m <- mb m + c1 g and v <- vb v + c2 g^2 with g the gradient times the factor.
+    __device__ __forceinline__ void moments(float (&m)[4], float (&v)[4], const float (&grad)[4], float mb, float vb) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const F2 g = mul2(pack2(grad[i], grad[i + 1]), both(factor), z);
+            unpack2(add2(mul2(pack2(m[i], m[i + 1]), both(mb), z), mul2(g, both(c1), z)), m[i], m[i + 1]);
+            unpack2(add2(mul2(pack2(v[i], v[i + 1]), both(vb), z), mul2(mul2(g, g, z), both(c2), z)), v[i], v[i + 1]);
+        }
+    }
+};
+
+// Four magnitudes y <= 448 (but for the root's last bit, which saturates) in e4m3, rounded up with the probability
+// of the remainder.  A normal number's 20 bits below its third mantissa bit get a random number added and are cut
+// off; below 2^-6 the grid's spacing is 2^-9 throughout.  r: 16 random bits each, in bits 4 .. 19.
+template <bool KEEP_NONZERO>
+__device__ __forceinline__ void round_e4m3(float (&y)[4], const uint32_t (&r)[4])
 {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0u;
+    constexpr uint32_t kNormal = (127u - 6u) << 23;
+    uint32_t least = 0xffffffffu;
+    float q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        q[i] = __uint_as_float((__float_as_uint(y[i]) + r[i]) & 0xfff00000u);
+        least = min(least, __float_as_uint(y[i]) - 1u);
+    }
+    if (least < kNormal - 1u) {  // some 0 < y < 2^-6
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (__float_as_uint(y[i]) - 1u < kNormal - 1u) {
+                const float up = __fmaf_rn(static_cast<float>(r[i]), 0x1p-20f, __fmul_rn(y[i], 512.0f));
+                const float n = __fsub_rn(__fadd_rd(up, 0x1p23f), 0x1p23f);  // its floor
+                q[i] = __fmul_rn(KEEP_NONZERO ? fmaxf(n, 1.0f) : n, 0x1p-9f);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = q[i];
+}
+
+// Codes of four values of the format (the last one's in the highest byte); NaN stays NaN.
+__device__ __forceinline__ uint32_t e4m3_codes(const float (&x)[4])
+{
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
+    return lo | static_cast<uint32_t>(hi) << 16;
 }
 
 // A warp takes blocks of 256 coordinates: four consecutive ones per lane in each half, so that every access of the
 // warp is one contiguous piece, and the block's scale is one warp reduction.  All loads of a block are issued before
 // the first is used.
 template <class P, class G, class C, int BITS>
-__global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const AdamArgs a, const __grid_constant__ GradList list)
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
 {
     const int lane = threadIdx.x & 31;
     const float factor = a.clip ? a.clip[1] : 1.0f;
     const AdamState st = *a.state;
     if (!isnan(factor)) {
         const int64_t warps = static_cast<int64_t>(gridDim.x) * (kAdamThreads / 32);
+        AdamStep s{factor, a.beta1, a.beta2, a.c1, a.c2, st.e, 0.0f, 0.0f, both(a.minus_zero)};
         int t = 0;
         for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kAdamThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
             t = tensor_of(a.first, a.n_tensors, u, t);
@@ -155,66 +285,114 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(con
                 ms = T.m_scale[block];
                 vs = T.v_scale[block];
             }
-            const float lr = __fmul_rn(a.lr, T.lr_scale), step = __fmul_rn(lr, st.a), rate = __fmul_rn(lr, T.weight_decay);
-            uint32_t am = 0, av = 0;
+            const float lr = __fmul_rn(a.lr, T.lr_scale);
+            s.step = __fmul_rn(lr, st.a);
+            s.rate = __fmul_rn(lr, T.weight_decay);
+            if constexpr (BITS == 32) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = h * 128 + lane * 4;
-                if constexpr (BITS == 8) {
-                    e4m3_values(mc[h], m[h]);
-                    e4m3_values(vc[h], v[h]);
-                }
+                for (int h = 0; h < 2; ++h) {
+                    const int j = h * 128 + lane * 4;
+                    s.moments(m[h], v[h], gk[h], s.beta1, s.beta2);
+                    float root[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float &mi = m[h][i], &vi = v[h][i];
-                    if constexpr (BITS == 8) {
-                        mi = __fmul_rn(mi, ms);
-                        vi = __fmul_rn(vi, vs);
-                        vi = __fmul_rn(vi, vi);
-                    }
-                    const float gi = __fmul_rn(gk[h][i], factor);
-                    mi = __fadd_rn(__fmul_rn(mi, a.beta1), __fmul_rn(gi, a.c1));
-                    vi = __fadd_rn(__fmul_rn(vi, a.beta2), __fmul_rn(__fmul_rn(gi, gi), a.c2));
-                    const float root = __fsqrt_rn(vi), x = pk[h][i];
-                    pk[h][i] = __fsub_rn(x, __fadd_rn(__fmul_rn(x, rate), __fmul_rn(__fdiv_rn(mi, __fadd_rn(root, st.e)), step)));
-                    if constexpr (BITS == 8) {
-                        vi = root;
-                        am = max(am, finite_magnitude(mi));
-                        av = max(av, finite_magnitude(root));
-                    }
-                }
-                store_some(p + j, n - j, vec, pk[h]);
-                if (copy) store_some(copy + j, n - j, vec, pk[h]);
-                if constexpr (BITS == 32) {
+                    for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
+                    s.params(pk[h], m[h], root, 1.0f);
+                    store_some(p + j, n - j, vec, pk[h]);
+                    if (copy) store_some(copy + j, n - j, vec, pk[h]);
                     store_some(m32 + j, n - j, vec, m[h]);
                     store_some(v32 + j, n - j, vec, v[h]);
                 }
-            }
-            if constexpr (BITS == 8) {
-                const int km = scale_exponent(__reduce_max_sync(0xffffffffu, am));
-                const int kv = scale_exponent(__reduce_max_sync(0xffffffffu, av));
-                const float im = __uint_as_float(static_cast<uint32_t>(127 - km) << 23);
-                const float iv = __uint_as_float(static_cast<uint32_t>(127 - kv) << 23);
+            } else {
+                // beta1 m scale and beta2 (r scale)^2 are one multiplication each where the power of two leaves
+                // the product normal: a scale below 2^-40 goes into the values first
+                const bool small = ms < 0x1p-40f || vs < 0x1p-40f;
+                const float mb = small ? s.beta1 : __fmul_rn(s.beta1, ms), vb = small ? s.beta2 : __fmul_rn(s.beta2, __fmul_rn(vs, vs));
+                float am = 0.0f, av = 0.0f;
+                bool finite = true;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    e4m3_values(mc[h], m[h]);
+                    e4m3_values(vc[h], v[h]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (small) {
+                            m[h][i] = __fmul_rn(m[h][i], ms);
+                            v[h][i] = __fmul_rn(v[h][i], vs);
+                        }
+                        v[h][i] = __fmul_rn(v[h][i], v[h][i]);
+                    }
+                    s.moments(m[h], v[h], gk[h], mb, vb);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        am = __uint_as_float(max(__float_as_uint(am), __float_as_uint(fabsf(m[h][i]))));
+                        av = __uint_as_float(max(__float_as_uint(av), __float_as_uint(v[h][i])));
+                    }
+                }
+                am = warp_max(am);
+                av = warp_max(av);
+                finite = __float_as_uint(am) < 0x7f800000u && __float_as_uint(av) < 0x7f800000u;
+                if (!finite) {  // the scales go by the finite values; the others are held as NaN
+                    am = av = 0.0f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            am = fmaxf(am, finite_magnitude(m[h][i]));
+                            av = fmaxf(av, finite_magnitude(v[h][i]));
+                        }
+                    am = warp_max(am);
+                    av = warp_max(av);
+                }
+                // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
+                const bool lift = finite && av < 0x1p60f;
+                const float unit = lift ? 0x1p-32f : 1.0f;
+                const int km = scale_exponent(am), kv = scale_exponent(__fsqrt_rn(av));
+                const float im = power_of_two(-km), iv = __fmul_rn(power_of_two(-kv), unit);
                 if (lane == 0) {
-                    T.m_scale[block] = __uint_as_float(static_cast<uint32_t>(127 + km) << 23);
-                    T.v_scale[block] = __uint_as_float(static_cast<uint32_t>(127 + kv) << 23);
+                    T.m_scale[block] = power_of_two(km);
+                    T.v_scale[block] = power_of_two(kv);
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int j = h * 128 + lane * 4;
+                    float root[4];
+                    if (lift) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) root[i] = __fmul_rn(v[h][i], 0x1p64f);
+                        sqrt_pair(root[0], root[1]);
+                        sqrt_pair(root[2], root[3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
+                    }
+                    s.params(pk[h], m[h], root, unit);
+                    store_some(p + j, n - j, vec, pk[h]);
+                    if (copy) store_some(copy + j, n - j, vec, pk[h]);
                     const uint64_t quad = static_cast<uint64_t>(base + j) >> 2;
-                    const uint4 w = philox4x32_10(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
-                                                             static_cast<uint32_t>(a.tensor0 + t), static_cast<uint32_t>(st.t)),
-                                                  make_uint2(static_cast<uint32_t>(a.seed), static_cast<uint32_t>(a.seed >> 32)));
+                    const uint4 w = philox_words(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
+                                                            static_cast<uint32_t>(a.tensor0 + t), static_cast<uint32_t>(st.t)), a.keys);
                     const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-                    uint32_t cm = 0, cv = 0;
+                    float ym[4], yv[4];
+                    uint32_t rm[4], rv[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        cm |= e4m3_code(m[h][i], im, word[i] & 0xffffu, false) << (8 * i);
-                        cv |= e4m3_code(v[h][i], iv, word[i] >> 16, true) << (8 * i);
+                        ym[i] = __fmul_rn(fabsf(m[h][i]), im);
+                        yv[i] = __fmul_rn(root[i], iv);
+                        rm[i] = (word[i] << 4) & 0xffff0u;
+                        rv[i] = (word[i] >> 12) & 0xffff0u;
                     }
-                    store_codes(m8 + j, n - j, vec, cm);
-                    store_codes(v8 + j, n - j, vec, cv);
+                    round_e4m3<false>(ym, rm);
+                    round_e4m3<true>(yv, rv);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        ym[i] = copysignf(ym[i], m[h][i]);
+                        if (!finite) {
+                            if (!isfinite(m[h][i])) ym[i] = __int_as_float(0x7fc00000);
+                            if (!isfinite(v[h][i])) yv[i] = __int_as_float(0x7fc00000);
+                        }
+                    }
+                    store_codes(m8 + j, n - j, vec, e4m3_codes(ym));
+                    store_codes(v8 + j, n - j, vec, e4m3_codes(yv));
                 }
             }
         }
@@ -271,7 +449,7 @@ int validate(const ea_adamw_config *cfg)
     if (cfg->state_bits != 32 && cfg->state_bits != 8) return lm_fail(EA_E_INVAL, "state_bits is 32 or 8");
     if (!(cfg->beta1 >= 0.0f && cfg->beta1 < 1.0f)) return lm_fail(EA_E_INVAL, "beta1 must be in [0, 1)");
     if (!(cfg->beta2 >= 0.0f && cfg->beta2 < 1.0f)) return lm_fail(EA_E_INVAL, "beta2 must be in [0, 1)");
-    if (!(cfg->eps > 0.0f) || !std::isfinite(cfg->eps)) return lm_fail(EA_E_INVAL, "eps must be > 0");
+    if (!(cfg->eps >= 1e-30f) || !std::isfinite(cfg->eps)) return lm_fail(EA_E_INVAL, "eps must be >= 1e-30");
     if (cfg->step < 0 || cfg->step >= (int64_t{1} << 32)) return lm_fail(EA_E_INVAL, "step out of [0, 2^32)");
     const int32_t state = cfg->state_bits == 32 ? EA_T_F32 : -1;
     for (int32_t i = 0; i < cfg->n_tensors; ++i) {
@@ -435,7 +613,9 @@ int ea_adamw_step(ea_adamw *h, const void *const *grads, float lr, const float *
         a.beta1d = h->cfg.beta1;
         a.beta2d = h->cfg.beta2;
         a.eps = h->cfg.eps;
-        a.seed = h->cfg.seed;
+        a.minus_zero = -0.0f;
+        for (uint32_t k = 0; k < 10; ++k)
+            a.keys[k] = make_uint2(static_cast<uint32_t>(h->cfg.seed) + k * 0x9E3779B9u, static_cast<uint32_t>(h->cfg.seed >> 32) + k * 0xBB67AE85u);
         a.clip = clip;
         if (h->cfg.param_type == EA_T_F32) launch_adamw<float>(*h, l, a, list);
         else launch_adamw<bf16>(*h, l, a, list);

@@ -1,12 +1,14 @@
 // ea_norm.cu -- ea_grad_norm: the 2-norm of a list of gradients and the factor that clips them.
+#include <type_traits>
+
 #include "ea_lm.cuh"
 
 namespace ea {
 
 constexpr int kNormThreads = 256;
-constexpr int kNormCtasPerSm = 6;
+constexpr int kNormCtasPerSm = 4;
 constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kNormUnit = 512;  // coordinates of a warp's unit of work
+constexpr int kNormBytes = 4096;  // of a warp's unit of work: eight 16-byte loads per lane
 
 struct NormArgs {
     int64_t units;           // of this launch
@@ -22,31 +24,37 @@ struct NormArgs {
     float *out;
 };
 
-template <class G>
-struct alignas(16) NormPack {
-    G x[16 / sizeof(G)];
-};
-
-// Sum of the squares of N values.  Squares are formed and added in binary32, at most 16 of them, where the largest
-// magnitude lies in [2^-40, 2^60]: none overflows, and one that underflows is below 2^-69 of the largest.  Other
-// values -- tiny, huge, infinite or NaN ones -- are squared in binary64.
-template <int N>
-__device__ __forceinline__ double squares(const float (&x)[N])
+// The elements of 16 bytes as binary32.
+__device__ __forceinline__ void unpack(const uint4 &v, float (&x)[4], const float *)
 {
-    static_assert(N <= 16);
-    uint32_t most = 0;
-    float sum = 0.0f;
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
+}
+template <class G>
+__device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8], const G *)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-        sum = __fmaf_rn(x[i], x[i], sum);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same<G, bf16>::value) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
     }
-    if (most == 0) return 0.0;
-    if (most - (87u << 23) <= (100u << 23)) return sum;
-    double wide = 0.0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) wide += static_cast<double>(x[i]) * x[i];
-    return wide;
+}
+
+// Sum of the squares of `count` elements from g on in binary64: any magnitude.
+template <class G>
+__device__ __noinline__ double wide_squares(const G *g, int count)
+{
+    double sum = 0.0;
+    for (int i = 0; i < count; ++i) {
+        const double x = to_f32(g[i]);
+        sum += x * x;
+    }
+    return sum;
 }
 
 // The CTA's sum, in a fixed order, valid in thread 0.  One barrier before `red` may be reused.
@@ -63,13 +71,15 @@ __device__ __forceinline__ double norm_block_sum(double v, double *red)
     return v;
 }
 
-// A read-only pass: a warp takes units of kNormUnit coordinates of one tensor, its loads 16 bytes wide and all in
-// flight at once (a tensor that starts off a 16-byte boundary gives its first elements to its first unit).  Each
-// CTA leaves one binary64 partial sum, and the last one to finish adds those in order.
+// A read-only pass: a warp takes units of kNormBytes of one tensor, its loads 16 bytes wide and all in flight at
+// once (a tensor that starts off a 16-byte boundary gives its first elements to its first unit).  A lane's squares
+// are formed and added in binary32, a few dozen of them, where their sum shows that none overflowed and that any that
+// underflowed do not count; otherwise, and between units, in binary64.  Each CTA leaves one partial sum, and the
+// last one to finish adds those in order.
 template <class G>
 __global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(const NormArgs a, const __grid_constant__ GradList list)
 {
-    constexpr int kVec = 16 / sizeof(G), kPacks = kNormUnit / (32 * kVec);
+    constexpr int kVec = 16 / sizeof(G), kPacks = kNormBytes / 512, kNormUnit = kNormBytes / sizeof(G);
     __shared__ double red[kNormWarps];
     __shared__ bool last;
     const int lane = threadIdx.x & 31;
@@ -84,26 +94,38 @@ __global__ void __launch_bounds__(kNormThreads, kNormCtasPerSm) norm_kernel(cons
         const int64_t begin = unit == 0 ? 0 : unit * kNormUnit - off;
         const int64_t end = u + 1 == a.first[t + 1] ? size : (unit + 1) * kNormUnit - off;
         const int64_t body = unit == 0 ? min(size, off ? kVec - off : 0) : begin;  // the first whole pack
-        float x[kVec];
-        NormPack<G> pack[kPacks];
+        const int packs = static_cast<int>(min((end - body) / kVec, static_cast<int64_t>(32 * kPacks)));
+        const uint4 *pack = reinterpret_cast<const uint4 *>(g + body) + lane;
+        uint4 v[kPacks];
+        if (packs == 32 * kPacks) {
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const int64_t j = body + (k * 32 + lane) * kVec;
-            if (j + kVec <= end) pack[k] = *reinterpret_cast<const NormPack<G> *>(g + j);
-            else pack[k] = NormPack<G>{};
+            for (int k = 0; k < kPacks; ++k) v[k] = pack[32 * k];
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPacks; ++k) v[k] = 32 * k + lane < packs ? pack[32 * k] : make_uint4(0, 0, 0, 0);
         }
+        float part = 0.0f;
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
+            float x[kVec], s = 0.0f;
+            unpack(v[k], x, g);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) x[i] = to_f32(pack[k].x[i]);
-            sum += squares(x);
+            for (int i = 0; i < kVec; ++i) s = __fmaf_rn(x[i], x[i], s);
+            part = __fadd_rn(part, s);
+        }
+        if (part >= 0x1p-80f && part < __int_as_float(0x7f800000)) {
+            sum += part;
+        } else {
+            uint32_t any = 0;  // zeros are common, whole units of them
+#pragma unroll
+            for (int k = 0; k < kPacks; ++k) any |= v[k].x | v[k].y | v[k].z | v[k].w;
+            if (any)
+                for (int k = 0; 32 * k + lane < packs; ++k) sum += wide_squares(g + body + (32 * k + lane) * kVec, kVec);
         }
         // what is left on either side: fewer than kVec elements before, fewer than 2 kVec after (in the last unit)
-        const int64_t packs = min((end - body) / kVec, static_cast<int64_t>(32 * kPacks)), tail = body + packs * kVec;
-        const int64_t edge = lane < kVec ? begin + lane : tail + lane - kVec;
-        if (lane < kVec ? edge < body : edge < end) {
-            const float one[1] = {to_f32(g[edge])};
-            sum += squares(one);
+        if (begin < body || body + packs * kVec < end) {
+            const int64_t tail = body + packs * kVec, edge = lane < kVec ? begin + lane : tail + lane - kVec;
+            if (lane < kVec ? edge < body : edge < end) sum += wide_squares(g + edge, 1);
         }
     }
     const double total = norm_block_sum(sum, red);
@@ -208,9 +230,10 @@ int ea_grad_norm_init(const ea_grad_norm_config *cfg, void *workspace, size_t wo
         h->sizes.assign(cfg->sizes, cfg->sizes + cfg->n_tensors);
         for (int i = 0; i < cfg->n_tensors; i += kGradBatch) {
             ea_norm::Launch l{i, std::min(kGradBatch, cfg->n_tensors - i), 0, 0, static_cast<int64_t>(h->table.size())};
+            const int64_t unit = kNormBytes / static_cast<int64_t>(type_bytes(cfg->grad_type));
             for (int k = 0; k < l.n_tensors; ++k) {
                 h->table.push_back(l.units);
-                l.units += (h->sizes[i + k] + kNormUnit - 1) / kNormUnit;
+                l.units += (h->sizes[i + k] + unit - 1) / unit;
             }
             h->table.push_back(l.units);
             const int64_t ctas = (l.units + kNormThreads / 32 - 1) / (kNormThreads / 32);

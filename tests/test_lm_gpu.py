@@ -451,6 +451,38 @@ def test_adamw_8(ptype, gtype, copy, sizes):
                          words >> 16, True, f"r of {i}")
 
 
+@pytest.mark.parametrize("ptype,gtype", [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F16), (BF16, F32), (F32, F16)])
+@pytest.mark.parametrize("mag", [1e-3, 1e-19])
+def test_adamw_8_states_are_binary32(ptype, gtype, mag):
+    """The moments and the root before they are rounded to 8 bits, one binary32 rounding per operation: torch's
+    elementary operations, each its own kernel, and the format's rounding in integers give the same bytes."""
+    n = 3_000_000 if mag == 1e-3 else 300_000
+    p, opt = _randn(n, seed=90, dtype=ptype), None
+    factor = torch.tensor([1.0, 0.37], device="cuda")
+    opt = ea.AdamW([p], state_bits=8, grad_dtype=gtype, seed=77)
+    blk = torch.arange(n, device="cuda") // 256
+    j = np.arange(n // 4)
+    for t in range(3):
+        g = (_randn(n, seed=91 + t) * torch.rand(n, generator=_gen(t), device="cuda").pow_(4) * mag).to(gtype)
+        old = {k: v[0].float().clone() for k, v in opt.states.items()}
+        opt.step([g], lr=1e-3, clip=factor)
+        gf = g.float() * factor[1]
+        m = old["m"] * old["m_scale"][blk] * 0.9 + gf * float(np.float32(1) - np.float32(0.9))
+        r = old["r"] * old["r_scale"][blk]
+        root = (r * r * 0.999 + gf * gf * float(np.float32(1) - np.float32(0.999))).sqrt()
+        words = torch.from_numpy(_philox(77, [j, j * 0, j * 0, j * 0 + t]).T.reshape(-1).astype(np.int64)).cuda()
+        for k, x, r16 in (("m", m, words & 0xFFFF), ("r", root, words >> 16)):
+            top = torch.zeros(-(-n // 256), device="cuda").scatter_reduce_(0, blk, x.abs(), "amax")
+            e = (((top.view(torch.int32) + 0x1FFFFF) >> 23) - 135).clamp(min=-126)
+            y = x.abs() * ((127 - e) << 23).view(torch.float32)[blk]
+            q = ((y.view(torch.int32) + (r16 << 4).to(torch.int32)) & -0x100000).view(torch.float32)
+            q = torch.where(y >= 2.0 ** -6, q, torch.floor(y * 512 + r16.float() * 2.0 ** -16) * 2.0 ** -9)
+            q = torch.where(root > 0, q.clamp(min=2.0 ** -9), q) if k == "r" else torch.copysign(q, x)
+            assert torch.equal(opt.states[k + "_scale"][0], ((127 + e) << 23).view(torch.float32)), (k, t)
+            got = opt.states[k][0].float()
+            assert torch.equal(got, q), (k, t, int((got != q).sum()))
+
+
 def test_adamw_8_rounding_is_unbiased():
     """The mean of the held first moment over many coordinates with the same value: within 6 standard deviations
     of that value (a deviation is at most half the grid's spacing)."""
