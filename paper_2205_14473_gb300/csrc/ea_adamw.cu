@@ -3,12 +3,14 @@
 // moments in binary32 or in 8 bits.
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "ea_lm.cuh"
 
 namespace ea {
 
 constexpr int kAdamThreads = 256;
-constexpr int kAdamCtasPerSm = 3;  // 85 registers per thread; a persistent grid of them
+constexpr int kAdamCtasPerSm = 2;  // 128 registers per thread; a persistent grid of them
 constexpr int kBlock = EA_ADAMW_BLOCK;  // a warp's unit of work: eight coordinates per lane
 
 // What a step needs to know of the steps before it.  The last CTA of a step that is not skipped advances it.
@@ -113,66 +115,72 @@ __device__ __forceinline__ void e4m3_values(uint32_t codes, float (&x)[4])
     x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
 }
 
-// Four elements from p on, where `whole`, else those below n (the others are 0).
+// Four consecutive elements as they lie in memory: one 16-, 8- or 4-byte access.
 template <class T>
-__device__ __forceinline__ void load_some(const T *p, int n, bool whole, float (&x)[4])
-{
-    if (whole) {
-        load4(p, x);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i < n ? to_f32(p[i]) : 0.0f;
-    }
-}
+struct alignas(4 * sizeof(T)) Quad {
+    T x[4];
+};
+
+// Those from p on, where `whole`, else the ones below n (the others are 0).
 template <class T>
-__device__ __forceinline__ void store_some(T *p, int n, bool whole, const float (&x)[4])
+__device__ __forceinline__ Quad<T> load_quad(const T *p, int n, bool whole)
 {
+    using Word = typename std::conditional<sizeof(T) == 4, uint4, typename std::conditional<sizeof(T) == 2, uint2, uint32_t>::type>::type;
+    union {
+        Word w;
+        Quad<T> q;
+    } v{};
     if (whole) {
-        store4(p, x);
+        v.w = *reinterpret_cast<const Word *>(p);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = from_f32<T>(x[i]);
+            if (i < n) v.q.x[i] = p[i];
     }
+    return v.q;
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t *p, int n, bool whole)
+template <class T>
+__device__ __forceinline__ void store_quad(T *p, int n, bool whole, const Quad<T> &q)
 {
-    if (whole) return *reinterpret_cast<const uint32_t *>(p);
-    uint32_t v = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < n) v |= static_cast<uint32_t>(p[i]) << (8 * i);
-    return v;
-}
-__device__ __forceinline__ void store_codes(uint8_t *p, int n, bool whole, uint32_t v)
-{
+    using Word = typename std::conditional<sizeof(T) == 4, uint4, typename std::conditional<sizeof(T) == 2, uint2, uint32_t>::type>::type;
     if (whole) {
-        *reinterpret_cast<uint32_t *>(p) = v;
+        *reinterpret_cast<Word *>(p) = *reinterpret_cast<const Word *>(&q);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = static_cast<uint8_t>(v >> (8 * i));
+            if (i < n) p[i] = q.x[i];
     }
+}
+template <class T>
+__device__ __forceinline__ void quad_values(const Quad<T> &q, float (&x)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = to_f32(q.x[i]);
+}
+template <class T>
+__device__ __forceinline__ Quad<T> quad_of(const float (&x)[4])
+{
+    Quad<T> q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.x[i] = from_f32<T>(x[i]);
+    return q;
 }
 
 // The exponent k of the smallest power of two >= 2^-126 with amax / 2^k <= 448 = 1.75 * 2^8.
-__device__ __forceinline__ int scale_exponent(float amax)
+__device__ __forceinline__ int scale_exponent(uint32_t amax_bits)
 {
-    return max(static_cast<int>((__float_as_uint(amax) + 0x1fffffu) >> 23) - 127 - 8, -126);
+    return max(static_cast<int>((amax_bits + 0x1fffffu) >> 23) - 127 - 8, -126);
 }
 __device__ __forceinline__ float power_of_two(int k) { return __uint_as_float(static_cast<uint32_t>(127 + k) << 23); }
 
-__device__ __forceinline__ float finite_magnitude(float x)
+// |x|'s bits, which order as it does; 0 where it is not finite.
+__device__ __forceinline__ uint32_t finite_magnitude(float x)
 {
-    const float m = fabsf(x);
-    return m < __int_as_float(0x7f800000) ? m : 0.0f;
+    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
 }
 
-// The largest of the warp's non-negative values.
-__device__ __forceinline__ float warp_max(float x) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x))); }
-
-// What a step does to four coordinates is written in two forms that give the same bits: AdamStep::pairs on packed
-// pairs and, in the 8-bit states, the quantizer below.
+// A step's arithmetic on four coordinates, in packed pairs.
 struct AdamStep {
     float factor, beta1, beta2, c1, c2, e, step, rate;
     F2 z;  // (-0, -0)
@@ -238,163 +246,269 @@ __device__ __forceinline__ uint32_t e4m3_codes(const float (&x)[4])
     return lo | static_cast<uint32_t>(hi) << 16;
 }
 
-// A warp takes blocks of 256 coordinates: four consecutive ones per lane in each half, so that every access of the
-// warp is one contiguous piece, and the block's scale is one warp reduction.  All loads of a block are issued before
-// the first is used.
+// Where a warp stands: its block's tensor and addresses, and how much of the block there is.
+template <class P, class G>
+struct AdamCursor {
+    int64_t u;       // block of the launch
+    int64_t block;   // of the tensor
+    int t, n;        // tensor; coordinates of the block
+    bool vec;        // a whole block, every address aligned to four elements
+    P *p;
+    const G *g;
+    void *m, *v;
+};
+
+// A block's loads: 4 coordinates in each half of the block per lane.
+template <class P, class G, class S>
+struct AdamBlock {
+    Quad<P> p[2];
+    Quad<G> g[2];
+    Quad<S> m[2], v[2];
+    float ms, vs;
+};
+
+// 8-bit states are handled as bytes, 32-bit ones as numbers.
+template <int BITS>
+using AdamCell = typename std::conditional<BITS == 32, float, uint8_t>::type;
+
+template <int BITS, class P, class G, class C>
+__device__ __forceinline__ void adam_seek(const AdamArgs &a, const GradList &list, int64_t u, AdamCursor<P, G> &c)
+{
+    using S = AdamCell<BITS>;
+    c.t = tensor_of(a.first, a.n_tensors, u, c.t);
+    const ea_adamw_tensor &T = a.tensors[c.t];
+    c.u = u;
+    c.block = u - a.first[c.t];
+    const int64_t at = c.block * kBlock;
+    c.n = static_cast<int>(min(T.size - at, static_cast<int64_t>(kBlock)));
+    c.p = static_cast<P *>(T.param) + at;
+    c.g = static_cast<const G *>(list.g[c.t]) + at;
+    c.m = static_cast<S *>(T.m) + at;
+    c.v = static_cast<S *>(T.v) + at;
+    // (a block's offset keeps the alignment of its tensor)
+    c.vec = c.n == kBlock && reinterpret_cast<uintptr_t>(c.p) % sizeof(Quad<P>) == 0 && reinterpret_cast<uintptr_t>(c.g) % sizeof(Quad<G>) == 0 &&
+            reinterpret_cast<uintptr_t>(T.copy) % sizeof(Quad<C>) == 0 &&
+            (reinterpret_cast<uintptr_t>(c.m) | reinterpret_cast<uintptr_t>(c.v)) % sizeof(Quad<S>) == 0;
+}
+
+template <int BITS, class P, class G>
+__device__ __forceinline__ void adam_load(const AdamArgs &a, const AdamCursor<P, G> &c, AdamBlock<P, G, AdamCell<BITS>> &b)
+{
+    using S = AdamCell<BITS>;
+    const int j0 = (threadIdx.x & 31) * 4;
+    const S *m = static_cast<const S *>(c.m), *v = static_cast<const S *>(c.v);
+    if (c.vec) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = j0 + 128 * h;
+            b.p[h] = load_quad(c.p + j, 4, true);
+            b.g[h] = load_quad(c.g + j, 4, true);
+            b.m[h] = load_quad(m + j, 4, true);
+            b.v[h] = load_quad(v + j, 4, true);
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = j0 + 128 * h;
+            b.p[h] = load_quad(c.p + j, c.n - j, false);
+            b.g[h] = load_quad(c.g + j, c.n - j, false);
+            b.m[h] = load_quad(m + j, c.n - j, false);
+            b.v[h] = load_quad(v + j, c.n - j, false);
+        }
+    }
+    if constexpr (BITS == 8) {
+        b.ms = a.tensors[c.t].m_scale[c.block];
+        b.vs = a.tensors[c.t].v_scale[c.block];
+    }
+}
+
+template <int BITS, class P, class G, class C>
+__device__ __forceinline__ void adam_store(const AdamArgs &a, const AdamCursor<P, G> &c, const float (&p)[2][4],
+                                           const Quad<AdamCell<BITS>> (&m)[2], const Quad<AdamCell<BITS>> (&v)[2])
+{
+    using S = AdamCell<BITS>;
+    const int j0 = (threadIdx.x & 31) * 4;
+    C *copy = static_cast<C *>(a.tensors[c.t].copy);
+    if (copy) copy += c.block * kBlock;
+    if (c.vec) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = j0 + 128 * h;
+            store_quad(c.p + j, 4, true, quad_of<P>(p[h]));
+            if (copy) store_quad(copy + j, 4, true, quad_of<C>(p[h]));
+            store_quad(static_cast<S *>(c.m) + j, 4, true, m[h]);
+            store_quad(static_cast<S *>(c.v) + j, 4, true, v[h]);
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = j0 + 128 * h, n = c.n - j;
+            store_quad(c.p + j, n, false, quad_of<P>(p[h]));
+            if (copy) store_quad(copy + j, n, false, quad_of<C>(p[h]));
+            store_quad(static_cast<S *>(c.m) + j, n, false, m[h]);
+            store_quad(static_cast<S *>(c.v) + j, n, false, v[h]);
+        }
+    }
+}
+
+// The 32-bit step of a block.
+template <class P, class G, class C>
+__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamState &, const AdamStep &s, const AdamCursor<P, G> &c,
+                                           const AdamBlock<P, G, float> &b)
+{
+    float p[2][4];
+    Quad<float> mq[2], vq[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float m[4], v[4], g[4], root[4];
+        quad_values(b.p[h], p[h]);
+        quad_values(b.g[h], g);
+        quad_values(b.m[h], m);
+        quad_values(b.v[h], v);
+        s.moments(m, v, g, s.beta1, s.beta2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[i]);
+        s.params(p[h], m, root, 1.0f);
+        mq[h] = quad_of<float>(m);
+        vq[h] = quad_of<float>(v);
+    }
+    adam_store<32, P, G, C>(a, c, p, mq, vq);
+}
+
+// The 8-bit step of a block.
+template <class P, class G, class C>
+__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamState &st, const AdamStep &s, const AdamCursor<P, G> &c,
+                                           const AdamBlock<P, G, uint8_t> &b)
+{
+    float m[2][4], v[2][4], p[2][4];
+    Quad<uint8_t> mq[2], vq[2];
+    // beta1 m scale and beta2 (r scale)^2 are one multiplication each where the power of two leaves the product
+    // normal: a scale below 2^-40 goes into the values first
+    const bool small = b.ms < 0x1p-40f || b.vs < 0x1p-40f;
+    const float mb = small ? s.beta1 : __fmul_rn(s.beta1, b.ms), vb = small ? s.beta2 : __fmul_rn(s.beta2, __fmul_rn(b.vs, b.vs));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.m[h]), m[h]);
+        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.v[h]), v[h]);
+    }
+    if (small)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m[i >> 2][i & 3] = __fmul_rn(m[i >> 2][i & 3], b.ms);
+            v[i >> 2][i & 3] = __fmul_rn(v[i >> 2][i & 3], b.vs);
+        }
+    uint32_t am = 0, av = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float g[4];
+        quad_values(b.g[h], g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[h][i] = __fmul_rn(v[h][i], v[h][i]);
+        s.moments(m[h], v[h], g, mb, vb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            am = max(am, __float_as_uint(fabsf(m[h][i])));
+            av = max(av, __float_as_uint(v[h][i]));
+        }
+    }
+    am = __reduce_max_sync(0xffffffffu, am);
+    av = __reduce_max_sync(0xffffffffu, av);
+    const bool finite = max(am, av) < 0x7f800000u;
+    if (!finite) {  // the scales go by the finite values; the others are held as NaN
+        am = av = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            am = max(am, finite_magnitude(m[i >> 2][i & 3]));
+            av = max(av, finite_magnitude(v[i >> 2][i & 3]));
+        }
+        am = __reduce_max_sync(0xffffffffu, am);
+        av = __reduce_max_sync(0xffffffffu, av);
+    }
+    // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
+    const bool lift = finite && av < (127u + 60u) << 23;
+    const float unit = lift ? 0x1p-32f : 1.0f;
+    const int km = scale_exponent(am), kv = scale_exponent(__float_as_uint(__fsqrt_rn(__uint_as_float(av))));
+    const float im = power_of_two(-km), iv = __fmul_rn(power_of_two(-kv), unit);
+    if ((threadIdx.x & 31) == 0) {
+        a.tensors[c.t].m_scale[c.block] = power_of_two(km);
+        a.tensors[c.t].v_scale[c.block] = power_of_two(kv);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float root[4];
+        if (lift) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) root[i] = __fmul_rn(v[h][i], 0x1p64f);
+            sqrt_pair(root[0], root[1]);
+            sqrt_pair(root[2], root[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
+        }
+        quad_values(b.p[h], p[h]);
+        s.params(p[h], m[h], root, unit);
+        const uint64_t quad = (static_cast<uint64_t>(c.block) * kBlock + 128 * h + (threadIdx.x & 31) * 4) >> 2;
+        const uint4 w = philox_words(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
+                                                static_cast<uint32_t>(a.tensor0 + c.t), static_cast<uint32_t>(st.t)), a.keys);
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        float ym[4], yv[4];
+        uint32_t rm[4], rv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ym[i] = __fmul_rn(fabsf(m[h][i]), im);
+            yv[i] = __fmul_rn(root[i], iv);
+            rm[i] = (word[i] << 4) & 0xffff0u;
+            rv[i] = (word[i] >> 12) & 0xffff0u;
+        }
+        round_e4m3<false>(ym, rm);
+        round_e4m3<true>(yv, rv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ym[i] = copysignf(ym[i], m[h][i]);
+        if (!finite)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!isfinite(m[h][i])) ym[i] = __int_as_float(0x7fc00000);
+                if (!isfinite(v[h][i])) yv[i] = __int_as_float(0x7fc00000);
+            }
+        *reinterpret_cast<uint32_t *>(&mq[h]) = e4m3_codes(ym);
+        *reinterpret_cast<uint32_t *>(&vq[h]) = e4m3_codes(yv);
+    }
+    adam_store<8, P, G, C>(a, c, p, mq, vq);
+}
+
+// A CTA takes a contiguous piece of the launch's blocks of 256 coordinates, its warps in turn: so a warp's tensor
+// seldom changes, and every CTA has the same number of blocks but for one.  A lane holds four consecutive
+// coordinates in each half of a block: every access of the warp is one contiguous piece, and the block's scale is
+// one warp reduction.  The next block's loads are issued before this one's arithmetic, 8-bit states' 70
+// instructions per coordinate.
 template <class P, class G, class C, int BITS>
 __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
 {
-    const int lane = threadIdx.x & 31;
+    constexpr int kWarps = kAdamThreads / 32;
     const float factor = a.clip ? a.clip[1] : 1.0f;
     const AdamState st = *a.state;
-    if (!isnan(factor)) {
-        const int64_t warps = static_cast<int64_t>(gridDim.x) * (kAdamThreads / 32);
+    const int64_t begin = a.units * blockIdx.x / gridDim.x, end = a.units * (blockIdx.x + 1) / gridDim.x;
+    AdamCursor<P, G> c;
+    c.t = 0;
+    int64_t u = begin + (threadIdx.x >> 5);
+    if (!isnan(factor) && u < end) {
         AdamStep s{factor, a.beta1, a.beta2, a.c1, a.c2, st.e, 0.0f, 0.0f, both(a.minus_zero)};
-        int t = 0;
-        for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kAdamThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
-            t = tensor_of(a.first, a.n_tensors, u, t);
-            const ea_adamw_tensor &T = a.tensors[t];
-            const int64_t block = u - a.first[t], base = block * kBlock;
-            const int n = static_cast<int>(min(T.size - base, static_cast<int64_t>(kBlock)));
-            P *p = static_cast<P *>(T.param) + base;
-            C *copy = T.copy ? static_cast<C *>(T.copy) + base : nullptr;
-            const G *g = static_cast<const G *>(list.g[t]) + base;
-            float *m32 = static_cast<float *>(T.m) + base, *v32 = static_cast<float *>(T.v) + base;
-            uint8_t *m8 = static_cast<uint8_t *>(T.m) + base, *v8 = static_cast<uint8_t *>(T.v) + base;
-            const uintptr_t state = reinterpret_cast<uintptr_t>(T.m) | reinterpret_cast<uintptr_t>(T.v);
-            const bool vec = n == kBlock && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(P)) == 0 &&
-                             reinterpret_cast<uintptr_t>(g) % (4 * sizeof(G)) == 0 &&
-                             reinterpret_cast<uintptr_t>(copy) % (4 * sizeof(C)) == 0 && state % (BITS == 32 ? 16 : 4) == 0;
-            float pk[2][4], gk[2][4], m[2][4], v[2][4];
-            uint32_t mc[2], vc[2];
-            float ms = 0.0f, vs = 0.0f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int j = h * 128 + lane * 4;
-                load_some(p + j, n - j, vec, pk[h]);
-                load_some(g + j, n - j, vec, gk[h]);
-                if constexpr (BITS == 32) {
-                    load_some(m32 + j, n - j, vec, m[h]);
-                    load_some(v32 + j, n - j, vec, v[h]);
-                } else {
-                    mc[h] = load_codes(m8 + j, n - j, vec);
-                    vc[h] = load_codes(v8 + j, n - j, vec);
-                }
+        AdamBlock<P, G, AdamCell<BITS>> b;
+        adam_seek<BITS, P, G, C>(a, list, u, c);
+        adam_load<BITS>(a, c, b);
+        while (true) {
+            const AdamCursor<P, G> now = c;
+            const AdamBlock<P, G, AdamCell<BITS>> block = b;
+            u += kWarps;
+            if (u < end) {
+                adam_seek<BITS, P, G, C>(a, list, u, c);
+                adam_load<BITS>(a, c, b);
             }
-            if constexpr (BITS == 8) {
-                ms = T.m_scale[block];
-                vs = T.v_scale[block];
-            }
-            const float lr = __fmul_rn(a.lr, T.lr_scale);
+            const float lr = __fmul_rn(a.lr, a.tensors[now.t].lr_scale);
             s.step = __fmul_rn(lr, st.a);
-            s.rate = __fmul_rn(lr, T.weight_decay);
-            if constexpr (BITS == 32) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = h * 128 + lane * 4;
-                    s.moments(m[h], v[h], gk[h], s.beta1, s.beta2);
-                    float root[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
-                    s.params(pk[h], m[h], root, 1.0f);
-                    store_some(p + j, n - j, vec, pk[h]);
-                    if (copy) store_some(copy + j, n - j, vec, pk[h]);
-                    store_some(m32 + j, n - j, vec, m[h]);
-                    store_some(v32 + j, n - j, vec, v[h]);
-                }
-            } else {
-                // beta1 m scale and beta2 (r scale)^2 are one multiplication each where the power of two leaves
-                // the product normal: a scale below 2^-40 goes into the values first
-                const bool small = ms < 0x1p-40f || vs < 0x1p-40f;
-                const float mb = small ? s.beta1 : __fmul_rn(s.beta1, ms), vb = small ? s.beta2 : __fmul_rn(s.beta2, __fmul_rn(vs, vs));
-                float am = 0.0f, av = 0.0f;
-                bool finite = true;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    e4m3_values(mc[h], m[h]);
-                    e4m3_values(vc[h], v[h]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (small) {
-                            m[h][i] = __fmul_rn(m[h][i], ms);
-                            v[h][i] = __fmul_rn(v[h][i], vs);
-                        }
-                        v[h][i] = __fmul_rn(v[h][i], v[h][i]);
-                    }
-                    s.moments(m[h], v[h], gk[h], mb, vb);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        am = __uint_as_float(max(__float_as_uint(am), __float_as_uint(fabsf(m[h][i]))));
-                        av = __uint_as_float(max(__float_as_uint(av), __float_as_uint(v[h][i])));
-                    }
-                }
-                am = warp_max(am);
-                av = warp_max(av);
-                finite = __float_as_uint(am) < 0x7f800000u && __float_as_uint(av) < 0x7f800000u;
-                if (!finite) {  // the scales go by the finite values; the others are held as NaN
-                    am = av = 0.0f;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            am = fmaxf(am, finite_magnitude(m[h][i]));
-                            av = fmaxf(av, finite_magnitude(v[h][i]));
-                        }
-                    am = warp_max(am);
-                    av = warp_max(av);
-                }
-                // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
-                const bool lift = finite && av < 0x1p60f;
-                const float unit = lift ? 0x1p-32f : 1.0f;
-                const int km = scale_exponent(am), kv = scale_exponent(__fsqrt_rn(av));
-                const float im = power_of_two(-km), iv = __fmul_rn(power_of_two(-kv), unit);
-                if (lane == 0) {
-                    T.m_scale[block] = power_of_two(km);
-                    T.v_scale[block] = power_of_two(kv);
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int j = h * 128 + lane * 4;
-                    float root[4];
-                    if (lift) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) root[i] = __fmul_rn(v[h][i], 0x1p64f);
-                        sqrt_pair(root[0], root[1]);
-                        sqrt_pair(root[2], root[3]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
-                    }
-                    s.params(pk[h], m[h], root, unit);
-                    store_some(p + j, n - j, vec, pk[h]);
-                    if (copy) store_some(copy + j, n - j, vec, pk[h]);
-                    const uint64_t quad = static_cast<uint64_t>(base + j) >> 2;
-                    const uint4 w = philox_words(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
-                                                            static_cast<uint32_t>(a.tensor0 + t), static_cast<uint32_t>(st.t)), a.keys);
-                    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-                    float ym[4], yv[4];
-                    uint32_t rm[4], rv[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        ym[i] = __fmul_rn(fabsf(m[h][i]), im);
-                        yv[i] = __fmul_rn(root[i], iv);
-                        rm[i] = (word[i] << 4) & 0xffff0u;
-                        rv[i] = (word[i] >> 12) & 0xffff0u;
-                    }
-                    round_e4m3<false>(ym, rm);
-                    round_e4m3<true>(yv, rv);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        ym[i] = copysignf(ym[i], m[h][i]);
-                        if (!finite) {
-                            if (!isfinite(m[h][i])) ym[i] = __int_as_float(0x7fc00000);
-                            if (!isfinite(v[h][i])) yv[i] = __int_as_float(0x7fc00000);
-                        }
-                    }
-                    store_codes(m8 + j, n - j, vec, e4m3_codes(ym));
-                    store_codes(v8 + j, n - j, vec, e4m3_codes(yv));
-                }
-            }
+            s.rate = __fmul_rn(lr, a.tensors[now.t].weight_decay);
+            adam_block<P, G, C>(a, st, s, now, block);
+            if (u >= end) break;
         }
     }
     if (!a.last) return;

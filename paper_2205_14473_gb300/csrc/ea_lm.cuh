@@ -1,5 +1,5 @@
-// ea_lm.cuh -- what the units of include/ea_lm.h share: element types, loads and stores of four
-// consecutive elements as binary32, the list of gradients that a launch carries, and the host's checks.
+// ea_lm.cuh -- what the units of include/ea_lm.h share: element types, launches, the list of gradients that a
+// launch carries, and the host's checks.
 #pragma once
 
 #include <algorithm>
@@ -34,32 +34,6 @@ template <>
 __device__ __forceinline__ bf16 from_f32<bf16>(float x) { return __float2bfloat16_rn(x); }
 template <>
 __device__ __forceinline__ f16 from_f32<f16>(float x) { return __float2half_rn(x); }
-
-// Four consecutive elements as one 16-, 8- or 4-byte access (aligned to its size).
-__device__ __forceinline__ void load4(const float *p, float (&x)[4])
-{
-    const float4 v = *reinterpret_cast<const float4 *>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-}
-template <class T>
-__device__ __forceinline__ void load4(const T *p, float (&x)[4])
-{
-    static_assert(sizeof(T) == 2);
-    alignas(8) T v[4];
-    *reinterpret_cast<uint2 *>(v) = *reinterpret_cast<const uint2 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = to_f32(v[i]);
-}
-__device__ __forceinline__ void store4(float *p, const float (&x)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-template <class T>
-__device__ __forceinline__ void store4(T *p, const float (&x)[4])
-{
-    static_assert(sizeof(T) == 2);
-    alignas(8) T v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = from_f32<T>(x[i]);
-    *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(v);
-}
 
 inline size_t type_bytes(int32_t type) { return type == EA_T_F32 || type == EA_T_I32 ? 4 : type == EA_T_I64 ? 8 : 2; }
 inline bool is_float_type(int32_t type) { return type == EA_T_F32 || type == EA_T_BF16 || type == EA_T_F16; }
