@@ -64,8 +64,6 @@ __device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
 // after it would be merged into one rounding, whatever their PTX says.
 __device__ __forceinline__ F2 mul2(F2 a, F2 b, F2 minus_zero) { return fma2(a, b, minus_zero); }
 
-__device__ __forceinline__ F2 negate2(F2 a) { return F2{a.v ^ 0x8000000080000000ull}; }
-
 // Within 2^-23 relative of the reciprocal of a normal number.
 __device__ __forceinline__ float recip_normal(float x)
 {
@@ -74,24 +72,24 @@ __device__ __forceinline__ float recip_normal(float x)
     return r;
 }
 
-// The square roots of two numbers, zero or normal, rounded to nearest: from y ~ 1 / sqrt(x), g = x y and h = y / 2
-// are refined together (Goldschmidt), g <- g + g (1/2 - g h), h <- h + h (1/2 - g h), and the remainder x - g^2,
-// exact in a fused operation, corrects g's last bit (Markstein, "Computation of elementary functions on the IBM
-// RISC System/6000 processor", 1990).  Equal to sqrtf for every number above 2^-100.  It is half the
-// instructions of two calls, and no branch stands between the eight coordinates of a lane.
-__device__ __forceinline__ void sqrt_pair(float &a, float &b)
+// The square roots of x = 2^64 (a, b), rounded to nearest; a and b zero or at least 2^-149.  From y ~ 1 / sqrt(x),
+// g = x y and -h = -y / 2 are refined together (Goldschmidt: g += g e, h += h e with e = 1/2 - g h), and the
+// remainder x - g^2, exact in a fused operation, corrects g's last bit (Markstein, "Computation of elementary
+// functions on the IBM RISC System/6000 processor", 1990).  Equal to sqrtf for every mantissa and parity of the
+// exponent, at a third of its instructions and with no branch between a lane's coordinates.
+__device__ __forceinline__ F2 sqrt_lifted(F2 v, F2 none)
 {
-    float ya, yb;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(fmaxf(a, 0x1p-126f)));
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(fmaxf(b, 0x1p-126f)));
-    const F2 x = pack2(a, b), y = pack2(ya, yb);
-    const F2 none = both(-0.0f);  // nothing here may be merged to another effect: every sum is a fused one already
-    F2 g = fma2(x, y, none), h = fma2(y, both(0.5f), none);
-    const F2 e = fma2(negate2(g), h, both(0.5f));
+    float xa, xb, ya, yb;
+    const F2 x = fma2(v, both(0x1p64f), none), minus_x = fma2(v, both(-0x1p64f), none);
+    unpack2(fma2(v, both(0x1p64f), both(0x1p-100f)), xa, xb);  // not zero
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(xa));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(xb));
+    const F2 y = pack2(ya, yb);
+    F2 g = fma2(x, y, none), h = fma2(y, both(-0.5f), none);
+    const F2 e = fma2(g, h, both(0.5f));
     g = fma2(g, e, g);
     h = fma2(h, e, h);
-    g = fma2(fma2(negate2(g), g, x), h, g);
-    unpack2(g, a, b);
+    return fma2(fma2(g, g, minus_x), h, g);
 }
 
 // Philox4x32-10 with the round keys formed once on the host.
@@ -182,80 +180,95 @@ __device__ __forceinline__ uint32_t finite_magnitude(float x)
 
 // A step's arithmetic on four coordinates, in packed pairs.
 struct AdamStep {
-    float factor, beta1, beta2, c1, c2, e, step, rate;
-    F2 z;  // (-0, -0)
-
-    // The new parameters, from the moments and the second one's root (times `unit`, a power of two).
-    __device__ __forceinline__ void params(float (&p)[4], const float (&m)[4], const float (&root)[4], float unit) const
-    {
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            float d0, d1;
-            unpack2(fma2(pack2(root[i], root[i + 1]), both(unit), both(e)), d0, d1);
-            const F2 q = mul2(pack2(m[i], m[i + 1]), pack2(recip_normal(d0), recip_normal(d1)), z);
-            const F2 x = pack2(p[i], p[i + 1]), d = add2(mul2(x, both(rate), z), mul2(q, both(step), z));
-            unpack2(fma2(d, both(-1.0f), x), p[i], p[i + 1]);
-        }
-    }
+    F2 factor, beta1, beta2, c1, c2, e, step, rate;
+    F2 none;  // (-0, -0)
 
     // m <- mb m + c1 g and v <- vb v + c2 g^2 with g the gradient times the factor.
-    __device__ __forceinline__ void moments(float (&m)[4], float (&v)[4], const float (&grad)[4], float mb, float vb) const
+    __device__ __forceinline__ void moments(F2 &m, F2 &v, F2 grad, F2 mb, F2 vb) const
     {
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            const F2 g = mul2(pack2(grad[i], grad[i + 1]), both(factor), z);
-            unpack2(add2(mul2(pack2(m[i], m[i + 1]), both(mb), z), mul2(g, both(c1), z)), m[i], m[i + 1]);
-            unpack2(add2(mul2(pack2(v[i], v[i + 1]), both(vb), z), mul2(mul2(g, g, z), both(c2), z)), v[i], v[i + 1]);
-        }
+        const F2 g = mul2(grad, factor, none);
+        m = add2(mul2(m, mb, none), mul2(g, c1, none));
+        v = add2(mul2(v, vb, none), mul2(mul2(g, g, none), c2, none));
+    }
+
+    // The new parameters, from the moments and the second one's root (times `unit`, a power of two).
+    __device__ __forceinline__ F2 params(F2 p, F2 m, F2 root, F2 unit) const
+    {
+        float a, b;
+        unpack2(fma2(root, unit, e), a, b);
+        const F2 q = mul2(m, pack2(recip_normal(a), recip_normal(b)), none);
+        return fma2(fma2(q, step, mul2(p, rate, none)), both(-1.0f), p);
     }
 };
 
-// Four magnitudes y <= 448 (but for the root's last bit, which saturates) in e4m3, rounded up with the probability
-// of the remainder.  A normal number's 20 bits below its third mantissa bit get a random number added and are cut
-// off; below 2^-6 the grid's spacing is 2^-9 throughout.  r: 16 random bits each, in bits 4 .. 19.
-template <bool KEEP_NONZERO>
-__device__ __forceinline__ void round_e4m3(float (&y)[4], const uint32_t (&r)[4])
+__device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+
+// max(|a|, |b|), NaN if either is.
+__device__ __forceinline__ float max_magnitude(float a, float b)
 {
-    constexpr uint32_t kNormal = (127u - 6u) << 23;
-    uint32_t least = 0xffffffffu;
-    float q[4];
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
+// Codes of four values x with |x| <= 448 in e4m3, the magnitudes rounded up with the probability of the remainder
+// (word: random bits, the low half's or, HIGH, the high half's).
+//   normal numbers: the code is the float's exponent and first three mantissa bits, re-biased: with the 20 bits
+//     below at the top of a register's lower 24, 16 random bits are added there and the carry does the rounding --
+//     one byte permutation, which also brings in the bias, and one multiply-add per value.  The sign is shifted out;
+//   below 2^-6 the grid's spacing is 2^-9 throughout: taken value by value, where there is one.
+// CLAMP: a value that is not zero does not become zero.
+template <bool HIGH, bool CLAMP>
+__device__ __forceinline__ uint32_t e4m3_round(const float (&x)[4], const uint32_t (&word)[4], bool finite)
+{
+    uint32_t t[4];
+    const float least = fminf(fminf(fabsf(x[0]), fabsf(x[1])), fminf(fabsf(x[2]), fabsf(x[3])));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        q[i] = __uint_as_float((__float_as_uint(y[i]) + r[i]) & 0xfff00000u);
-        least = min(least, __float_as_uint(y[i]) - 1u);
-    }
-    if (least < kNormal - 1u) {  // some 0 < y < 2^-6
+    for (int i = 0; i < 4; ++i) t[i] = bits(x[i]) * 16u + __byte_perm(word[i], 0x00400000u, HIGH ? 0x6324 : 0x6104);
+    if (least < 0x1p-6f || !finite) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (__float_as_uint(y[i]) - 1u < kNormal - 1u) {
-                const float up = __fmaf_rn(static_cast<float>(r[i]), 0x1p-20f, __fmul_rn(y[i], 512.0f));
-                const float n = __fsub_rn(__fadd_rd(up, 0x1p23f), 0x1p23f);  // its floor
-                q[i] = __fmul_rn(KEEP_NONZERO ? fmaxf(n, 1.0f) : n, 0x1p-9f);
+        for (int i = 0; i < 4; ++i) {
+            const float y = fabsf(x[i]);
+            if (y < 0x1p-6f) {
+                const float r = static_cast<float>(HIGH ? word[i] >> 16 : word[i] & 0xffffu);
+                const float up = __fmaf_rn(r, 0x1p-16f, __fmul_rn(y, 512.0f));
+                const uint32_t n = static_cast<uint32_t>(__float2int_rd(up));
+                t[i] = (CLAMP && y > 0.0f ? max(n, 1u) : n) << 24;
+            } else if (!(y < __int_as_float(0x7f800000))) {
+                t[i] = 0x7f000000u;
             }
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = q[i];
+    uint32_t codes = __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
+    if (!CLAMP) {  // signed values
+        const uint32_t signs = __byte_perm(__byte_perm(bits(x[0]), bits(x[1]), 0x0073), __byte_perm(bits(x[2]), bits(x[3]), 0x0073), 0x5410);
+        codes |= signs & 0x80808080u;
+    }
+    return codes;
 }
 
-// Codes of four values of the format (the last one's in the highest byte); NaN stays NaN.
-__device__ __forceinline__ uint32_t e4m3_codes(const float (&x)[4])
-{
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1]), "f"(x[0]));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3]), "f"(x[2]));
-    return lo | static_cast<uint32_t>(hi) << 16;
-}
+// 8-bit states are handled as bytes, 32-bit ones as numbers.
+template <int BITS>
+using AdamCell = typename std::conditional<BITS == 32, float, uint8_t>::type;
 
-// Where a warp stands: its block's tensor and addresses, and how much of the block there is.
-template <class P, class G>
-struct AdamCursor {
-    int64_t u;       // block of the launch
-    int64_t block;   // of the tensor
-    int t, n;        // tensor; coordinates of the block
-    bool vec;        // a whole block, every address aligned to four elements
+// Addresses of this lane's first coordinate in a block, and of the block's scales.
+template <class P, class G, class C, class S>
+struct AdamPlace {
     P *p;
     const G *g;
-    void *m, *v;
+    C *copy;
+    S *m, *v;
+    float *ms, *vs;
+    __device__ __forceinline__ void advance(int blocks)
+    {
+        p += blocks * kBlock;
+        g += blocks * kBlock;
+        if (copy) copy += blocks * kBlock;
+        m += blocks * kBlock;
+        v += blocks * kBlock;
+        ms += blocks;
+        vs += blocks;
+    }
 };
 
 // A block's loads: 4 coordinates in each half of the block per lane.
@@ -267,248 +280,205 @@ struct AdamBlock {
     float ms, vs;
 };
 
-// 8-bit states are handled as bytes, 32-bit ones as numbers.
-template <int BITS>
-using AdamCell = typename std::conditional<BITS == 32, float, uint8_t>::type;
-
-template <int BITS, class P, class G, class C>
-__device__ __forceinline__ void adam_seek(const AdamArgs &a, const GradList &list, int64_t u, AdamCursor<P, G> &c)
+// WHOLE: a whole block whose addresses are all aligned to four elements; else n coordinates of one, from this
+// lane's first on.
+template <bool WHOLE, int BITS, class P, class G, class C, class S>
+__device__ __forceinline__ void adam_load(const AdamPlace<P, G, C, S> &at, int n, AdamBlock<P, G, S> &b)
 {
-    using S = AdamCell<BITS>;
-    c.t = tensor_of(a.first, a.n_tensors, u, c.t);
-    const ea_adamw_tensor &T = a.tensors[c.t];
-    c.u = u;
-    c.block = u - a.first[c.t];
-    const int64_t at = c.block * kBlock;
-    c.n = static_cast<int>(min(T.size - at, static_cast<int64_t>(kBlock)));
-    c.p = static_cast<P *>(T.param) + at;
-    c.g = static_cast<const G *>(list.g[c.t]) + at;
-    c.m = static_cast<S *>(T.m) + at;
-    c.v = static_cast<S *>(T.v) + at;
-    // (a block's offset keeps the alignment of its tensor)
-    c.vec = c.n == kBlock && reinterpret_cast<uintptr_t>(c.p) % sizeof(Quad<P>) == 0 && reinterpret_cast<uintptr_t>(c.g) % sizeof(Quad<G>) == 0 &&
-            reinterpret_cast<uintptr_t>(T.copy) % sizeof(Quad<C>) == 0 &&
-            (reinterpret_cast<uintptr_t>(c.m) | reinterpret_cast<uintptr_t>(c.v)) % sizeof(Quad<S>) == 0;
-}
-
-template <int BITS, class P, class G>
-__device__ __forceinline__ void adam_load(const AdamArgs &a, const AdamCursor<P, G> &c, AdamBlock<P, G, AdamCell<BITS>> &b)
-{
-    using S = AdamCell<BITS>;
-    const int j0 = (threadIdx.x & 31) * 4;
-    const S *m = static_cast<const S *>(c.m), *v = static_cast<const S *>(c.v);
-    if (c.vec) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = j0 + 128 * h;
-            b.p[h] = load_quad(c.p + j, 4, true);
-            b.g[h] = load_quad(c.g + j, 4, true);
-            b.m[h] = load_quad(m + j, 4, true);
-            b.v[h] = load_quad(v + j, 4, true);
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = j0 + 128 * h;
-            b.p[h] = load_quad(c.p + j, c.n - j, false);
-            b.g[h] = load_quad(c.g + j, c.n - j, false);
-            b.m[h] = load_quad(m + j, c.n - j, false);
-            b.v[h] = load_quad(v + j, c.n - j, false);
-        }
+    for (int h = 0; h < 2; ++h) {
+        b.p[h] = load_quad(at.p + 128 * h, n - 128 * h, WHOLE);
+        b.g[h] = load_quad(at.g + 128 * h, n - 128 * h, WHOLE);
+        b.m[h] = load_quad(at.m + 128 * h, n - 128 * h, WHOLE);
+        b.v[h] = load_quad(at.v + 128 * h, n - 128 * h, WHOLE);
     }
-    if constexpr (BITS == 8) {
-        b.ms = a.tensors[c.t].m_scale[c.block];
-        b.vs = a.tensors[c.t].v_scale[c.block];
+    if (BITS == 8) {
+        b.ms = *at.ms;
+        b.vs = *at.vs;
     }
 }
 
-template <int BITS, class P, class G, class C>
-__device__ __forceinline__ void adam_store(const AdamArgs &a, const AdamCursor<P, G> &c, const float (&p)[2][4],
-                                           const Quad<AdamCell<BITS>> (&m)[2], const Quad<AdamCell<BITS>> (&v)[2])
+template <bool WHOLE, class P, class G, class C, class S>
+__device__ __forceinline__ void adam_store(const AdamPlace<P, G, C, S> &at, int n, int h, const float (&p)[4], const Quad<S> &m, const Quad<S> &v)
 {
-    using S = AdamCell<BITS>;
-    const int j0 = (threadIdx.x & 31) * 4;
-    C *copy = static_cast<C *>(a.tensors[c.t].copy);
-    if (copy) copy += c.block * kBlock;
-    if (c.vec) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = j0 + 128 * h;
-            store_quad(c.p + j, 4, true, quad_of<P>(p[h]));
-            if (copy) store_quad(copy + j, 4, true, quad_of<C>(p[h]));
-            store_quad(static_cast<S *>(c.m) + j, 4, true, m[h]);
-            store_quad(static_cast<S *>(c.v) + j, 4, true, v[h]);
-        }
-    } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = j0 + 128 * h, n = c.n - j;
-            store_quad(c.p + j, n, false, quad_of<P>(p[h]));
-            if (copy) store_quad(copy + j, n, false, quad_of<C>(p[h]));
-            store_quad(static_cast<S *>(c.m) + j, n, false, m[h]);
-            store_quad(static_cast<S *>(c.v) + j, n, false, v[h]);
-        }
-    }
+    store_quad(at.p + 128 * h, n - 128 * h, WHOLE, quad_of<P>(p));
+    if (at.copy) store_quad(at.copy + 128 * h, n - 128 * h, WHOLE, quad_of<C>(p));
+    store_quad(at.m + 128 * h, n - 128 * h, WHOLE, m);
+    store_quad(at.v + 128 * h, n - 128 * h, WHOLE, v);
 }
 
 // The 32-bit step of a block.
-template <class P, class G, class C>
-__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamState &, const AdamStep &s, const AdamCursor<P, G> &c,
-                                           const AdamBlock<P, G, float> &b)
+template <bool WHOLE, class P, class G, class C>
+__device__ __forceinline__ void adam_block(const AdamArgs &, const AdamStep &s, const AdamPlace<P, G, C, float> &at, int n,
+                                           const AdamBlock<P, G, float> &b, uint64_t, uint32_t, uint32_t)
 {
-    float p[2][4];
-    Quad<float> mq[2], vq[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        float m[4], v[4], g[4], root[4];
-        quad_values(b.p[h], p[h]);
+        float p[4], m[4], v[4], g[4];
+        quad_values(b.p[h], p);
         quad_values(b.g[h], g);
         quad_values(b.m[h], m);
         quad_values(b.v[h], v);
-        s.moments(m, v, g, s.beta1, s.beta2);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[i]);
-        s.params(p[h], m, root, 1.0f);
-        mq[h] = quad_of<float>(m);
-        vq[h] = quad_of<float>(v);
+        for (int i = 0; i < 4; i += 2) {
+            F2 m2 = pack2(m[i], m[i + 1]), v2 = pack2(v[i], v[i + 1]);
+            s.moments(m2, v2, pack2(g[i], g[i + 1]), s.beta1, s.beta2);
+            unpack2(m2, m[i], m[i + 1]);
+            unpack2(v2, v[i], v[i + 1]);
+            const F2 root = pack2(__fsqrt_rn(v[i]), __fsqrt_rn(v[i + 1]));
+            unpack2(s.params(pack2(p[i], p[i + 1]), m2, root, both(1.0f)), p[i], p[i + 1]);
+        }
+        adam_store<WHOLE>(at, n, h, p, quad_of<float>(m), quad_of<float>(v));
     }
-    adam_store<32, P, G, C>(a, c, p, mq, vq);
 }
 
-// The 8-bit step of a block.
-template <class P, class G, class C>
-__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamState &st, const AdamStep &s, const AdamCursor<P, G> &c,
-                                           const AdamBlock<P, G, uint8_t> &b)
+// The 8-bit step of a block.  quad: its first group of four coordinates of this lane, within the tensor.
+template <bool WHOLE, class P, class G, class C>
+__device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s, const AdamPlace<P, G, C, uint8_t> &at, int n,
+                                           const AdamBlock<P, G, uint8_t> &b, uint64_t quad, uint32_t tensor, uint32_t t)
 {
-    float m[2][4], v[2][4], p[2][4];
-    Quad<uint8_t> mq[2], vq[2];
+    F2 m[4], v[4];
     // beta1 m scale and beta2 (r scale)^2 are one multiplication each where the power of two leaves the product
     // normal: a scale below 2^-40 goes into the values first
     const bool small = b.ms < 0x1p-40f || b.vs < 0x1p-40f;
-    const float mb = small ? s.beta1 : __fmul_rn(s.beta1, b.ms), vb = small ? s.beta2 : __fmul_rn(s.beta2, __fmul_rn(b.vs, b.vs));
+    const F2 mb = small ? s.beta1 : mul2(s.beta1, both(b.ms), s.none);
+    const F2 vb = small ? s.beta2 : mul2(s.beta2, mul2(both(b.vs), both(b.vs), s.none), s.none);
+    float am = 0.0f, av = 0.0f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.m[h]), m[h]);
-        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.v[h]), v[h]);
-    }
-    if (small)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i >> 2][i & 3] = __fmul_rn(m[i >> 2][i & 3], b.ms);
-            v[i >> 2][i & 3] = __fmul_rn(v[i >> 2][i & 3], b.vs);
-        }
-    uint32_t am = 0, av = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        float g[4];
+        float mx[4], vx[4], g[4];
+        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.m[h]), mx);
+        e4m3_values(*reinterpret_cast<const uint32_t *>(&b.v[h]), vx);
         quad_values(b.g[h], g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[h][i] = __fmul_rn(v[h][i], v[h][i]);
-        s.moments(m[h], v[h], g, mb, vb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            am = max(am, __float_as_uint(fabsf(m[h][i])));
-            av = max(av, __float_as_uint(v[h][i]));
-        }
-    }
-    am = __reduce_max_sync(0xffffffffu, am);
-    av = __reduce_max_sync(0xffffffffu, av);
-    const bool finite = max(am, av) < 0x7f800000u;
-    if (!finite) {  // the scales go by the finite values; the others are held as NaN
-        am = av = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            am = max(am, finite_magnitude(m[i >> 2][i & 3]));
-            av = max(av, finite_magnitude(v[i >> 2][i & 3]));
-        }
-        am = __reduce_max_sync(0xffffffffu, am);
-        av = __reduce_max_sync(0xffffffffu, av);
-    }
-    // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
-    const bool lift = finite && av < (127u + 60u) << 23;
-    const float unit = lift ? 0x1p-32f : 1.0f;
-    const int km = scale_exponent(am), kv = scale_exponent(__float_as_uint(__fsqrt_rn(__uint_as_float(av))));
-    const float im = power_of_two(-km), iv = __fmul_rn(power_of_two(-kv), unit);
-    if ((threadIdx.x & 31) == 0) {
-        a.tensors[c.t].m_scale[c.block] = power_of_two(km);
-        a.tensors[c.t].v_scale[c.block] = power_of_two(kv);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        float root[4];
-        if (lift) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) root[i] = __fmul_rn(v[h][i], 0x1p64f);
-            sqrt_pair(root[0], root[1]);
-            sqrt_pair(root[2], root[3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) root[i] = __fsqrt_rn(v[h][i]);
-        }
-        quad_values(b.p[h], p[h]);
-        s.params(p[h], m[h], root, unit);
-        const uint64_t quad = (static_cast<uint64_t>(c.block) * kBlock + 128 * h + (threadIdx.x & 31) * 4) >> 2;
-        const uint4 w = philox_words(make_uint4(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32),
-                                                static_cast<uint32_t>(a.tensor0 + c.t), static_cast<uint32_t>(st.t)), a.keys);
-        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-        float ym[4], yv[4];
-        uint32_t rm[4], rv[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            ym[i] = __fmul_rn(fabsf(m[h][i]), im);
-            yv[i] = __fmul_rn(root[i], iv);
-            rm[i] = (word[i] << 4) & 0xffff0u;
-            rv[i] = (word[i] >> 12) & 0xffff0u;
-        }
-        round_e4m3<false>(ym, rm);
-        round_e4m3<true>(yv, rv);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ym[i] = copysignf(ym[i], m[h][i]);
-        if (!finite)
+        if (small)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (!isfinite(m[h][i])) ym[i] = __int_as_float(0x7fc00000);
-                if (!isfinite(v[h][i])) yv[i] = __int_as_float(0x7fc00000);
+                mx[i] = __fmul_rn(mx[i], b.ms);
+                vx[i] = __fmul_rn(vx[i], b.vs);
             }
-        *reinterpret_cast<uint32_t *>(&mq[h]) = e4m3_codes(ym);
-        *reinterpret_cast<uint32_t *>(&vq[h]) = e4m3_codes(yv);
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            F2 &m2 = m[2 * h + i / 2], &v2 = v[2 * h + i / 2];
+            m2 = pack2(mx[i], mx[i + 1]);
+            v2 = pack2(vx[i], vx[i + 1]);
+            v2 = mul2(v2, v2, s.none);
+            s.moments(m2, v2, pack2(g[i], g[i + 1]), mb, vb);
+            float x, y;
+            unpack2(m2, x, y);
+            am = max_magnitude(max_magnitude(am, x), y);
+            unpack2(v2, x, y);
+            av = max_magnitude(max_magnitude(av, x), y);
+        }
     }
-    adam_store<8, P, G, C>(a, c, p, mq, vq);
+    uint32_t mmax = __reduce_max_sync(0xffffffffu, bits(am)), vmax = __reduce_max_sync(0xffffffffu, bits(av));
+    const bool finite = max(mmax, vmax) < 0x7f800000u;
+    if (!finite) {  // the scales go by the finite values; the others are held as NaN
+        mmax = vmax = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x, y;
+            unpack2(m[i], x, y);
+            mmax = max(mmax, max(finite_magnitude(x), finite_magnitude(y)));
+            unpack2(v[i], x, y);
+            vmax = max(vmax, max(finite_magnitude(x), finite_magnitude(y)));
+        }
+        mmax = __reduce_max_sync(0xffffffffu, mmax);
+        vmax = __reduce_max_sync(0xffffffffu, vmax);
+    }
+    // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
+    const bool lift = finite && vmax < (127u + 60u) << 23;
+    const F2 unit = both(lift ? 0x1p-32f : 1.0f);
+    const int km = scale_exponent(mmax), kv = scale_exponent(bits(__fsqrt_rn(__uint_as_float(vmax))));
+    const F2 im = both(power_of_two(-km)), iv = mul2(both(power_of_two(-kv)), unit, s.none);
+    if ((threadIdx.x & 31) == 0) {
+        *at.ms = power_of_two(km);
+        *at.vs = power_of_two(kv);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float p[4], ym[4], yv[4];
+        quad_values(b.p[h], p);
+        const uint64_t q = quad + 32 * h;
+        const uint4 w = philox_words(make_uint4(static_cast<uint32_t>(q), static_cast<uint32_t>(q >> 32), tensor, t), a.keys);
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const F2 m2 = m[2 * h + i / 2], v2 = v[2 * h + i / 2];
+            F2 root;
+            if (lift) {
+                root = sqrt_lifted(v2, s.none);
+            } else {
+                float x, y;
+                unpack2(v2, x, y);
+                root = pack2(__fsqrt_rn(x), __fsqrt_rn(y));
+            }
+            unpack2(s.params(pack2(p[i], p[i + 1]), m2, root, unit), p[i], p[i + 1]);
+            unpack2(mul2(m2, im, s.none), ym[i], ym[i + 1]);
+            unpack2(mul2(root, iv, s.none), yv[i], yv[i + 1]);
+        }
+        Quad<uint8_t> mq, vq;
+        *reinterpret_cast<uint32_t *>(&mq) = mmax || !finite ? e4m3_round<false, false>(ym, word, finite) : 0;
+        *reinterpret_cast<uint32_t *>(&vq) = vmax || !finite ? e4m3_round<true, true>(yv, word, finite) : 0;
+        adam_store<WHOLE>(at, n, h, p, mq, vq);
+    }
 }
 
-// A CTA takes a contiguous piece of the launch's blocks of 256 coordinates, its warps in turn: so a warp's tensor
-// seldom changes, and every CTA has the same number of blocks but for one.  A lane holds four consecutive
-// coordinates in each half of a block: every access of the warp is one contiguous piece, and the block's scale is
-// one warp reduction.  The next block's loads are issued before this one's arithmetic, 8-bit states' 70
-// instructions per coordinate.
+// A CTA takes a contiguous piece of the launch's blocks of 256 coordinates, its warps in turn: every CTA has the same
+// number of blocks but for one, and a warp goes along a tensor with its addresses in registers.  A lane holds four
+// consecutive coordinates in each half of a block: every access of the warp is one contiguous piece, and the block's
+// scale is one warp reduction.  Whole aligned blocks have the next one's loads issued before their arithmetic.
 template <class P, class G, class C, int BITS>
 __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
 {
+    using S = AdamCell<BITS>;
     constexpr int kWarps = kAdamThreads / 32;
     const float factor = a.clip ? a.clip[1] : 1.0f;
     const AdamState st = *a.state;
     const int64_t begin = a.units * blockIdx.x / gridDim.x, end = a.units * (blockIdx.x + 1) / gridDim.x;
-    AdamCursor<P, G> c;
-    c.t = 0;
-    int64_t u = begin + (threadIdx.x >> 5);
-    if (!isnan(factor) && u < end) {
-        AdamStep s{factor, a.beta1, a.beta2, a.c1, a.c2, st.e, 0.0f, 0.0f, both(a.minus_zero)};
-        AdamBlock<P, G, AdamCell<BITS>> b;
-        adam_seek<BITS, P, G, C>(a, list, u, c);
-        adam_load<BITS>(a, c, b);
-        while (true) {
-            const AdamCursor<P, G> now = c;
-            const AdamBlock<P, G, AdamCell<BITS>> block = b;
-            u += kWarps;
-            if (u < end) {
-                adam_seek<BITS, P, G, C>(a, list, u, c);
-                adam_load<BITS>(a, c, b);
+    if (!isnan(factor) && begin < end) {
+        const int warp = threadIdx.x >> 5, lane4 = (threadIdx.x & 31) * 4;
+        AdamStep s{both(factor), both(a.beta1), both(a.beta2), both(a.c1), both(a.c2), both(st.e), F2{}, F2{}, both(a.minus_zero)};
+        for (int i = tensor_of(a.first, a.n_tensors, begin, 0); i < a.n_tensors; ++i) {
+            const int64_t first = a.first[i], lo = max(begin, first), hi = min(end, a.first[i + 1]);
+            if (first >= end) break;
+            int64_t u = lo + ((warp - (lo - begin)) & (kWarps - 1));  // this warp's next block
+            if (u >= hi) continue;
+            const ea_adamw_tensor &T = a.tensors[i];
+            const int64_t size = T.size, off = (u - first) * kBlock + lane4;
+            const float lr = __fmul_rn(a.lr, T.lr_scale);
+            s.step = both(__fmul_rn(lr, st.a));
+            s.rate = both(__fmul_rn(lr, T.weight_decay));
+            AdamPlace<P, G, C, S> at{static_cast<P *>(T.param) + off, static_cast<const G *>(list.g[i]) + off,
+                                     T.copy ? static_cast<C *>(T.copy) + off : nullptr, static_cast<S *>(T.m) + off,
+                                     static_cast<S *>(T.v) + off, T.m_scale + (u - first), T.v_scale + (u - first)};
+            const uint32_t tensor = static_cast<uint32_t>(a.tensor0 + i), t = static_cast<uint32_t>(st.t);
+            uint64_t quad = static_cast<uint64_t>(off) >> 2;
+            const bool aligned = reinterpret_cast<uintptr_t>(at.p) % sizeof(Quad<P>) == 0 && reinterpret_cast<uintptr_t>(at.g) % sizeof(Quad<G>) == 0 &&
+                                 reinterpret_cast<uintptr_t>(at.copy) % sizeof(Quad<C>) == 0 &&
+                                 (reinterpret_cast<uintptr_t>(at.m) | reinterpret_cast<uintptr_t>(at.v)) % sizeof(Quad<S>) == 0;
+            const int64_t whole = aligned ? min(hi, first + size / kBlock) : u;  // blocks below it are whole and aligned
+            AdamBlock<P, G, S> b;
+            if (u < whole) {
+                adam_load<true, BITS>(at, kBlock, b);
+#pragma unroll 2
+                while (true) {
+                    const AdamBlock<P, G, S> now = b;
+                    const AdamPlace<P, G, C, S> here = at;
+                    u += kWarps;
+                    at.advance(kWarps);
+                    if (u < whole) adam_load<true, BITS>(at, kBlock, b);
+                    adam_block<true>(a, s, here, kBlock, now, quad, tensor, t);
+                    quad += kWarps * kBlock / 4;
+                    if (u >= whole) break;
+                }
             }
-            const float lr = __fmul_rn(a.lr, a.tensors[now.t].lr_scale);
-            s.step = __fmul_rn(lr, st.a);
-            s.rate = __fmul_rn(lr, a.tensors[now.t].weight_decay);
-            adam_block<P, G, C>(a, st, s, now, block);
-            if (u >= end) break;
+            for (; u < hi; u += kWarps) {
+                const int n = static_cast<int>(min(size - (u - first) * kBlock, static_cast<int64_t>(kBlock))) - lane4;
+                adam_load<false, BITS>(at, n, b);
+                adam_block<false>(a, s, at, n, b, quad, tensor, t);
+                at.advance(kWarps);
+                quad += kWarps * kBlock / 4;
+            }
         }
     }
     if (!a.last) return;
