@@ -5,6 +5,7 @@
 
 #include <type_traits>
 
+#include "ea_async.cuh"
 #include "ea_lm.cuh"
 
 namespace ea {
@@ -72,11 +73,11 @@ __device__ __forceinline__ float recip_normal(float x)
     return r;
 }
 
-// The square roots of x = 2^64 (a, b), rounded to nearest; a and b zero or at least 2^-149.  From y ~ 1 / sqrt(x),
-// g = x y and -h = -y / 2 are refined together (Goldschmidt: g += g e, h += h e with e = 1/2 - g h), and the
-// remainder x - g^2, exact in a fused operation, corrects g's last bit (Markstein, "Computation of elementary
-// functions on the IBM RISC System/6000 processor", 1990).  Equal to sqrtf for every mantissa and parity of the
-// exponent, at a third of its instructions and with no branch between a lane's coordinates.
+// The square roots of 2^64 v for two v, zero or at least 2^-149, rounded to nearest: from y ~ 1 / sqrt(x), the
+// remainder x - g^2 of g = x y, exact in a fused operation, corrects g to its last bit (Markstein, "Computation of
+// elementary functions on the IBM RISC System/6000 processor", 1990; without the refinement of y and g that the paper
+// has in between).  Compared with sqrtf for every mantissa in both parities of the exponent, and for subnormal v: equal.
+// It is a third of the call's instructions, and no branch stands between a lane's coordinates.
 __device__ __forceinline__ F2 sqrt_lifted(F2 v, F2 none)
 {
     float xa, xb, ya, yb;
@@ -84,12 +85,8 @@ __device__ __forceinline__ F2 sqrt_lifted(F2 v, F2 none)
     unpack2(fma2(v, both(0x1p64f), both(0x1p-100f)), xa, xb);  // not zero
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(ya) : "f"(xa));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(yb) : "f"(xb));
-    const F2 y = pack2(ya, yb);
-    F2 g = fma2(x, y, none), h = fma2(y, both(-0.5f), none);
-    const F2 e = fma2(g, h, both(0.5f));
-    g = fma2(g, e, g);
-    h = fma2(h, e, h);
-    return fma2(fma2(g, g, minus_x), h, g);
+    const F2 y = pack2(ya, yb), g = fma2(x, y, none);
+    return fma2(fma2(g, g, minus_x), fma2(y, both(-0.5f), none), g);
 }
 
 // Philox4x32-10 with the round keys formed once on the host.
@@ -271,33 +268,75 @@ struct AdamPlace {
     }
 };
 
-// A block's loads: 4 coordinates in each half of the block per lane.
+// What a lane reads of a block: 4 coordinates in each half.
 template <class P, class G, class S>
 struct AdamBlock {
     Quad<P> p[2];
     Quad<G> g[2];
     Quad<S> m[2], v[2];
-    float ms, vs;
 };
 
-// WHOLE: a whole block whose addresses are all aligned to four elements; else n coordinates of one, from this
-// lane's first on.
-template <bool WHOLE, int BITS, class P, class G, class C, class S>
+// A stage of a warp's ring in shared memory: a block, laid out so that a lane copies in, and reads back, its own
+// quads alone (no synchronisation between lanes) and the warp's accesses are contiguous.
+template <class P, class G, class S>
+struct AdamStage {
+    Quad<P> p[2][32];
+    Quad<G> g[2][32];
+    Quad<S> m[2][32], v[2][32];
+};
+
+template <class T>
+__device__ __forceinline__ void copy_quad(Quad<T> *to, const T *from)
+{
+    if constexpr (sizeof(T) == 4) cp_async16(to, from);
+    else if constexpr (sizeof(T) == 2) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_addr(to)), "l"(from) : "memory");
+    else cp_async4(to, from);
+}
+
+// The copies of a whole, aligned block, `ahead` blocks from `at`, into a stage.
+template <class P, class G, class C, class S>
+__device__ __forceinline__ void adam_fetch(const AdamPlace<P, G, C, S> &at, int ahead, AdamStage<P, G, S> &st)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int off = ahead * kBlock + 128 * h;
+        copy_quad(&st.p[h][lane], at.p + off);
+        copy_quad(&st.g[h][lane], at.g + off);
+        copy_quad(&st.m[h][lane], static_cast<const S *>(at.m) + off);
+        copy_quad(&st.v[h][lane], static_cast<const S *>(at.v) + off);
+    }
+}
+
+template <class P, class G, class S>
+__device__ __forceinline__ AdamBlock<P, G, S> adam_read(const AdamStage<P, G, S> &st)
+{
+    const int lane = threadIdx.x & 31;
+    AdamBlock<P, G, S> b;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        b.p[h] = st.p[h][lane];
+        b.g[h] = st.g[h][lane];
+        b.m[h] = st.m[h][lane];
+        b.v[h] = st.v[h][lane];
+    }
+    return b;
+}
+
+// n coordinates of a block, from this lane's first on.
+template <class P, class G, class C, class S>
 __device__ __forceinline__ void adam_load(const AdamPlace<P, G, C, S> &at, int n, AdamBlock<P, G, S> &b)
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        b.p[h] = load_quad(at.p + 128 * h, n - 128 * h, WHOLE);
-        b.g[h] = load_quad(at.g + 128 * h, n - 128 * h, WHOLE);
-        b.m[h] = load_quad(at.m + 128 * h, n - 128 * h, WHOLE);
-        b.v[h] = load_quad(at.v + 128 * h, n - 128 * h, WHOLE);
-    }
-    if (BITS == 8) {
-        b.ms = *at.ms;
-        b.vs = *at.vs;
+        b.p[h] = load_quad(at.p + 128 * h, n - 128 * h, false);
+        b.g[h] = load_quad(at.g + 128 * h, n - 128 * h, false);
+        b.m[h] = load_quad(at.m + 128 * h, n - 128 * h, false);
+        b.v[h] = load_quad(at.v + 128 * h, n - 128 * h, false);
     }
 }
 
+// WHOLE: a whole block whose addresses are all aligned to four elements.
 template <bool WHOLE, class P, class G, class C, class S>
 __device__ __forceinline__ void adam_store(const AdamPlace<P, G, C, S> &at, int n, int h, const float (&p)[4], const Quad<S> &m, const Quad<S> &v)
 {
@@ -310,7 +349,7 @@ __device__ __forceinline__ void adam_store(const AdamPlace<P, G, C, S> &at, int 
 // The 32-bit step of a block.
 template <bool WHOLE, class P, class G, class C>
 __device__ __forceinline__ void adam_block(const AdamArgs &, const AdamStep &s, const AdamPlace<P, G, C, float> &at, int n,
-                                           const AdamBlock<P, G, float> &b, uint64_t, uint32_t, uint32_t)
+                                           const AdamBlock<P, G, float> &b, float, float, uint64_t, uint32_t, uint32_t)
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -335,14 +374,15 @@ __device__ __forceinline__ void adam_block(const AdamArgs &, const AdamStep &s, 
 // The 8-bit step of a block.  quad: its first group of four coordinates of this lane, within the tensor.
 template <bool WHOLE, class P, class G, class C>
 __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s, const AdamPlace<P, G, C, uint8_t> &at, int n,
-                                           const AdamBlock<P, G, uint8_t> &b, uint64_t quad, uint32_t tensor, uint32_t t)
+                                           const AdamBlock<P, G, uint8_t> &b, float ms, float vs, uint64_t quad, uint32_t tensor,
+                                           uint32_t t)
 {
     F2 m[4], v[4];
     // beta1 m scale and beta2 (r scale)^2 are one multiplication each where the power of two leaves the product
     // normal: a scale below 2^-40 goes into the values first
-    const bool small = b.ms < 0x1p-40f || b.vs < 0x1p-40f;
-    const F2 mb = small ? s.beta1 : mul2(s.beta1, both(b.ms), s.none);
-    const F2 vb = small ? s.beta2 : mul2(s.beta2, mul2(both(b.vs), both(b.vs), s.none), s.none);
+    const bool small = ms < 0x1p-40f || vs < 0x1p-40f;
+    const F2 mb = small ? s.beta1 : mul2(s.beta1, both(ms), s.none);
+    const F2 vb = small ? s.beta2 : mul2(s.beta2, mul2(both(vs), both(vs), s.none), s.none);
     float am = 0.0f, av = 0.0f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -353,8 +393,8 @@ __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s,
         if (small)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                mx[i] = __fmul_rn(mx[i], b.ms);
-                vx[i] = __fmul_rn(vx[i], b.vs);
+                mx[i] = __fmul_rn(mx[i], ms);
+                vx[i] = __fmul_rn(vx[i], vs);
             }
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
@@ -426,17 +466,26 @@ __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s,
 // A CTA takes a contiguous piece of the launch's blocks of 256 coordinates, its warps in turn: every CTA has the same
 // number of blocks but for one, and a warp goes along a tensor with its addresses in registers.  A lane holds four
 // consecutive coordinates in each half of a block: every access of the warp is one contiguous piece, and the block's
-// scale is one warp reduction.  Whole aligned blocks have the next one's loads issued before their arithmetic.
+// scale is one warp reduction.  Whole aligned blocks come through a ring of kAdamStages stages per warp in shared
+// memory, filled by asynchronous copies: the loads in flight take no registers, which the arithmetic of the 8-bit
+// states needs, and enough of them are in flight to cover their latency.
+// Stages: up to 4, in half of an SM's shared memory.
+template <class Stage>
+constexpr int kAdamStages = std::min(4, 108 * 1024 / (static_cast<int>(sizeof(Stage)) * (kAdamThreads / 32)));
+
 template <class P, class G, class C, int BITS>
 __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
 {
     using S = AdamCell<BITS>;
-    constexpr int kWarps = kAdamThreads / 32;
+    using Stage = AdamStage<P, G, S>;
+    constexpr int kWarps = kAdamThreads / 32, kStages = kAdamStages<Stage>;
+    extern __shared__ __align__(16) unsigned char smem[];
     const float factor = a.clip ? a.clip[1] : 1.0f;
     const AdamState st = *a.state;
     const int64_t begin = a.units * blockIdx.x / gridDim.x, end = a.units * (blockIdx.x + 1) / gridDim.x;
     if (!isnan(factor) && begin < end) {
         const int warp = threadIdx.x >> 5, lane4 = (threadIdx.x & 31) * 4;
+        Stage *ring = reinterpret_cast<Stage *>(smem) + warp * kStages;
         AdamStep s{both(factor), both(a.beta1), both(a.beta2), both(a.c1), both(a.c2), both(st.e), F2{}, F2{}, both(a.minus_zero)};
         for (int i = tensor_of(a.first, a.n_tensors, begin, 0); i < a.n_tensors; ++i) {
             const int64_t first = a.first[i], lo = max(begin, first), hi = min(end, a.first[i + 1]);
@@ -457,25 +506,44 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(con
                                  reinterpret_cast<uintptr_t>(at.copy) % sizeof(Quad<C>) == 0 &&
                                  (reinterpret_cast<uintptr_t>(at.m) | reinterpret_cast<uintptr_t>(at.v)) % sizeof(Quad<S>) == 0;
             const int64_t whole = aligned ? min(hi, first + size / kBlock) : u;  // blocks below it are whole and aligned
-            AdamBlock<P, G, S> b;
+            float ms = 0.0f, vs = 0.0f;
             if (u < whole) {
-                adam_load<true, BITS>(at, kBlock, b);
-#pragma unroll 2
-                while (true) {
-                    const AdamBlock<P, G, S> now = b;
-                    const AdamPlace<P, G, C, S> here = at;
-                    u += kWarps;
+                if (BITS == 8) {
+                    ms = *at.ms;
+                    vs = *at.vs;
+                }
+#pragma unroll
+                for (int k = 0; k < kStages - 1; ++k) {
+                    if (u + k * kWarps < whole) adam_fetch(at, k * kWarps, ring[k]);
+                    cp_async_commit();
+                }
+                int in = kStages - 1, out = 0;
+                for (; u < whole; u += kWarps) {
+                    if (u + (kStages - 1) * kWarps < whole) adam_fetch(at, (kStages - 1) * kWarps, ring[in]);
+                    cp_async_commit();
+                    cp_async_wait<kStages - 1>();
+                    const AdamBlock<P, G, S> b = adam_read(ring[out]);
+                    const float ms_now = ms, vs_now = vs;
+                    if (BITS == 8 && u + kWarps < whole) {
+                        ms = at.ms[kWarps];
+                        vs = at.vs[kWarps];
+                    }
+                    adam_block<true>(a, s, at, kBlock, b, ms_now, vs_now, quad, tensor, t);
                     at.advance(kWarps);
-                    if (u < whole) adam_load<true, BITS>(at, kBlock, b);
-                    adam_block<true>(a, s, here, kBlock, now, quad, tensor, t);
                     quad += kWarps * kBlock / 4;
-                    if (u >= whole) break;
+                    in = in + 1 == kStages ? 0 : in + 1;
+                    out = out + 1 == kStages ? 0 : out + 1;
                 }
             }
             for (; u < hi; u += kWarps) {
                 const int n = static_cast<int>(min(size - (u - first) * kBlock, static_cast<int64_t>(kBlock))) - lane4;
-                adam_load<false, BITS>(at, n, b);
-                adam_block<false>(a, s, at, n, b, quad, tensor, t);
+                AdamBlock<P, G, S> b;
+                adam_load(at, n, b);
+                if (BITS == 8) {
+                    ms = *at.ms;
+                    vs = *at.vs;
+                }
+                adam_block<false>(a, s, at, n, b, ms, vs, quad, tensor, t);
                 at.advance(kWarps);
                 quad += kWarps * kBlock / 4;
             }
@@ -518,6 +586,8 @@ struct ea_adamw {
     int64_t *d_first = nullptr;
     ea_adamw_tensor *d_tensors = nullptr;
     AdamState *d_state = nullptr;
+    void (*kernel)(AdamArgs, GradList) = nullptr;
+    size_t smem = 0;
 };
 
 namespace {
@@ -574,27 +644,29 @@ AdamLayout adam_layout(const ea_adamw_config &cfg)
     return {up((n + launches) * 8), up(n * sizeof(ea_adamw_tensor)), up(sizeof(AdamState))};
 }
 
-template <class P, class G>
-void launch_adamw(const ea_adamw &h, const ea_adamw::Launch &l, const AdamArgs &a, const GradList &list)
-{
-    const bool half = h.cfg.copy_type == EA_T_F16;
-    if (h.cfg.state_bits == 32) {
-        if (half) adamw_kernel<P, G, f16, 32><<<l.grid, kAdamThreads, 0, h.stream>>>(a, list);
-        else adamw_kernel<P, G, bf16, 32><<<l.grid, kAdamThreads, 0, h.stream>>>(a, list);
-    } else {
-        if (half) adamw_kernel<P, G, f16, 8><<<l.grid, kAdamThreads, 0, h.stream>>>(a, list);
-        else adamw_kernel<P, G, bf16, 8><<<l.grid, kAdamThreads, 0, h.stream>>>(a, list);
-    }
-}
+using AdamKernel = void (*)(AdamArgs, GradList);
 
-template <class P>
-void launch_adamw(const ea_adamw &h, const ea_adamw::Launch &l, const AdamArgs &a, const GradList &list)
+// The kernel for a configuration's types, and the bytes of its ring.
+template <class P, class G, class C, int BITS>
+void adam_kernel(AdamKernel &f, size_t &smem)
 {
-    switch (h.cfg.grad_type) {
-    case EA_T_F32: launch_adamw<P, float>(h, l, a, list); break;
-    case EA_T_BF16: launch_adamw<P, bf16>(h, l, a, list); break;
-    default: launch_adamw<P, f16>(h, l, a, list);
-    }
+    f = adamw_kernel<P, G, C, BITS>;
+    using Stage = AdamStage<P, G, AdamCell<BITS>>;
+    smem = sizeof(Stage) * kAdamStages<Stage> * (kAdamThreads / 32);
+}
+template <class P, class G>
+void adam_kernel(const ea_adamw_config &c, AdamKernel &f, size_t &smem)
+{
+    const bool half = c.copy_type == EA_T_F16;
+    if (c.state_bits == 32) half ? adam_kernel<P, G, f16, 32>(f, smem) : adam_kernel<P, G, bf16, 32>(f, smem);
+    else half ? adam_kernel<P, G, f16, 8>(f, smem) : adam_kernel<P, G, bf16, 8>(f, smem);
+}
+template <class P>
+void adam_kernel(const ea_adamw_config &c, AdamKernel &f, size_t &smem)
+{
+    if (c.grad_type == EA_T_F32) adam_kernel<P, float>(c, f, smem);
+    else if (c.grad_type == EA_T_BF16) adam_kernel<P, bf16>(c, f, smem);
+    else adam_kernel<P, f16>(c, f, smem);
 }
 
 }  // namespace
@@ -621,6 +693,10 @@ int ea_adamw_init(const ea_adamw_config *cfg, void *workspace, size_t workspace_
     ea_adamw *h = new (std::nothrow) ea_adamw;
     if (!h) return lm_fail(EA_E_INVAL, "out of host memory");
     r = h->dev.query();
+    if (cfg->param_type == EA_T_F32) adam_kernel<float>(*cfg, h->kernel, h->smem);
+    else adam_kernel<bf16>(*cfg, h->kernel, h->smem);
+    if (r == EA_OK)
+        r = lm_cuda(cudaFuncSetAttribute(h->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(h->smem)), "shared memory");
     try {
         h->stream = static_cast<cudaStream_t>(stream);
         h->cfg = *cfg;
@@ -701,9 +777,7 @@ int ea_adamw_step(ea_adamw *h, const void *const *grads, float lr, const float *
         for (uint32_t k = 0; k < 10; ++k)
             a.keys[k] = make_uint2(static_cast<uint32_t>(h->cfg.seed) + k * 0x9E3779B9u, static_cast<uint32_t>(h->cfg.seed >> 32) + k * 0xBB67AE85u);
         a.clip = clip;
-        if (h->cfg.param_type == EA_T_F32) launch_adamw<float>(*h, l, a, list);
-        else launch_adamw<bf16>(*h, l, a, list);
-        if ((r = lm_cuda(cudaGetLastError(), "launch")) != EA_OK) return r;
+        if ((r = lm_cuda(launch_lm(h->kernel, dim3(l.grid), kAdamThreads, h->smem, h->stream, false, 1, a, list), "launch")) != EA_OK) return r;
     }
     return EA_OK;
 }

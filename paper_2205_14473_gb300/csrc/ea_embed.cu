@@ -44,17 +44,75 @@ __device__ __forceinline__ int64_t row_at(const EmbedArgs &a, uint32_t t)
     return i * a.row_outer + static_cast<int64_t>(t - i * a.inner) * a.row_inner;
 }
 
-// One CTA per token.
-template <class W, class Y>
-__global__ void __launch_bounds__(kEmbedThreads) lookup_kernel(const EmbedArgs a, const W *w, Y *y)
+// VEC consecutive elements, moved in words of up to 16 bytes (to which their address is aligned).
+template <class Y, int VEC>
+struct alignas(VEC * sizeof(Y) > 16 ? 16 : VEC * sizeof(Y)) Pack {
+    Y y[VEC];
+};
+template <class Y, int VEC, bool STORE>
+__device__ __forceinline__ void move_pack(Y *p, Pack<Y, VEC> &x)
 {
-    for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-        const int64_t v = token_at(a, static_cast<uint32_t>(t));
-        Y *row = y + row_at(a, static_cast<uint32_t>(t));
-        const bool inside = v >= 0 && v < a.vocab;
-        if (!inside && threadIdx.x == 0) atomicOr(a.status, kStatusToken);
-        for (int64_t j = threadIdx.x; j < a.dim; j += kEmbedThreads)
-            row[j] = from_f32<Y>(inside ? __fmul_rn(to_f32(w[v * a.table_stride + j]), a.scale) : 0.0f);
+    using Word = typename std::conditional<sizeof(x) >= 16, uint4, typename std::conditional<sizeof(x) == 8, uint2, Pack<Y, VEC>>::type>::type;
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(sizeof(x) / sizeof(Word)); ++k) {
+        if (STORE) reinterpret_cast<Word *>(p)[k] = reinterpret_cast<const Word *>(&x)[k];
+        else reinterpret_cast<Word *>(&x)[k] = reinterpret_cast<const Word *>(p)[k];
+    }
+}
+template <class Y, int VEC>
+__device__ __forceinline__ void load_pack(const Y *p, Pack<Y, VEC> &x) { move_pack<Y, VEC, false>(const_cast<Y *>(p), x); }
+template <class Y, int VEC>
+__device__ __forceinline__ void store_pack(Y *p, Pack<Y, VEC> &x) { move_pack<Y, VEC, true>(p, x); }
+
+// ------------------------------------------------------------------------------------------- lookup
+//
+// A copy of rows: a row is packs of 16 bytes of the table (single elements where an address or the width is not a
+// multiple of that), and the packs of all tokens are dealt out in order, kLookupUnroll per thread and all of its
+// loads in flight together, so that one token's row is spread over as many threads as it has packs and a long call
+// is as evenly split whatever the width.
+
+constexpr int kLookupThreads = 256;
+constexpr int kLookupUnroll = 4;
+
+struct LookupArgs {
+    EmbedArgs e;
+    uint32_t packs, magic;  // per row; quotient by it, as in batch_row (packs >= 2)
+    int shift;
+    int64_t total;          // of all tokens
+};
+
+template <class W, class Y, int VEC>
+__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a, const W *w, Y *y)
+{
+    constexpr int64_t kSpan = kLookupThreads * kLookupUnroll;  // packs of a CTA
+    for (int64_t at = blockIdx.x * kSpan; at < a.total; at += gridDim.x * kSpan) {
+        const int64_t row0 = at / a.packs;
+        const uint32_t rest = static_cast<uint32_t>(at - row0 * a.packs) + threadIdx.x;
+        Pack<W, VEC> x[kLookupUnroll];
+        Y *to[kLookupUnroll];
+        bool inside[kLookupUnroll];
+#pragma unroll
+        for (int k = 0; k < kLookupUnroll; ++k) {
+            to[k] = nullptr;
+            inside[k] = false;
+            if (at + k * kLookupThreads + threadIdx.x < a.total) {
+                const uint32_t i = rest + k * kLookupThreads, r = a.packs > 1 ? __umulhi(i, a.magic) >> a.shift : i;
+                const uint32_t t = static_cast<uint32_t>(row0) + r, j = (i - r * a.packs) * VEC;
+                const int64_t v = token_at(a.e, t);
+                to[k] = y + row_at(a.e, t) + j;
+                inside[k] = v >= 0 && v < a.e.vocab;
+                if (inside[k]) load_pack<W, VEC>(w + v * a.e.table_stride + j, x[k]);
+                else if (j == 0) atomicOr(a.e.status, kStatusToken);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kLookupUnroll; ++k) {
+            if (!to[k]) continue;
+            Pack<Y, VEC> out;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) out.y[i] = from_f32<Y>(inside[k] ? __fmul_rn(to_f32(x[k].y[i]), a.e.scale) : 0.0f);
+            store_pack<Y, VEC>(to[k], out);
+        }
     }
 }
 
@@ -399,40 +457,17 @@ struct SumArgs {
     int accumulate;
 };
 
-template <class Y, int VEC>
-struct alignas(VEC > 1 ? 16 : sizeof(Y)) Pack {
-    Y y[VEC];
-};
-template <class Y, int VEC>
-__device__ __forceinline__ void load_pack(const Y *p, Pack<Y, VEC> &out)
-{
-    if constexpr (VEC > 1) *reinterpret_cast<uint4 *>(&out) = *reinterpret_cast<const uint4 *>(p);
-    else out.y[0] = *p;
-}
-
 template <class W, int VEC>
 __device__ __forceinline__ void store_sums(W *p, const float (&sum)[VEC], float scale, int accumulate)
 {
-    if constexpr (VEC == 1) {
-        const float x = __fmul_rn(sum[0], scale);
-        *p = from_f32<W>(accumulate ? __fadd_rn(to_f32(*p), x) : x);
-    } else {
-        constexpr int kBytes = VEC * sizeof(W), kWord = kBytes >= 16 ? 16 : 8;
-        constexpr int kPer = kWord / sizeof(W);
+    Pack<W, VEC> x;
+    if (accumulate) load_pack<W, VEC>(p, x);
 #pragma unroll
-        for (int k = 0; k < VEC; k += kPer) {
-            using Word = typename std::conditional<kWord == 16, uint4, uint2>::type;
-            alignas(16) Word word;
-            W *x = reinterpret_cast<W *>(&word);
-            if (accumulate) word = *reinterpret_cast<const Word *>(p + k);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const float s = __fmul_rn(sum[k + i], scale);
-                x[i] = from_f32<W>(accumulate ? __fadd_rn(to_f32(x[i]), s) : s);
-            }
-            *reinterpret_cast<Word *>(p + k) = word;
-        }
+    for (int i = 0; i < VEC; ++i) {
+        const float s = __fmul_rn(sum[i], scale);
+        x.y[i] = from_f32<W>(accumulate ? __fadd_rn(to_f32(x.y[i]), s) : s);
     }
+    store_pack<W, VEC>(p, x);
 }
 
 constexpr int kSumThreads = 256;
@@ -636,6 +671,15 @@ EmbedLayout embed_layout(const ea_embed_config &cfg)
     return l;
 }
 
+// The quotient by d >= 2 of a number below 2^30 is its product with magic, shifted by 32 + shift (see batch_row).
+void set_divisor(uint32_t d, uint32_t &magic, int &shift)
+{
+    int s = 0;
+    while ((int64_t{1} << s) < d) ++s;
+    magic = static_cast<uint32_t>((uint64_t{1} << (31 + s)) / d + 1);
+    shift = s - 1;
+}
+
 // Checks a call and fills in the kernels' arguments.
 int embed_args(const ea_embed *h, const ea_embed_call *c, const void *tokens, const void *rows, const void *table,
                EmbedArgs &a)
@@ -666,11 +710,8 @@ int embed_args(const ea_embed *h, const ea_embed_call *c, const void *tokens, co
         a.token_inner = c->token_outer;
         a.row_inner = c->row_outer;
     } else if (c->outer > 1 && (c->token_outer != c->inner * c->token_inner || c->row_outer != c->inner * c->row_inner)) {
-        int s = 0;
-        while ((int64_t{1} << s) < c->inner) ++s;
         a.inner = static_cast<uint32_t>(c->inner);
-        a.magic = static_cast<uint32_t>((uint64_t{1} << (31 + s)) / static_cast<uint64_t>(c->inner) + 1);
-        a.shift = s - 1;
+        set_divisor(a.inner, a.magic, a.shift);
     }
     a.table_stride = c->table_stride;
     a.vocab = h->cfg.vocab;
@@ -815,10 +856,21 @@ int ea_embed_lookup(ea_embed *h, const ea_embed_call *c, const void *tokens, con
     EmbedArgs a;
     const int r = embed_args(h, c, tokens, y, w, a);
     if (r != EA_OK || a.n == 0) return r;
+    const int vec = rows_aligned(y, c->row_type, a.dim, c->outer > 1 ? c->row_outer : 0, c->inner > 1 ? c->row_inner : 0) &&
+                            rows_aligned(w, c->table_type, a.dim, a.table_stride, 0)
+                        ? 16 / static_cast<int>(type_bytes(c->table_type)) : 1;
+    LookupArgs l{};
+    l.e = a;
+    l.packs = static_cast<uint32_t>(a.dim / vec);
+    l.total = a.n * l.packs;
+    if (l.packs > 1) set_divisor(l.packs, l.magic, l.shift);
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(over(l.total, kLookupThreads * kLookupUnroll), 1 << 20));
     with_type(c->table_type, [&](auto *wt) {
+        using W = std::remove_reference_t<decltype(*wt)>;
         with_type(c->row_type, [&](auto *yt) {
-            lookup_kernel<<<static_cast<unsigned>(std::min<int64_t>(a.n, 1 << 20)), kEmbedThreads, 0, h->stream>>>(
-                a, static_cast<decltype(wt)>(const_cast<void *>(w)), static_cast<decltype(yt)>(y));
+            using Y = std::remove_reference_t<decltype(*yt)>;
+            auto kernel = vec > 1 ? lookup_kernel<W, Y, 16 / sizeof(W)> : lookup_kernel<W, Y, 1>;
+            kernel<<<grid, kLookupThreads, 0, h->stream>>>(l, static_cast<const W *>(w), static_cast<Y *>(y));
         });
     });
     return lm_cuda(cudaGetLastError(), "launch");

@@ -127,6 +127,14 @@ struct GradList {
     const void *g[kGradBatch];
 };
 
+// Groups of cp.async: the copies issued since the last commit are one; wait until all but the last N are done.
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // The tensor of unit u: the last one whose first unit is <= u (empty tensors have none).  hint: one whose first
 // unit is <= u.
 __device__ __forceinline__ int tensor_of(const int64_t *first, int n, int64_t u, int hint)
