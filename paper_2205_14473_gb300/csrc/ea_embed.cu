@@ -73,6 +73,7 @@ __device__ __forceinline__ void store_pack(Y *p, Pack<Y, VEC> &x) { move_pack<Y,
 
 constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;
+constexpr int kLookupCtasPerSm = 5;
 
 struct LookupArgs {
     EmbedArgs e;
@@ -82,37 +83,54 @@ struct LookupArgs {
 };
 
 template <class W, class Y, int VEC>
-__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const LookupArgs a, const W *w, Y *y)
+__global__ void __launch_bounds__(kLookupThreads, kLookupCtasPerSm) lookup_kernel(const LookupArgs a, const W *w, Y *y)
 {
-    constexpr int64_t kSpan = kLookupThreads * kLookupUnroll;  // packs of a CTA
-    for (int64_t at = blockIdx.x * kSpan; at < a.total; at += gridDim.x * kSpan) {
+    constexpr int kSpan = kLookupThreads * kLookupUnroll;  // packs of a turn
+    __shared__ int64_t from[2][kSpan + 1], to[2][kSpan + 1];  // a turn's rows, in elements from w (-1: none) and y
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kSpan;
+    auto quotient = [&](uint32_t i) { return a.packs > 1 ? __umulhi(i, a.magic) >> a.shift : i; };
+    auto look = [&](int64_t at, int turn) {
         const int64_t row0 = at / a.packs;
-        const uint32_t rest = static_cast<uint32_t>(at - row0 * a.packs) + threadIdx.x;
+        const uint32_t skip = static_cast<uint32_t>(at - row0 * a.packs);
+        const uint32_t rows = quotient(skip + static_cast<uint32_t>(min(a.total - at, static_cast<int64_t>(kSpan))) - 1) + 1;
+        for (uint32_t r = threadIdx.x; r < rows; r += kLookupThreads) {
+            const uint32_t t = static_cast<uint32_t>(row0) + r;
+            const int64_t v = token_at(a.e, t);
+            const bool inside = v >= 0 && v < a.e.vocab;
+            if (!inside) atomicOr(a.e.status, kStatusToken);
+            from[turn][r] = inside ? v * a.e.table_stride : -1;
+            to[turn][r] = row_at(a.e, t);
+        }
+    };
+    int turn = 0;
+    look(static_cast<int64_t>(blockIdx.x) * kSpan, 0);
+    __syncthreads();
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kSpan; at < a.total; at += stride) {
+        const uint32_t skip = static_cast<uint32_t>(at % a.packs), n = static_cast<uint32_t>(min(a.total - at, static_cast<int64_t>(kSpan)));
         Pack<W, VEC> x[kLookupUnroll];
-        Y *to[kLookupUnroll];
+        Y *dst[kLookupUnroll];
         bool inside[kLookupUnroll];
 #pragma unroll
         for (int k = 0; k < kLookupUnroll; ++k) {
-            to[k] = nullptr;
-            inside[k] = false;
-            if (at + k * kLookupThreads + threadIdx.x < a.total) {
-                const uint32_t i = rest + k * kLookupThreads, r = a.packs > 1 ? __umulhi(i, a.magic) >> a.shift : i;
-                const uint32_t t = static_cast<uint32_t>(row0) + r, j = (i - r * a.packs) * VEC;
-                const int64_t v = token_at(a.e, t);
-                to[k] = y + row_at(a.e, t) + j;
-                inside[k] = v >= 0 && v < a.e.vocab;
-                if (inside[k]) load_pack<W, VEC>(w + v * a.e.table_stride + j, x[k]);
-                else if (j == 0) atomicOr(a.e.status, kStatusToken);
-            }
+            const uint32_t i = k * kLookupThreads + threadIdx.x;
+            dst[k] = nullptr;
+            if (i >= n) continue;
+            const uint32_t r = quotient(skip + i), j = (skip + i - r * a.packs) * VEC;
+            dst[k] = y + to[turn][r] + j;
+            inside[k] = from[turn][r] >= 0;
+            if (inside[k]) load_pack<W, VEC>(w + from[turn][r] + j, x[k]);
         }
+        turn ^= 1;
+        if (at + stride < a.total) look(at + stride, turn);  // the next turn's tokens, while these rows are on their way
 #pragma unroll
         for (int k = 0; k < kLookupUnroll; ++k) {
-            if (!to[k]) continue;
+            if (!dst[k]) continue;
             Pack<Y, VEC> out;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) out.y[i] = from_f32<Y>(inside[k] ? __fmul_rn(to_f32(x[k].y[i]), a.e.scale) : 0.0f);
-            store_pack<Y, VEC>(to[k], out);
+            store_pack<Y, VEC>(dst[k], out);
         }
+        __syncthreads();
     }
 }
 
@@ -137,9 +155,10 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256;                 // of one radix pass
 constexpr int kCluster = 8;                  // CTAs that sort together
 constexpr int kMaxItems = 16;                // keys per thread of a sorting CTA
+constexpr int kZeroCtasPerSm = 3;          // that write zero rows beside it
 constexpr int kOneCtaTokens = kSortThreads * 4;
 constexpr int kClusterTokens = kSortThreads * kMaxItems * kCluster;
-constexpr int kTileItems = 8;                // keys per thread of a tile of the longer sorts
+constexpr int kTileItems = 2;                // keys per thread of a tile of the longer sorts
 constexpr int kTile1 = kSortThreads * kTileItems;
 
 struct SortArgs {
@@ -471,14 +490,22 @@ __device__ __forceinline__ void store_sums(W *p, const float (&sum)[VEC], float 
 }
 
 constexpr int kSumThreads = 256;
-constexpr int kSumRows = 128;   // entries of the list that a CTA holds in shared memory at a time
-constexpr int kSumUnroll = 8;   // rows in flight per thread
+constexpr int kSumRows = 512;   // entries of the list that a CTA holds in shared memory at a time
+constexpr int kSumGroup = 4;    // rows of one group of asynchronous copies
+constexpr int kSumGroups = 4;   // groups in flight and in use
 
+// Bytes of the ring of rows in shared memory.
+inline size_t sum_smem(int vec, int threads) { return vec > 1 ? size_t{kSumGroup} * kSumGroups * threads * 16 : 0; }
+
+// A thread owns VEC columns of its chunk's rows.  Rows come through a ring in shared memory filled by asynchronous
+// copies, each thread copying and reading its own 16 bytes (no barrier between rows), so that as many rows as the ring
+// holds are in flight while the sum goes on; single elements (VEC = 1) are loaded a group at a time.
 template <class Y, class W, int VEC>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const Y *dy, W *dw)
 {
     __shared__ uint32_t keys[kSumRows];
     __shared__ int64_t rows[kSumRows];
+    extern __shared__ uint4 ring[];
     pdl_trigger();
     pdl_wait();
     const int64_t begin = blockIdx.x * a.chunk, end = min(a.e.n, begin + a.chunk);
@@ -514,13 +541,32 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
             rows[i] = row_at(a.e, a.pos[b + i]);
         }
         __syncthreads();
-        for (int i = 0; i < n; i += kSumUnroll) {
-            Pack<Y, VEC> x[kSumUnroll];
+        auto fetch = [&](int i0) {  // rows i0 .. i0 + kSumGroup - 1 into their places in the ring
+            if constexpr (VEC > 1) {
 #pragma unroll
-            for (int u = 0; u < kSumUnroll; ++u)
-                if (in && i + u < n && keys[i + u] != none) load_pack<Y, VEC>(dy + rows[i + u] + j, x[u]);
+                for (int u = 0; u < kSumGroup; ++u)
+                    if (in && i0 + u < n && keys[i0 + u] != none)
+                        cp_async16(&ring[((i0 + u) % (kSumGroup * kSumGroups)) * blockDim.x + threadIdx.x], dy + rows[i0 + u] + j);
+                cp_async_commit();
+            }
+        };
 #pragma unroll
-            for (int u = 0; u < kSumUnroll; ++u) {
+        for (int g = 0; g < kSumGroups - 1; ++g) fetch(g * kSumGroup);
+        for (int i = 0; i < n; i += kSumGroup) {
+            Pack<Y, VEC> x[kSumGroup];
+            if constexpr (VEC > 1) {
+                fetch(i + (kSumGroups - 1) * kSumGroup);
+                cp_async_wait<kSumGroups - 1>();
+#pragma unroll
+                for (int u = 0; u < kSumGroup; ++u)
+                    *reinterpret_cast<uint4 *>(&x[u]) = ring[((i + u) % (kSumGroup * kSumGroups)) * blockDim.x + threadIdx.x];
+            } else {
+#pragma unroll
+                for (int u = 0; u < kSumGroup; ++u)
+                    if (in && i + u < n && keys[i + u] != none) x[u].y[0] = dy[rows[i + u] + j];
+            }
+#pragma unroll
+            for (int u = 0; u < kSumGroup; ++u) {
                 if (i + u >= n) break;
                 const uint32_t k = keys[i + u];
                 if (k != cur) {
@@ -529,7 +575,10 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
                     from_head = false;
 #pragma unroll
                     for (int v = 0; v < VEC; ++v) sum[v] = 0.0f;
-                    if (k == none) return;
+                    if (k == none) {
+                        cp_async_wait_all();
+                        return;
+                    }
                 }
 #pragma unroll
                 for (int v = 0; v < VEC; ++v) sum[v] = __fadd_rn(sum[v], to_f32(x[u].y[v]));
@@ -623,6 +672,7 @@ int validate(const ea_embed_config *cfg)
 
 constexpr int kMaxVec = 8;
 constexpr int kMinChunk = 8;
+constexpr int kChunksPerSm = 8;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 int64_t over(int64_t x, int64_t a) { return (x + a - 1) / a; }
@@ -643,7 +693,7 @@ struct SumShape {
 // kMinChunk rows (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
 int64_t chunk_length(int64_t n, int64_t slabs, int sms)
 {
-    const int64_t most = std::max<int64_t>(1, sms * 16 / slabs);
+    const int64_t most = std::max<int64_t>(1, sms * kChunksPerSm / slabs);
     return std::max<int64_t>(kMinChunk, over(n, most));
 }
 
@@ -666,7 +716,7 @@ EmbedLayout embed_layout(const ea_embed_config &cfg)
     }
     // the most chunks that chunk_length allows at any number of tokens
     const int64_t slabs = SumShape(cfg.dim, kMaxVec).slabs;
-    const int64_t chunks = std::min(over(n, kMinChunk), std::max<int64_t>(1, kMaxSms * 16 / slabs));
+    const int64_t chunks = std::min(over(n, kMinChunk), std::max<int64_t>(1, kMaxSms * kChunksPerSm / slabs));
     l.partial = 2 * chunks * up(cfg.dim, kMaxVec) * 4;
     return l;
 }
@@ -759,7 +809,17 @@ int allow_sort_smem()
     auto allow = [](auto *kernel, size_t bytes) {
         return lm_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)), "shared memory");
     };
-    int r = allow(order_kernel<4>, kSortSmem<4>);
+    int r = EA_OK;
+    for (int32_t yt : {EA_T_F32, EA_T_BF16, EA_T_F16})
+        for (int32_t wt : {EA_T_F32, EA_T_BF16, EA_T_F16})
+            with_type(yt, [&](auto *y) {
+                with_type(wt, [&](auto *w) {
+                    using Y = std::remove_reference_t<decltype(*y)>;
+                    using W = std::remove_reference_t<decltype(*w)>;
+                    if (r == EA_OK) r = allow(sum_kernel<Y, W, 16 / sizeof(Y)>, sum_smem(2, kSumThreads));
+                });
+            });
+    if (r == EA_OK) r = allow(order_kernel<4>, kSortSmem<4>);
     if (r == EA_OK) r = allow(order_kernel<8>, kSortSmem<8>);
     if (r == EA_OK) r = allow(order_kernel<kMaxItems>, kSortSmem<kMaxItems>);
     return r;
@@ -774,7 +834,7 @@ cudaError_t order_tokens(ea_embed &h, const EmbedArgs &a, const ZeroTable &z, bo
     cudaError_t e = cudaSuccess;
     if (a.n <= kClusterTokens) {
         const int ctas = a.n <= kOneCtaTokens ? 1 : kCluster;
-        const int64_t rows = over(a.vocab, h.dev.sms), zero_ctas = zero ? up(over(a.vocab, rows), ctas) : 0;
+        const int64_t rows = over(a.vocab, h.dev.sms * kZeroCtasPerSm), zero_ctas = zero ? up(over(a.vocab, rows), ctas) : 0;
         with_items(a.n, ctas, [&](auto items) {
             constexpr int kItems = decltype(items)::value;
             const SortArgs s{a, h.key[0], h.pos[0], passes, bits};
@@ -864,7 +924,7 @@ int ea_embed_lookup(ea_embed *h, const ea_embed_call *c, const void *tokens, con
     l.packs = static_cast<uint32_t>(a.dim / vec);
     l.total = a.n * l.packs;
     if (l.packs > 1) set_divisor(l.packs, l.magic, l.shift);
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(over(l.total, kLookupThreads * kLookupUnroll), 1 << 20));
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(over(l.total, kLookupThreads * kLookupUnroll), h->dev.sms * kLookupCtasPerSm));
     with_type(c->table_type, [&](auto *wt) {
         using W = std::remove_reference_t<decltype(*wt)>;
         with_type(c->row_type, [&](auto *yt) {
@@ -899,7 +959,7 @@ int ea_embed_grad(ea_embed *h, const ea_embed_call *c, const void *tokens, const
             using W = std::remove_reference_t<decltype(*wt)>;
             const dim3 grid(chunks, static_cast<unsigned>(shape.slabs));
             auto kernel = vec > 1 ? sum_kernel<Y, W, 16 / sizeof(Y)> : sum_kernel<Y, W, 1>;
-            e = launch_lm(kernel, grid, shape.threads, 0, h->stream, true, 1, s, static_cast<const Y *>(dy), static_cast<W *>(dw));
+            e = launch_lm(kernel, grid, shape.threads, sum_smem(vec, shape.threads), h->stream, true, 1, s, static_cast<const Y *>(dy), static_cast<W *>(dw));
             if (e == cudaSuccess && chunks > 1)
                 e = launch_lm(combine_kernel<W>, dim3(chunks - 1, kCombineSplit), kCombineThreads, 0, h->stream, true, 1, s,
                               static_cast<W *>(dw));

@@ -100,75 +100,101 @@ class Embedding(_Handle):
         padding = -1 if padding_idx is None else int(padding_idx)
         if padding_idx is not None and padding < 0:
             _refuse("padding_idx must be a token or None")
-        self._c = ea_embed_call()
+        self._c, self._shape = ea_embed_call(), torch.Size((self.vocab, self.dim))
         self._open(ea_embed_config(self.vocab, self.dim, self.max_tokens, padding, scale), stream, device)
 
-    def _layout(self, tokens, rows, table, rows_name, table_name):
-        """Fills in self._c; returns the tensors to pass (a copy of a layout that two strides do not describe)."""
+    # What a call has to check goes into the one ea_embed_call of the handle.
+
+    def _tokens(self, tokens):
+        """Describes the tokens; returns those to pass: of a layout that two strides do not describe, a copy."""
         c = self._c
-        if tokens.dtype not in _TOKEN:
+        if not isinstance(tokens, torch.Tensor) or tokens.device != self.device:
+            self._on_device(tokens, "tokens")
+        kind = _TOKEN.get(tokens.dtype)
+        if kind is None:
             _refuse(f"tokens are int32 or int64, not {tokens.dtype}")
-        if rows.dtype not in _TYPE or table.dtype not in _TYPE:
-            _refuse(f"{rows_name} and {table_name} are float32, bfloat16 or float16, not {rows.dtype} and {table.dtype}")
-        if tuple(table.shape) != (self.vocab, self.dim):
-            _refuse(f"{table_name} is {tuple(table.shape)}, not {(self.vocab, self.dim)}")
-        if rows.shape[:-1] != tokens.shape or rows.dim() == 0 or rows.shape[-1] != self.dim:
-            _refuse(f"{rows_name} is {tuple(rows.shape)}, not {(*tokens.shape, self.dim)}")
-        ts, (w0, w1) = table.stride(), (self.vocab, self.dim)
-        if w1 > 1 and ts[1] != 1:
-            _refuse(f"the rows of {table_name} are not contiguous")
-        c.table_stride = ts[0] if w0 > 1 else max(ts[0], w1)
+        c.token_type = kind
         shape = tokens.shape
         if len(shape) == 2:
             c.outer, c.inner = shape
             c.token_outer, c.token_inner = tokens.stride()
+        elif len(shape) == 1:
+            c.outer, c.inner, c.token_outer, c.token_inner = 1, shape[0], 0, tokens.stride(0)
+        else:
+            tokens = tokens.contiguous()
+            c.outer, c.inner, c.token_outer, c.token_inner = 1, tokens.numel(), 0, 1
+        return tokens
+
+    def _rows(self, rows, tokens, name) -> None:
+        """Describes the rows that belong to tokens' shape."""
+        c = self._c
+        if not isinstance(rows, torch.Tensor) or rows.device != self.device:
+            self._on_device(rows, name)
+        if rows.shape != (*tokens.shape, self.dim):
+            _refuse(f"{name} is {tuple(rows.shape)}, not {(*tokens.shape, self.dim)}")
+        n = tokens.dim()
+        if self.dim > 1 and rows.stride(-1) != 1 or n not in (1, 2) and not rows.is_contiguous():
+            _refuse(f"the rows of {name} are not contiguous")
+        if n == 2:
             c.row_outer, c.row_inner = rows.stride()[:2]
         else:
-            c.outer, c.inner, c.token_outer, c.row_outer = 1, tokens.numel(), 0, 0
-            if len(shape) == 1:
-                c.token_inner, c.row_inner = tokens.stride(0), rows.stride(0)
-            else:
-                c.token_inner, c.row_inner = 1, self.dim
-        c.token_type, c.row_type, c.table_type = _TOKEN[tokens.dtype], _TYPE[rows.dtype], _TYPE[table.dtype]
+            c.row_outer, c.row_inner = 0, rows.stride(0) if n == 1 else self.dim
+        self._row_type(rows.dtype, name)
+
+    def _row_type(self, dtype, name) -> None:
+        kind = _TYPE.get(dtype)
+        if kind is None:
+            _refuse(f"{name} is float32, bfloat16 or float16, not {dtype}")
+        self._c.row_type = kind
+
+    def _table(self, table, name) -> None:
+        c = self._c
+        if not isinstance(table, torch.Tensor) or table.device != self.device:
+            self._on_device(table, name)
+        if table.shape != self._shape:
+            _refuse(f"{name} is {tuple(table.shape)}, not {(self.vocab, self.dim)}")
+        kind = _TYPE.get(table.dtype)
+        if kind is None:
+            _refuse(f"{name} is float32, bfloat16 or float16, not {table.dtype}")
+        outer, inner = table.stride()
+        if inner != 1 and self.dim > 1:
+            _refuse(f"the rows of {name} are not contiguous")
+        c.table_type, c.table_stride = kind, outer if self.vocab > 1 else max(outer, self.dim)
 
     def lookup(self, tokens, weight, out=None, dtype=None):
         """scale * weight[tokens], of shape tokens.shape + (dim,), in `dtype` (default: weight's) or into `out`."""
-        self._on_device(tokens, "tokens")
-        self._on_device(weight, "weight")
+        ids = self._tokens(tokens)
+        self._table(weight, "weight")
         if out is None:
-            out = torch.empty(*tokens.shape, self.dim, dtype=dtype or weight.dtype, device=self.device)
+            out = torch.empty((*tokens.shape, self.dim), dtype=dtype or weight.dtype, device=self.device)
+            self._c.row_outer, self._c.row_inner = self._c.inner * self.dim, self.dim
+            self._row_type(out.dtype, "out")
         else:
-            self._on_device(out, "out")
+            self._rows(out, tokens, "out")
             if dtype is not None and out.dtype != dtype:
                 _refuse(f"out is {out.dtype}, not {dtype}")
-        ids = tokens if tokens.dim() in (1, 2) else tokens.contiguous()
-        rows = out
-        if out.dim() and out.shape[-1] > 1 and out.stride(-1) != 1 or tokens.dim() not in (1, 2) and not out.is_contiguous():
-            _refuse("the rows of out are not contiguous")
-        self._layout(ids, rows, weight, "out", "weight")
         now = self._enter()
-        status = self._L.ea_embed_lookup(self.h, self._c, ids.data_ptr(), weight.data_ptr(), rows.data_ptr())
-        self._leave(status, now, ids, weight, rows)
+        status = self._L.ea_embed_lookup(self.h, self._c, ids.data_ptr(), weight.data_ptr(), out.data_ptr())
+        if status or now is not None:
+            self._leave(status, now, ids, weight, out)
         return out
 
     def grad(self, tokens, dy, out=None, accumulate: bool = False, dtype=torch.float32):
         """The gradient of weight, of shape (vocab, dim), from dy = the gradient of lookup's result, into `out`
         or, with accumulate, added to it."""
-        self._on_device(tokens, "tokens")
-        self._on_device(dy, "dy")
+        ids = self._tokens(tokens)
         if out is None:
             if accumulate:
                 _refuse("accumulate needs out")
-            out = torch.empty(self.vocab, self.dim, dtype=dtype, device=self.device)
-        else:
-            self._on_device(out, "out")
-        ids = tokens if tokens.dim() in (1, 2) else tokens.contiguous()
-        if dy.dim() and dy.shape[-1] > 1 and dy.stride(-1) != 1 or tokens.dim() not in (1, 2):
+            out = torch.empty(self._shape, dtype=dtype, device=self.device)
+        self._table(out, "out")
+        if isinstance(dy, torch.Tensor) and dy.dim() and (dy.stride(-1) != 1 or tokens.dim() not in (1, 2)):
             dy = dy.contiguous()
-        self._layout(ids, dy, out, "dy", "out")
+        self._rows(dy, tokens, "dy")
         now = self._enter()
         status = self._L.ea_embed_grad(self.h, self._c, ids.data_ptr(), dy.data_ptr(), out.data_ptr(), int(accumulate))
-        self._leave(status, now, ids, dy, out)
+        if status or now is not None:
+            self._leave(status, now, ids, dy, out)
         return out
 
     def sync(self) -> None:
@@ -227,7 +253,8 @@ class GradNorm(_Handle):
                 _refuse("out is two contiguous float32 values")
         now = self._enter()
         status = self._L.ea_grad_norm(self.h, g._ptrs, grad_scale, max_norm, out.data_ptr())
-        self._leave(status, now, out, *(g.tensors if now is not None else ()))
+        if status or now is not None:
+            self._leave(status, now, out, *g.tensors)
         return out
 
 
@@ -312,8 +339,8 @@ class AdamW(_Handle):
                 _refuse("clip is two contiguous float32 values")
         now = self._enter()
         status = self._L.ea_adamw_step(self.h, g._ptrs, lr, None if clip is None else clip.data_ptr())
-        self._leave(status, now, *(() if now is None else self._touched + tuple(g.tensors)),
-                    *(() if clip is None else (clip,)))
+        if status or now is not None:
+            self._leave(status, now, *self._touched, *g.tensors, *(() if clip is None else (clip,)))
 
     @property
     def t(self) -> int:
