@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupCtasPerSm) lookup_wide_
 //   up to kClusterTokens   order_kernel: one cluster of CTAs sorts in shared memory, exchanging digit counts and
 //                          keys through distributed shared memory, while the other CTAs write the zero rows of
 //                          the tokens that do not occur (those need no order, only the set of tokens);
-//   more                   hist, scan and scatter launches per digit, then zero_kernel;
+//   more                   hist, scan and scatter launches per digit; the first marks the tokens in a bitmap, and
+//                          the others, none of which fills the GPU, write a share of the zero rows each;
 //   then                   sum_kernel, combine_kernel.
 
 constexpr int kSortThreads = 512;
@@ -409,7 +410,20 @@ struct TileSortArgs {
     uint32_t *hist, *total;
     uint32_t tiles;
     int shift, bits;
+    uint32_t *seen;           // a bit for every token of the table that occurs (the first pass sets them; may be null)
+    ZeroTable z;              // and this launch's share of the zero rows, for the CTAs after the sort's
+    int64_t zero0, zero1, rows_per_cta;
 };
+
+constexpr int kSeenWords = 4096;
+
+// A CTA's part of the zero rows of a launch; `index` counts those CTAs.
+__device__ __forceinline__ void zero_share(const TileSortArgs &a, unsigned index)
+{
+    const int64_t row0 = a.zero0 + index * a.rows_per_cta, row1 = min(a.zero1, row0 + a.rows_per_cta);
+    for (int64_t v = row0 + (threadIdx.x >> 5); v < row1; v += blockDim.x >> 5)
+        if (!(a.seen[v >> 5] >> (v & 31) & 1u)) zero_row(a.z.dw + v * a.e.table_stride * a.z.elem, a.e.dim * a.z.elem);
+}
 
 template <int ITEMS>
 __device__ __forceinline__ void load_tile(const TileSortArgs &a, uint2 (&item)[ITEMS], uint32_t (&digit)[ITEMS], bool report)
@@ -427,14 +441,25 @@ __device__ __forceinline__ void load_tile(const TileSortArgs &a, uint2 (&item)[I
 
 __global__ void __launch_bounds__(kSortThreads) hist_kernel(const TileSortArgs a)
 {
-    __shared__ uint32_t count[kDigits];
+    __shared__ uint32_t count[kDigits], here[kSeenWords];
     pdl_trigger();
+    const bool mark = a.seen && !a.key_in, gather = mark && a.e.vocab <= 32 * kSeenWords;
+    const int words = static_cast<int>((min(a.e.vocab, int64_t{32} * kSeenWords) + 31) / 32);
     if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+    if (gather)
+        for (int i = threadIdx.x; i < words; i += kSortThreads) here[i] = 0;
     pdl_wait();
+    if (blockIdx.x >= a.tiles) return zero_share(a, blockIdx.x - a.tiles);
     __syncthreads();
     uint2 item[kTileItems];
     uint32_t digit[kTileItems];
     load_tile(a, item, digit, true);
+    // Tokens that occur: each CTA's are gathered in shared memory first, so that a frequent token is one request a CTA
+    // and a warp looks at 32 words of the table's bits at a time (a table of up to 32 kSeenWords tokens).
+    if (mark)
+#pragma unroll
+        for (int i = 0; i < kTileItems; ++i)
+            if (item[i].x < a.e.vocab) atomicOr(&(gather ? here : a.seen)[item[i].x >> 5], 1u << (item[i].x & 31));
 #pragma unroll
     for (int i = 0; i < kTileItems; ++i) {
         const uint32_t peers = __match_any_sync(0xffffffffu, digit[i]);
@@ -442,15 +467,20 @@ __global__ void __launch_bounds__(kSortThreads) hist_kernel(const TileSortArgs a
     }
     __syncthreads();
     if (threadIdx.x < (1u << a.bits)) a.hist[static_cast<size_t>(threadIdx.x) * a.tiles + blockIdx.x] = count[threadIdx.x];
+    if (gather)
+        for (int i = threadIdx.x; i < words; i += kSortThreads)
+            if (here[i] & ~*static_cast<volatile uint32_t *>(a.seen + i)) atomicOr(a.seen + i, here[i]);
 }
 
 // One CTA per digit: its counts become exclusive sums over the tiles, total[d] their sum.
-__global__ void __launch_bounds__(kSortThreads) scan_kernel(uint32_t *hist, uint32_t *total, uint32_t tiles)
+__global__ void __launch_bounds__(kSortThreads) scan_kernel(const TileSortArgs a)
 {
     __shared__ uint32_t warp_sums[kSortWarps];
     pdl_trigger();
     pdl_wait();
-    uint32_t *row = hist + static_cast<size_t>(blockIdx.x) * tiles, carry = 0;
+    if (blockIdx.x >= 1u << a.bits) return zero_share(a, blockIdx.x - (1u << a.bits));
+    const uint32_t tiles = a.tiles;
+    uint32_t *row = a.hist + static_cast<size_t>(blockIdx.x) * tiles, carry = 0;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     for (uint32_t i0 = 0; i0 < tiles; i0 += kSortThreads) {
         const uint32_t i = i0 + threadIdx.x, v = i < tiles ? row[i] : 0;
@@ -472,7 +502,7 @@ __global__ void __launch_bounds__(kSortThreads) scan_kernel(uint32_t *hist, uint
         carry += all;
         __syncthreads();
     }
-    if (threadIdx.x == 0) total[blockIdx.x] = carry;
+    if (threadIdx.x == 0) a.total[blockIdx.x] = carry;
 }
 
 __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const TileSortArgs a)
@@ -480,6 +510,7 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const TileSortArg
     __shared__ uint32_t hist[kSortWarps][kDigits], total[kDigits], base[kDigits], warp_sums[kDigits / 32];
     pdl_trigger();
     pdl_wait();
+    if (blockIdx.x >= a.tiles) return zero_share(a, blockIdx.x - a.tiles);
     uint2 item[kTileItems];
     uint32_t digit[kTileItems], rank[kTileItems];
     load_tile(a, item, digit, false);
@@ -497,32 +528,6 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(const TileSortArg
             a.pos[at] = item[i].y;
         }
     }
-}
-
-__device__ __forceinline__ int64_t lower_bound(const uint32_t *key, int64_t n, int64_t v)
-{
-    int64_t lo = 0, hi = n;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-constexpr int kZeroWords = 8192;
-
-// The zero rows, from a sorted list of the tokens.
-__global__ void __launch_bounds__(kSortThreads) zero_kernel(const EmbedArgs a, const uint32_t *key, const ZeroTable z, int64_t rows_per_cta)
-{
-    __shared__ uint32_t bits[kZeroWords];
-    pdl_trigger();
-    pdl_wait();
-    const int64_t row0 = blockIdx.x * rows_per_cta;
-    zero_rows(a, z, row0, min(a.vocab, row0 + rows_per_cta), bits, kZeroWords, [&](int64_t lo, int64_t hi, auto set) {
-        const int64_t end = lower_bound(key, a.n, hi);
-        for (int64_t i = lower_bound(key, a.n, lo) + threadIdx.x; i < end; i += kSortThreads) set(key[i]);
-    });
 }
 
 struct SumArgs {
@@ -566,29 +571,29 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
     extern __shared__ uint4 ring[];
     pdl_trigger();
     pdl_wait();
-    const int64_t begin = blockIdx.x * a.chunk, end = min(a.e.n, begin + a.chunk);
+    const int64_t chunk = blockIdx.x, begin = chunk * a.chunk, end = min(a.e.n, begin + a.chunk);
     const int64_t j = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * VEC;
     const uint32_t none = static_cast<uint32_t>(a.e.vocab);
     const bool in = j < a.e.dim;
-    const uint32_t first = a.key[begin];
+    const uint32_t first = a.key[begin], before = begin > 0 ? a.key[begin - 1] : none;
+    const uint32_t tail = a.key[end - 1], after = end < a.e.n ? a.key[end] : none;
     if (first == none) return;  // nothing but tokens without a gradient from here on
-    const bool head = begin > 0 && a.key[begin - 1] == first;
-    const uint32_t after = end < a.e.n ? a.key[end] : none;  // the token that the chunk's last run may go on with
-    float *part = a.partial + 2 * blockIdx.x * a.pad + j;
+    const bool head_in = before == first, goes_on = tail != none && tail == after;  // runs that cross the chunk's borders
+    float *part = a.partial + 2 * chunk * a.pad + j;
     float sum[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) sum[k] = 0.0f;
     uint32_t cur = first;
-    bool from_head = head;
-    auto flush = [&](bool goes_on) {
-        if (in) {
-            if (from_head || goes_on) {
-                float *p = part + (from_head ? 0 : a.pad);
+    bool from_head = head_in;
+    // The end of the run of `cur`, or of the chunk within one.
+    auto flush = [&](bool crosses) {
+        if (!in) return;
+        if (from_head || crosses) {
+            float *p = part + (from_head ? 0 : a.pad);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) p[k] = sum[k];
-            } else {
-                store_sums<W, VEC>(dw + cur * a.e.table_stride + j, sum, a.e.scale, a.accumulate);
-            }
+            for (int k = 0; k < VEC; ++k) p[k] = sum[k];
+        } else {
+            store_sums<W, VEC>(dw + cur * a.e.table_stride + j, sum, a.e.scale, a.accumulate);
         }
     };
     for (int64_t b = begin; b < end; b += kSumRows) {
@@ -599,12 +604,12 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
             rows[i] = row_at(a.e, a.pos[b + i]);
         }
         __syncthreads();
+        auto wanted = [&](int i) { return in && i < n && keys[i] != none; };
         auto fetch = [&](int i0) {  // rows i0 .. i0 + kSumGroup - 1 into their places in the ring
             if constexpr (VEC > 1) {
 #pragma unroll
                 for (int u = 0; u < kSumGroup; ++u)
-                    if (in && i0 + u < n && keys[i0 + u] != none)
-                        cp_async16(&ring[((i0 + u) % (kSumGroup * kSumGroups)) * blockDim.x + threadIdx.x], dy + rows[i0 + u] + j);
+                    if (wanted(i0 + u)) cp_async16(&ring[((i0 + u) % (kSumGroup * kSumGroups)) * blockDim.x + threadIdx.x], dy + rows[i0 + u] + j);
                 cp_async_commit();
             }
         };
@@ -621,7 +626,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
             } else {
 #pragma unroll
                 for (int u = 0; u < kSumGroup; ++u)
-                    if (in && i + u < n && keys[i + u] != none) x[u].y[0] = dy[rows[i + u] + j];
+                    if (wanted(i + u)) x[u].y[0] = dy[rows[i + u] + j];
             }
 #pragma unroll
             for (int u = 0; u < kSumGroup; ++u) {
@@ -643,24 +648,24 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumArgs a, const
             }
         }
     }
-    flush(after == cur);
+    flush(goes_on);
 }
 
 constexpr int kCombineThreads = 256, kCombineSplit = 4;
 
 // The rows of the tokens whose runs cross chunks.  CTA (c, y) takes the run that starts in chunk c and goes on in
 // the next, if there is one -- the tail of c and the heads of the chunks after it, as far as the run goes -- and
-// every kCombineSplit-th piece of its columns.  A long run is split over up to eight groups of
-// threads, which take its chunks in turn and are added in order.
+// every kCombineSplit-th piece of its columns.  The more chunks a run has, the more groups of threads take them in
+// turn; the groups' sums are added in order.
 template <class W>
 __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const SumArgs a, W *dw)
 {
     __shared__ float4 red[kCombineThreads];
     pdl_wait();
     const int64_t c = blockIdx.x, begin = c * a.chunk, next = begin + a.chunk;  // c is not the last chunk
-    const uint32_t v = a.key[next];
-    const bool starts = a.key[begin] != v || begin == 0 || a.key[begin - 1] != v;
-    if (v == static_cast<uint32_t>(a.e.vocab) || a.key[next - 1] != v || !starts) return;
+    const uint32_t none = static_cast<uint32_t>(a.e.vocab), v = a.key[next], tail = a.key[next - 1], first = a.key[begin],
+                   before = begin > 0 ? a.key[begin - 1] : none;
+    if (v == none || tail != v || (first == v && before == v)) return;
     int64_t last = c + 1;  // the chunks whose first entry is v: c + 1 .. last
     for (int64_t k = c + 2;; k += 32) {
         const int64_t at = (k + (threadIdx.x & 31)) * a.chunk;
@@ -670,14 +675,14 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const SumArgs 
         if (run < 32) break;
     }
     const int64_t parts = last - c;
-    const int groups = parts >= 16 ? 8 : parts >= 8 ? 4 : parts >= 4 ? 2 : 1, width = kCombineThreads / groups;
+    const int groups = parts > 32 ? 8 : parts > 16 ? 4 : parts > 8 ? 2 : 1, width = kCombineThreads / groups;
     const int group = threadIdx.x / width, lane = threadIdx.x % width;
     for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * width * 4; j0 < a.e.dim; j0 += static_cast<int64_t>(kCombineSplit) * width * 4) {
         const int64_t j = j0 + lane * 4;
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (j < a.e.dim) {
             if (group == 0) sum = *reinterpret_cast<const float4 *>(a.partial + (2 * c + 1) * a.pad + j);
-#pragma unroll 4
+#pragma unroll 8
             for (int64_t k = c + 1 + group; k <= last; k += groups) {
                 const float4 x = *reinterpret_cast<const float4 *>(a.partial + 2 * k * a.pad + j);
                 sum = make_float4(__fadd_rn(sum.x, x.x), __fadd_rn(sum.y, x.y), __fadd_rn(sum.z, x.z), __fadd_rn(sum.w, x.w));
@@ -710,8 +715,8 @@ struct ea_embed {
     cudaStream_t stream = nullptr;
     ea_embed_config cfg{};
     uint32_t *status = nullptr;
-    uint32_t *key[2] = {}, *pos[2] = {};  // the sorted list; the second pair, hist and total: longer sorts only
-    uint32_t *hist = nullptr, *total = nullptr;
+    uint32_t *key[2] = {}, *pos[2] = {};  // the sorted list; the second pair, hist, total and seen: longer sorts only
+    uint32_t *hist = nullptr, *total = nullptr, *seen = nullptr;
     float *partial = nullptr;
 };
 
@@ -730,7 +735,6 @@ int validate(const ea_embed_config *cfg)
 
 constexpr int kMaxVec = 8;
 constexpr int kMinChunk = 8;
-constexpr int kChunksPerSm = 8;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 int64_t over(int64_t x, int64_t a) { return (x + a - 1) / a; }
@@ -747,18 +751,22 @@ struct SumShape {
     }
 };
 
-// Entries of the sorted list per chunk: about 16 CTAs' worth of chunks per SM, slabs counted, and no fewer than
-// kMinChunk rows (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
-int64_t chunk_length(int64_t n, int64_t slabs, int sms)
+// Chunks that the sorted list is cut into at most: as many as run at a time, 1,024 threads per SM, slabs counted.
+int64_t most_chunks(const SumShape &shape, int sms)
 {
-    const int64_t most = std::max<int64_t>(1, sms * kChunksPerSm / slabs);
-    return std::max<int64_t>(kMinChunk, over(n, most));
+    return std::max<int64_t>(1, sms * (1024 / shape.threads) / shape.slabs);
+}
+
+// Entries per chunk, no fewer than kMinChunk (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
+int64_t chunk_length(int64_t n, const SumShape &shape, int sms)
+{
+    return std::max<int64_t>(kMinChunk, over(n, most_chunks(shape, sms)));
 }
 
 struct EmbedLayout {
-    size_t status, list, hist, total_, partial;
+    size_t status, list, hist, total_, seen, partial;
     int lists;
-    size_t total() const { return status + 2 * lists * list + hist + total_ + partial; }
+    size_t total() const { return status + 2 * lists * list + hist + total_ + seen + partial; }
 };
 
 EmbedLayout embed_layout(const ea_embed_config &cfg)
@@ -771,10 +779,10 @@ EmbedLayout embed_layout(const ea_embed_config &cfg)
     if (n > kClusterTokens) {
         l.hist = up(over(n, kTile1) * kDigits * 4, 256);
         l.total_ = kDigits * 4;
+        l.seen = up(over(cfg.vocab, 32) * 4, 256);
     }
-    // the most chunks that chunk_length allows at any number of tokens
-    const int64_t slabs = SumShape(cfg.dim, kMaxVec).slabs;
-    const int64_t chunks = std::min(over(n, kMinChunk), std::max<int64_t>(1, kMaxSms * kChunksPerSm / slabs));
+    int64_t chunks = 0;  // the most that chunk_length allows, in either type
+    for (int vec : {kMaxVec, 4, 1}) chunks = std::max(chunks, std::min(over(n, kMinChunk), most_chunks(SumShape(cfg.dim, vec), kMaxSms)));
     l.partial = 2 * chunks * up(cfg.dim, kMaxVec) * 4;
     return l;
 }
@@ -884,7 +892,7 @@ int allow_sort_smem()
 }
 
 // The sorted list of the tokens into h.key[0], h.pos[0]; with `zero`, the rows of dw whose token does not occur.
-cudaError_t order_tokens(ea_embed &h, const EmbedArgs &a, const ZeroTable &z, bool zero)
+int order_tokens(ea_embed &h, const EmbedArgs &a, const ZeroTable &z, bool zero)
 {
     int key_bits = 1;
     while ((a.vocab >> key_bits) != 0) ++key_bits;  // keys are 0 .. vocab
@@ -899,23 +907,44 @@ cudaError_t order_tokens(ea_embed &h, const EmbedArgs &a, const ZeroTable &z, bo
             e = launch_lm(order_kernel<kItems>, dim3(static_cast<unsigned>(ctas + zero_ctas)), kSortThreads, kSortSmem<kItems>, h.stream,
                           false, ctas, s, z, rows);
         });
-        return e;
+        return lm_cuda(e, "launch");
     }
-    const unsigned tiles = static_cast<unsigned>(over(a.n, kTile1));
-    for (int pass = 0; pass < passes && e == cudaSuccess; ++pass) {
+    TileSortArgs s{};
+    s.e = a;
+    s.hist = h.hist;
+    s.total = h.total;
+    s.tiles = static_cast<uint32_t>(over(a.n, kTile1));
+    s.bits = bits;
+    s.seen = zero ? h.seen : nullptr;
+    s.z = z;
+    if (zero) e = cudaMemsetAsync(h.seen, 0, over(a.vocab, 32) * 4, h.stream);
+    const int launches = 3 * passes - 1;  // that write zero rows: all but the first
+    int done = -1;
+    auto launch = [&](auto *kernel, unsigned grid) {
+        s.zero0 = s.zero1 = 0;
+        s.rows_per_cta = 1;
+        unsigned zero_ctas = 0;
+        if (zero && done >= 0) {
+            s.zero0 = a.vocab * done / launches;
+            s.zero1 = a.vocab * (done + 1) / launches;
+            s.rows_per_cta = std::max<int64_t>(1, over(s.zero1 - s.zero0, h.dev.sms * 2));
+            zero_ctas = static_cast<unsigned>(over(s.zero1 - s.zero0, s.rows_per_cta));
+        }
+        if (e == cudaSuccess) e = launch_lm(kernel, dim3(grid + zero_ctas), kSortThreads, 0, h.stream, done >= 0, 1, s);
+        ++done;
+    };
+    for (int pass = 0; pass < passes; ++pass) {
         const int to = (passes - 1 - pass) & 1;  // the last pass writes the first pair
-        TileSortArgs s{a, pass ? h.key[to ^ 1] : nullptr, pass ? h.pos[to ^ 1] : nullptr, h.key[to], h.pos[to], h.hist, h.total, tiles,
-                       pass * bits, bits};
-        e = launch_lm(hist_kernel, dim3(tiles), kSortThreads, 0, h.stream, pass > 0, 1, s);
-        if (e == cudaSuccess) e = launch_lm(scan_kernel, dim3(1u << bits), kSortThreads, 0, h.stream, true, 1, h.hist, h.total, tiles);
-        if (e == cudaSuccess) e = launch_lm(scatter_kernel, dim3(tiles), kSortThreads, 0, h.stream, true, 1, s);
+        s.key_in = pass ? h.key[to ^ 1] : nullptr;
+        s.pos_in = pass ? h.pos[to ^ 1] : nullptr;
+        s.key = h.key[to];
+        s.pos = h.pos[to];
+        s.shift = pass * bits;
+        launch(hist_kernel, s.tiles);
+        launch(scan_kernel, 1u << bits);
+        launch(scatter_kernel, s.tiles);
     }
-    if (e == cudaSuccess && zero) {
-        const int64_t rows = over(a.vocab, h.dev.sms * 4);
-        e = launch_lm(zero_kernel, dim3(static_cast<unsigned>(over(a.vocab, rows))), kSortThreads, 0, h.stream, true, 1, a,
-                      static_cast<const uint32_t *>(h.key[0]), z, rows);
-    }
-    return e;
+    return lm_cuda(e, "launch");
 }
 
 }  // namespace
@@ -956,6 +985,7 @@ int ea_embed_init(const ea_embed_config *cfg, void *workspace, size_t workspace_
     }
     h->hist = reinterpret_cast<uint32_t *>(take(l.hist));
     h->total = reinterpret_cast<uint32_t *>(take(l.total_));
+    h->seen = reinterpret_cast<uint32_t *>(take(l.seen));
     h->partial = reinterpret_cast<float *>(take(l.partial));
     r = h->dev.query();
     h->dev.sms = std::min(h->dev.sms, kMaxSms);
@@ -1024,13 +1054,14 @@ int ea_embed_grad(ea_embed *h, const ea_embed_call *c, const void *tokens, const
     if (a.n == 0 && accumulate) return EA_OK;
     const int wb = static_cast<int>(type_bytes(c->table_type));
     const ZeroTable z{static_cast<unsigned char *>(dw), wb};
-    cudaError_t e = order_tokens(*h, a, z, !accumulate);
-    if (e != cudaSuccess || a.n == 0) return lm_cuda(e, "launch");
+    const int ordered = order_tokens(*h, a, z, !accumulate);
+    if (ordered != EA_OK || a.n == 0) return ordered;
+    cudaError_t e = cudaSuccess;
     const int vec = rows_aligned(dy, c->row_type, a.dim, c->outer > 1 ? c->row_outer : 0, c->inner > 1 ? c->row_inner : 0) &&
                             rows_aligned(dw, c->table_type, a.dim, a.table_stride, 0)
                         ? 16 / static_cast<int>(type_bytes(c->row_type)) : 1;
     const SumShape shape(a.dim, vec);
-    SumArgs s{a, h->key[0], h->pos[0], h->partial, up(a.dim, kMaxVec), chunk_length(a.n, shape.slabs, h->dev.sms), accumulate};
+    const SumArgs s{a, h->key[0], h->pos[0], h->partial, up(a.dim, kMaxVec), chunk_length(a.n, shape, h->dev.sms), accumulate};
     const unsigned chunks = static_cast<unsigned>(over(a.n, s.chunk));
     with_type(c->row_type, [&](auto *yt) {
         using Y = std::remove_reference_t<decltype(*yt)>;
