@@ -10,8 +10,8 @@
 
 namespace ea {
 
-constexpr int kAdamThreads = 256;
-constexpr int kAdamCtasPerSm = 2;  // 128 registers per thread; a persistent grid of them
+constexpr int kAdamThreads = 128;
+constexpr int kAdamCtasPerSm = 4;  // 128 registers per thread; a persistent grid of them
 constexpr int kBlock = EA_ADAMW_BLOCK;  // a warp's unit of work: eight coordinates per lane
 
 // What a step needs to know of the steps before it.  The last CTA of a step that is not skipped advances it.
@@ -469,9 +469,9 @@ __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s,
 // scale is one warp reduction.  Whole aligned blocks come through a ring of kAdamStages stages per warp in shared
 // memory, filled by asynchronous copies: the loads in flight take no registers, which the arithmetic of the 8-bit
 // states needs, and enough of them are in flight to cover their latency.
-// Stages: up to 4, in half of an SM's shared memory.
+// Stages: up to 4, in a quarter of an SM's shared memory.
 template <class Stage>
-constexpr int kAdamStages = std::min(4, 108 * 1024 / (static_cast<int>(sizeof(Stage)) * (kAdamThreads / 32)));
+constexpr int kAdamStages = std::min(4, 54 * 1024 / (static_cast<int>(sizeof(Stage)) * (kAdamThreads / 32)));
 
 template <class P, class G, class C, int BITS>
 __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
