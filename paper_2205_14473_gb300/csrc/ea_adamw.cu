@@ -1,6 +1,14 @@
 // ea_adamw.cu -- ea_adamw_step: one AdamW step (Loshchilov and Hutter; Adam's bias correction folded into the
 // step size and epsilon as in the last remark of Kingma and Ba's Section 2) over a list of tensors, with
 // moments in binary32 or in 8 bits.
+//
+// Measured on one GB300 (us a step, GB/s of the bytes that it cannot do without, against a copy's 6,800):
+//   354 M binary32 parameters, bfloat16 gradients and copy, 32-bit states  1,512 to 1,540 us, 6,430 GB/s: HBM
+//   ResNet-18's 62 tensors, all binary32                                   60 us, 5,440 GB/s: launch and first loads
+//   108 M bfloat16 parameters and gradients, 8-bit states                  337 us, 3,240 GB/s: instruction issue
+// An 8-bit step is about 70 instructions per coordinate (ten rounds of the generator for four coordinates are ten of
+// them, a fifth of the time); with the arithmetic taken out the same kernel takes 334 us where each block's scales go
+// by themselves, and 185 where eight blocks' go together, but that costs the full step more than it saves.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -474,7 +482,8 @@ template <class Stage>
 constexpr int kAdamStages = std::min(4, 54 * 1024 / (static_cast<int>(sizeof(Stage)) * (kAdamThreads / 32)));
 
 template <class P, class G, class C, int BITS>
-__global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm)
+    adamw_kernel(const __grid_constant__ AdamArgs a, const __grid_constant__ GradList list)
 {
     using S = AdamCell<BITS>;
     using Stage = AdamStage<P, G, S>;
@@ -502,7 +511,8 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm) adamw_kernel(con
                                      static_cast<S *>(T.v) + off, T.m_scale + (u - first), T.v_scale + (u - first)};
             const uint32_t tensor = static_cast<uint32_t>(a.tensor0 + i), t = static_cast<uint32_t>(st.t);
             uint64_t quad = static_cast<uint64_t>(off) >> 2;
-            const bool aligned = reinterpret_cast<uintptr_t>(at.p) % sizeof(Quad<P>) == 0 && reinterpret_cast<uintptr_t>(at.g) % sizeof(Quad<G>) == 0 &&
+            const bool aligned = reinterpret_cast<uintptr_t>(at.p) % sizeof(Quad<P>) == 0 &&
+                                 reinterpret_cast<uintptr_t>(at.g) % sizeof(Quad<G>) == 0 &&
                                  reinterpret_cast<uintptr_t>(at.copy) % sizeof(Quad<C>) == 0 &&
                                  (reinterpret_cast<uintptr_t>(at.m) | reinterpret_cast<uintptr_t>(at.v)) % sizeof(Quad<S>) == 0;
             const int64_t whole = aligned ? min(hi, first + size / kBlock) : u;  // blocks below it are whole and aligned

@@ -1,5 +1,11 @@
 // ea_embed.cu -- the lookup of tokens in an embedding table (ea_embed_lookup) and the gradient of the table
 // (ea_embed_grad).
+//
+// Both move rows and do next to no arithmetic.  Measured on one GB300 (us a call, calls one behind another; GB/s of the
+// bytes that a call cannot do without, against a copy's 6,800):
+//   lookup, 16,384 of 50,257 x 1600, 32 to 16 bits   19.2 us, 4,840 GB/s (a plain copy of as many bytes: 25.8 us)
+//   gradient of that batch, 32 bits written          86 us, 4,350 GB/s: the sort and the zero rows (52 us), sums, joins
+//   gradient, 260,096 tokens, 768 wide, half padding 94 us, 3,160 GB/s: six launches of sort (38 us), sums at 7 TB/s (41)
 #include <cooperative_groups.h>
 #include <type_traits>
 
@@ -71,7 +77,7 @@ __device__ __forceinline__ void store_pack(Y *p, Pack<Y, VEC> &x) { move_pack<Y,
 //   rows of kWideRow packs or more: a warp takes a piece of one row, so that its addresses are formed once for all of
 //     its packs; one token's row is still spread over as many warps as it has pieces;
 //   narrower ones: the packs of all tokens are dealt out in order, so that no lane idles.
-// The index arithmetic decides: dealt out in order, 16,384 rows of 400 packs took 23.8 us, half of it instructions.
+// The index arithmetic decides: dealt out in order, 16,384 rows of 400 packs took 23.8 us; a piece per warp takes 19.2.
 
 constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;  // narrow rows
@@ -161,7 +167,8 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupCtasPerSm) lookup_wide_
     const int64_t warps = static_cast<int64_t>(gridDim.x) * (kLookupThreads / 32);
     const int64_t start = static_cast<int64_t>(blockIdx.x) * (kLookupThreads / 32) + (threadIdx.x >> 5);
     if (start >= a.total) return;
-    uint32_t t = static_cast<uint32_t>(a.pieces == 1 ? start : start / a.pieces), c = static_cast<uint32_t>(start - static_cast<int64_t>(t) * a.pieces);
+    uint32_t t = static_cast<uint32_t>(a.pieces == 1 ? start : start / a.pieces);
+    uint32_t c = static_cast<uint32_t>(start - static_cast<int64_t>(t) * a.pieces);
     int64_t v = token_at(a.e, t);
     for (int64_t u = start; u < a.total; u += warps) {
         const bool inside = v >= 0 && v < a.e.vocab;
@@ -1069,7 +1076,8 @@ int ea_embed_grad(ea_embed *h, const ea_embed_call *c, const void *tokens, const
             using W = std::remove_reference_t<decltype(*wt)>;
             const dim3 grid(chunks, static_cast<unsigned>(shape.slabs));
             auto kernel = vec > 1 ? sum_kernel<Y, W, 16 / sizeof(Y)> : sum_kernel<Y, W, 1>;
-            e = launch_lm(kernel, grid, shape.threads, sum_smem(vec, shape.threads), h->stream, true, 1, s, static_cast<const Y *>(dy), static_cast<W *>(dw));
+            e = launch_lm(kernel, grid, shape.threads, sum_smem(vec, shape.threads), h->stream, true, 1, s, static_cast<const Y *>(dy),
+                          static_cast<W *>(dw));
             if (e == cudaSuccess && chunks > 1)
                 e = launch_lm(combine_kernel<W>, dim3(chunks - 1, kCombineSplit), kCombineThreads, 0, h->stream, true, 1, s,
                               static_cast<W *>(dw));

@@ -1,4 +1,7 @@
 // ea_norm.cu -- ea_grad_norm: the 2-norm of a list of gradients and the factor that clips them.
+//
+// One launch for up to kGradBatch tensors.  108 M bfloat16 values take 39.8 us (5,450 GB/s of a copy's 6,800), 62
+// tensors of 11.7 M binary32 values 16.4 us (2,850 GB/s: 3 us of launch, two turns of loads, the last CTA's sum).
 #include <type_traits>
 
 #include "ea_lm.cuh"

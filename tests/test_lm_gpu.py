@@ -98,6 +98,20 @@ def test_lookup_of_strided_tokens_tables_and_rows():
     _check_lookup(table.lookup(batch[:, 2], flat[1:].view(vocab, dim)), batch[:, 2], flat[1:].view(vocab, dim), 1.0)
 
 
+@pytest.mark.parametrize("dim", [5000, 5003, 2056])
+@pytest.mark.parametrize("n", [1, 5, 3000])
+def test_lookup_of_long_rows(dim, n):
+    """Rows of several pieces, more of them than run at a time."""
+    w, ids = _randn(300, dim, seed=dim), _tokens((n,), 300, n)
+    _check_lookup(ea.Embedding(300, dim, n, scale=0.5).lookup(ids, w, dtype=BF16), ids, w, 0.5)
+
+
+@pytest.mark.parametrize("dim", [7, 64, 100])
+def test_lookup_of_many_short_rows(dim):
+    w, ids = _randn(5000, dim, seed=dim, dtype=BF16), _tokens((300, 1001), 5000, dim)
+    _check_lookup(ea.Embedding(5000, dim, 300 * 1001).lookup(ids[:, :-1], w), ids[:, :-1], w, 1.0)
+
+
 def test_lookup_keeps_infinities_and_nan():
     w = _randn(4, 16, seed=8)
     w[0, 3], w[1, 5], w[2, 7] = float("inf"), float("-inf"), float("nan")
@@ -200,9 +214,9 @@ def test_grad_of_one_token_and_of_padding(n, tied):
         _check_grad(got, ids, dy, 1.0, padding=0, before=before if tied else None)
 
 
-@pytest.mark.parametrize("n,vocab", [(70_000, 50_257), (200_000, 1000), (131_073, 3)])
-def test_grad_of_many_tokens(n, vocab):
-    dim = 40
+@pytest.mark.parametrize("n,vocab,dim", [(70_000, 50_257, 40), (200_000, 1000, 40), (131_073, 3, 40), (70_000, 200_000, 9),
+                                         (65_536, 300, 8), (65_537, 131_073, 8)])
+def test_grad_of_many_tokens(n, vocab, dim):
     ids, dy = _tokens((n,), vocab, 16, skew=1.0), _randn(n, dim, seed=17, dtype=BF16)
     table = ea.Embedding(vocab, dim, n)
     got = table.grad(ids, dy)
@@ -452,10 +466,12 @@ def test_adamw_8(ptype, gtype, copy, sizes):
 
 
 @pytest.mark.parametrize("ptype,gtype", [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F16), (BF16, F32), (F32, F16)])
-@pytest.mark.parametrize("mag", [1e-3, 1e-19])
+@pytest.mark.parametrize("mag", [1e-3, 1e-19, 1e13])
 def test_adamw_8_states_are_binary32(ptype, gtype, mag):
     """The moments and the root before they are rounded to 8 bits, one binary32 rounding per operation: torch's
     elementary operations, each its own kernel, and the format's rounding in integers give the same bytes."""
+    if mag > 1e4 and gtype == F16:
+        mag = 1e4                                           # the type's range; 1e13 has squares beyond 2^60
     n = 3_000_000 if mag == 1e-3 else 300_000
     p, opt = _randn(n, seed=90, dtype=ptype), None
     factor = torch.tensor([1.0, 0.37], device="cuda")
