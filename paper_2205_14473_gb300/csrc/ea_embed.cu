@@ -758,17 +758,19 @@ struct SumShape {
     }
 };
 
-// Chunks that the sorted list is cut into at most: as many as run at a time, 1,024 threads per SM, slabs counted.
-int64_t most_chunks(const SumShape &shape, int sms)
+// Chunks that the sorted list is cut into at most.  The cut decides which binary32 sums are formed before they are
+// joined, so it goes by the width alone, whatever the types, the rows' alignment and the device: 1,024 threads on each of
+// 152 SMs where rows are read in packs of kMaxVec, slabs counted.  Binary32 rows, which fill as many threads with half as
+// many chunks: 260,096 x 768 186 us (with half as many chunks 203), half of them padding 134 (123); 16,384 x 1600 90.6 (90.2).
+constexpr int kCutSms = 152;
+int64_t most_chunks(int64_t dim)
 {
-    return std::max<int64_t>(1, sms * (1024 / shape.threads) / shape.slabs);
+    const SumShape shape(dim, kMaxVec);
+    return std::max<int64_t>(1, kCutSms * (1024 / shape.threads) / shape.slabs);
 }
 
 // Entries per chunk, no fewer than kMinChunk (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
-int64_t chunk_length(int64_t n, const SumShape &shape, int sms)
-{
-    return std::max<int64_t>(kMinChunk, over(n, most_chunks(shape, sms)));
-}
+int64_t chunk_length(int64_t n, int64_t dim) { return std::max<int64_t>(kMinChunk, over(n, most_chunks(dim))); }
 
 struct EmbedLayout {
     size_t status, list, hist, total_, seen, partial;
@@ -788,9 +790,7 @@ EmbedLayout embed_layout(const ea_embed_config &cfg)
         l.total_ = kDigits * 4;
         l.seen = up(over(cfg.vocab, 32) * 4, 256);
     }
-    int64_t chunks = 0;  // the most that chunk_length allows, in either type
-    for (int vec : {kMaxVec, 4, 1}) chunks = std::max(chunks, std::min(over(n, kMinChunk), most_chunks(SumShape(cfg.dim, vec), kMaxSms)));
-    l.partial = 2 * chunks * up(cfg.dim, kMaxVec) * 4;
+    l.partial = 2 * std::min(over(n, kMinChunk), most_chunks(cfg.dim)) * up(cfg.dim, kMaxVec) * 4;  // all that chunk_length allows
     return l;
 }
 
@@ -1068,7 +1068,7 @@ int ea_embed_grad(ea_embed *h, const ea_embed_call *c, const void *tokens, const
                             rows_aligned(dw, c->table_type, a.dim, a.table_stride, 0)
                         ? 16 / static_cast<int>(type_bytes(c->row_type)) : 1;
     const SumShape shape(a.dim, vec);
-    const SumArgs s{a, h->key[0], h->pos[0], h->partial, up(a.dim, kMaxVec), chunk_length(a.n, shape, h->dev.sms), accumulate};
+    const SumArgs s{a, h->key[0], h->pos[0], h->partial, up(a.dim, kMaxVec), chunk_length(a.n, a.dim), accumulate};
     const unsigned chunks = static_cast<unsigned>(over(a.n, s.chunk));
     with_type(c->row_type, [&](auto *yt) {
         using Y = std::remove_reference_t<decltype(*yt)>;

@@ -225,6 +225,29 @@ def test_grad_of_many_tokens(n, vocab, dim):
         assert torch.equal(table.grad(ids, dy), got)
 
 
+@pytest.mark.parametrize("n,vocab,dim", [(20_000, 300, 64), (3000, 7, 1600), (70_000, 1000, 104), (5000, 40, 8)])
+@pytest.mark.parametrize("yt,wt", [(BF16, F32), (F32, F32), (F32, BF16), (F16, F16)])
+@pytest.mark.parametrize("tied", [False, True])
+def test_grad_has_the_same_bits_at_any_alignment(n, vocab, dim, yt, wt, tied):
+    """The order of the sums goes by the tokens and the sizes: rows and tables off a 16-byte boundary, and rows with gaps
+    between them, get the bits of aligned ones (runs of one token that cross many pieces of the sorted list)."""
+    ids, dy, before = _tokens((n,), vocab, 30, skew=0.5), _randn(n, dim, seed=31, dtype=yt), _randn(vocab, dim, seed=32, dtype=wt)
+    table = ea.Embedding(vocab, dim, n, scale=1.5)
+    want = table.grad(ids, dy, out=before.clone(), accumulate=tied)
+
+    def off(t, k):
+        flat = torch.empty(t.numel() + k, device="cuda", dtype=t.dtype)
+        flat[k:] = t.flatten()
+        return flat[k:].view(t.shape)
+
+    wide = torch.empty(n, dim + 3, device="cuda", dtype=yt)
+    wide[:, 1:dim + 1] = dy
+    for rows, out in ((dy, off(before, 1)), (off(dy, 1), before.clone()), (off(dy, 3), off(before, 5)), (wide[:, 1:dim + 1], before.clone())):
+        assert torch.equal(table.grad(ids, rows, out=out, accumulate=tied), want)
+    by_batch = table.grad(ids.view(-1, 4).to(torch.int32), dy.view(-1, 4, dim), out=before.clone(), accumulate=tied)
+    assert torch.equal(by_batch, want)
+
+
 def test_grad_of_strided_inputs():
     vocab, dim, b, s = 30, 12, 6, 50
     batch, dh = _tokens((b, s + 1), vocab, 18), _randn(b, s + 1, dim + 4, seed=19)
