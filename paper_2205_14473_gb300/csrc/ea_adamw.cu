@@ -700,13 +700,14 @@ int ea_adamw_init(const ea_adamw_config *cfg, void *workspace, size_t workspace_
     if (r != EA_OK) return r;
     const AdamLayout L = adam_layout(*cfg);
     if ((r = check_workspace(workspace, workspace_bytes, L.total())) != EA_OK) return r;
+    DeviceOf dev;
+    if ((r = dev.query()) != EA_OK) return r;
     ea_adamw *h = new (std::nothrow) ea_adamw;
     if (!h) return lm_fail(EA_E_INVAL, "out of host memory");
-    r = h->dev.query();
+    h->dev = dev;
     if (cfg->param_type == EA_T_F32) adam_kernel<float>(*cfg, h->kernel, h->smem);
     else adam_kernel<bf16>(*cfg, h->kernel, h->smem);
-    if (r == EA_OK)
-        r = lm_cuda(cudaFuncSetAttribute(h->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(h->smem)), "shared memory");
+    r = lm_cuda(cudaFuncSetAttribute(h->kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(h->smem)), "shared memory");
     try {
         h->stream = static_cast<cudaStream_t>(stream);
         h->cfg = *cfg;

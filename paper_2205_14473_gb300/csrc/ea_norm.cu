@@ -224,9 +224,11 @@ int ea_grad_norm_init(const ea_grad_norm_config *cfg, void *workspace, size_t wo
     if (r != EA_OK) return r;
     const NormLayout L = norm_layout(*cfg, kMaxSms);
     if ((r = check_workspace(workspace, workspace_bytes, L.total())) != EA_OK) return r;
+    DeviceOf dev;
+    if ((r = dev.query()) != EA_OK) return r;
     ea_norm *h = new (std::nothrow) ea_norm;
     if (!h) return lm_fail(EA_E_INVAL, "out of host memory");
-    r = h->dev.query();
+    h->dev = dev;
     try {
         h->stream = static_cast<cudaStream_t>(stream);
         h->type = cfg->grad_type;

@@ -1,6 +1,8 @@
 """The operators of include/ea_lm.h without a GPU: what they refuse before any CUDA call, and the sizes of their
 workspaces."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -92,3 +94,31 @@ def test_null_handles(ea_lib):
     assert ea_lib.ea_grad_norm(None, one, 1.0, 1.0, 4096) == ea.EA_E_INVAL
     assert ea_lib.ea_adamw_step(None, one, 1e-3, None) == ea.EA_E_INVAL
     assert ea_lib.ea_adamw_step_index(None, None) == ea.EA_E_INVAL
+
+
+def test_init_without_a_device(tmp_path):
+    """Where the device cannot be asked for its SMs an init call ends there: built with the C++ library's assertions, it
+    reports the CUDA error instead of sharing work out over no SMs."""
+    from paper_2205_14473_gb300 import build as B
+
+    main = tmp_path / "main.cpp"
+    main.write_text("""
+        #include "ea_lm.h"
+        namespace ea { void set_last_error(const char *) {} }
+        int main()
+        {
+            const int64_t size = 10;
+            void *at = reinterpret_cast<void *>(4096);
+            ea_grad_norm_config n{1, EA_T_F32, &size};
+            ea_norm *norm = nullptr;
+            ea_adamw_tensor t{size, at, at, at, nullptr, nullptr, nullptr, 0.0f, 1.0f};
+            ea_adamw_config a{1, EA_T_F32, EA_T_F32, EA_T_BF16, 32, 0.9f, 0.999f, 1e-8f, 0, 0, &t};
+            ea_adamw *adamw = nullptr;
+            if (ea_grad_norm_init(&n, at, size_t{1} << 20, nullptr, &norm) != EA_E_CUDA || norm) return 1;
+            if (ea_adamw_init(&a, at, size_t{1} << 20, nullptr, &adamw) != EA_E_CUDA || adamw) return 2;
+            return 0;
+        }""")
+    units = [os.path.join(B.CSRC, f) for f in ("ea_norm.cu", "ea_adamw.cu")]
+    subprocess.run([B.NVCC, "-gencode", "arch=compute_103a,code=compute_103a", "-std=c++17", "--threads", "2", "-Xcompiler",
+                    "-D_GLIBCXX_ASSERTIONS", "-I" + os.path.join(B.ROOT, "include"), "-o", tmp_path / "main", main, *units], check=True)
+    assert subprocess.run([tmp_path / "main"], env={**os.environ, "CUDA_VISIBLE_DEVICES": ""}).returncode == 0
