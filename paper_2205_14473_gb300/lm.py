@@ -10,12 +10,14 @@ lookup and the table's gradient, the clipped gradient norm, and AdamW over many 
     opt.step(grads, lr=1e-3, clip=norm(grads, max_norm=1.0))
 
 As with EARound, the calls only marshal arguments, a handle is bound to one stream (by default the current one
-where it is made), and every call is asynchronous on it.  A call made while another stream is current is
-ordered after the work of that stream so far, and that stream's later work after the call.
+where it is made), and every call is asynchronous on it.  A call made while another stream of the handle's device is
+current is ordered after the work of that stream so far, and that stream's later work after the call; which device is
+current does not matter.
 """
 from __future__ import annotations
 
 import ctypes
+from itertools import chain
 
 import torch
 
@@ -61,20 +63,22 @@ class _Handle:
             getattr(self._L, self._kind + "_destroy")(h)
             self.h = None
 
-    def _enter(self):
-        """Orders the handle's stream after the current one where they differ, and returns that."""
-        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
-            return None
-        now = torch.cuda.current_stream(self.device)
-        self.stream.wait_stream(now)
-        return now
-
-    def _leave(self, status: int, now, *tensors) -> None:
-        """The end of a call that read or wrote `tensors`, with _enter's result."""
-        if now is not None:
-            now.wait_stream(self.stream)
-            for t in tensors:
-                t.record_stream(self.stream)
+    def _call(self, f, args, tensors) -> None:
+        """f, a call of the library on this handle that reads or writes `tensors`, with the handle's device current and in
+        order with the current stream."""
+        if torch._C._cuda_getDevice() == self._index and torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
+            status = f(self.h, *args)
+        else:
+            with torch.cuda.device(self._index):
+                now = torch.cuda.current_stream()
+                if now.cuda_stream == self._raw:
+                    status = f(self.h, *args)
+                else:
+                    self.stream.wait_stream(now)
+                    status = f(self.h, *args)
+                    now.wait_stream(self.stream)
+                    for t in tensors:
+                        t.record_stream(self.stream)
         if status:
             _check(status)
 
@@ -173,10 +177,7 @@ class Embedding(_Handle):
             self._rows(out, tokens, "out")
             if dtype is not None and out.dtype != dtype:
                 _refuse(f"out is {out.dtype}, not {dtype}")
-        now = self._enter()
-        status = self._L.ea_embed_lookup(self.h, self._c, ids.data_ptr(), weight.data_ptr(), out.data_ptr())
-        if status or now is not None:
-            self._leave(status, now, ids, weight, out)
+        self._call(self._L.ea_embed_lookup, (self._c, ids.data_ptr(), weight.data_ptr(), out.data_ptr()), (ids, weight, out))
         return out
 
     def grad(self, tokens, dy, out=None, accumulate: bool = False, dtype=torch.float32):
@@ -191,14 +192,12 @@ class Embedding(_Handle):
         if isinstance(dy, torch.Tensor) and dy.dim() and (dy.stride(-1) != 1 or tokens.dim() not in (1, 2)):
             dy = dy.contiguous()
         self._rows(dy, tokens, "dy")
-        now = self._enter()
-        status = self._L.ea_embed_grad(self.h, self._c, ids.data_ptr(), dy.data_ptr(), out.data_ptr(), int(accumulate))
-        if status or now is not None:
-            self._leave(status, now, ids, dy, out)
+        self._call(self._L.ea_embed_grad, (self._c, ids.data_ptr(), dy.data_ptr(), out.data_ptr(), int(accumulate)), (ids, dy, out))
         return out
 
     def sync(self) -> None:
-        _check(self._L.ea_embed_sync_status(self.h))
+        with torch.cuda.device(self._index):
+            _check(self._L.ea_embed_sync_status(self.h))
 
 
 class TensorList:
@@ -251,10 +250,7 @@ class GradNorm(_Handle):
             self._on_device(out, "out")
             if out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
                 _refuse("out is two contiguous float32 values")
-        now = self._enter()
-        status = self._L.ea_grad_norm(self.h, g._ptrs, grad_scale, max_norm, out.data_ptr())
-        if status or now is not None:
-            self._leave(status, now, out, *g.tensors)
+        self._call(self._L.ea_grad_norm, (g._ptrs, grad_scale, max_norm, out.data_ptr()), chain((out,), g.tensors))
         return out
 
 
@@ -337,13 +333,12 @@ class AdamW(_Handle):
             self._on_device(clip, "clip")
             if clip.dtype != torch.float32 or clip.numel() != 2 or not clip.is_contiguous():
                 _refuse("clip is two contiguous float32 values")
-        now = self._enter()
-        status = self._L.ea_adamw_step(self.h, g._ptrs, lr, None if clip is None else clip.data_ptr())
-        if status or now is not None:
-            self._leave(status, now, *self._touched, *g.tensors, *(() if clip is None else (clip,)))
+        self._call(self._L.ea_adamw_step, (g._ptrs, lr, None if clip is None else clip.data_ptr()),
+                   chain(self._touched, g.tensors, () if clip is None else (clip,)))
 
     @property
     def t(self) -> int:
         n = _i64(0)
-        _check(self._L.ea_adamw_step_index(self.h, ctypes.byref(n)))
+        with torch.cuda.device(self._index):
+            _check(self._L.ea_adamw_step_index(self.h, ctypes.byref(n)))
         return n.value

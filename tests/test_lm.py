@@ -122,3 +122,66 @@ def test_init_without_a_device(tmp_path):
     subprocess.run([B.NVCC, "-gencode", "arch=compute_103a,code=compute_103a", "-std=c++17", "--threads", "2", "-Xcompiler",
                     "-D_GLIBCXX_ASSERTIONS", "-I" + os.path.join(B.ROOT, "include"), "-o", tmp_path / "main", main, *units], check=True)
     assert subprocess.run([tmp_path / "main"], env={**os.environ, "CUDA_VISIBLE_DEVICES": ""}).returncode == 0
+
+
+@pytest.mark.parametrize("here,raw", [(0, 7), (1, 7), (1, 5)])
+def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
+    """A handle of device 1 on stream 7, called while device `here` and stream `raw` of device 1 are current (all of it
+    faked): the library sees device 1, the streams wait for one another where they differ, and device `here` is current
+    again afterwards."""
+    import contextlib
+    from types import SimpleNamespace
+
+    import torch
+
+    from paper_2205_14473_gb300 import lm
+
+    log, device = [], [here]
+
+    @contextlib.contextmanager
+    def switch(index):
+        before, device[0] = device[0], index
+        yield
+        device[0] = before
+
+    def stream(which):
+        return SimpleNamespace(cuda_stream=which, wait_stream=lambda other: log.append((which, other.cuda_stream)))
+
+    def call(name):
+        def f(*args):
+            log.append((name, device[0]))
+            return ea.EA_OK
+        return f
+
+    monkeypatch.setattr(torch.cuda, "device", switch)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: stream(raw))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: device[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: raw, raising=False)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: log.append(("record", s.cuda_stream)))
+
+    def handle(kind, **fields):
+        h = kind.__new__(kind)
+        names = ("ea_embed_lookup", "ea_embed_grad", "ea_embed_sync_status", "ea_grad_norm", "ea_adamw_step", "ea_adamw_step_index",
+                 "ea_embed_destroy", "ea_grad_norm_destroy", "ea_adamw_destroy")
+        h.__dict__.update(device=torch.device("cpu"), _index=1, _raw=7, stream=stream(7), h=1, _L=SimpleNamespace(**{n: call(n) for n in names}),
+                          **fields)
+        return h
+
+    def seen(name, tensors, f):
+        log.clear()
+        f()
+        want = [(name, 1)] if raw == 7 else [(7, 5), (name, 1), (5, 7)] + [("record", 7)] * tensors
+        assert log == want and device[0] == here, name
+
+    w, g = torch.ones(4, 2), torch.ones(8)
+    table = handle(lm.Embedding, vocab=4, dim=2, _shape=torch.Size((4, 2)), _c=A.ea_embed_call())
+    ids = torch.tensor([1, 3])
+    seen("ea_embed_lookup", 3, lambda: table.lookup(ids, w))
+    seen("ea_embed_grad", 3, lambda: table.grad(ids, torch.ones(2, 2)))
+    norm = handle(lm.GradNorm, sizes=[8], dtype=torch.float32)
+    seen("ea_grad_norm", 2, lambda: norm([g]))
+    opt = handle(lm.AdamW, sizes=[8], dtype=torch.float32, _touched=(g, g, g))
+    seen("ea_adamw_step", 5, lambda: opt.step([g], lr=1e-3, clip=torch.ones(2)))
+    log.clear()
+    table.sync()
+    assert opt.t == 0 and log == [("ea_embed_sync_status", 1), ("ea_adamw_step_index", 1)] and device[0] == here
