@@ -27,6 +27,7 @@ from .lm_abi import (EA_ADAMW_BLOCK, EA_T_BF16, EA_T_F16, EA_T_F32, EA_T_I32, EA
 
 _TYPE = {torch.float32: EA_T_F32, torch.bfloat16: EA_T_BF16, torch.float16: EA_T_F16}
 _TOKEN = {torch.int32: EA_T_I32, torch.int64: EA_T_I64}
+_C = torch._C
 
 
 def _refuse(msg: str, status: int = EA_E_INVAL):
@@ -63,24 +64,27 @@ class _Handle:
             getattr(self._L, self._kind + "_destroy")(h)
             self.h = None
 
-    def _call(self, f, args, tensors) -> None:
-        """f, a call of the library on this handle that reads or writes `tensors`, with the handle's device current and in
-        order with the current stream."""
-        if torch._C._cuda_getDevice() == self._index and torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
+    def _call(self, f, args, *tensors) -> None:
+        """f, a call of the library on this handle that reads or writes `tensors` (lists of them)."""
+        if _C._cuda_getDevice() == self._index and _C._cuda_getCurrentRawStream(self._index) == self._raw:
             status = f(self.h, *args)
         else:
-            with torch.cuda.device(self._index):
-                now = torch.cuda.current_stream()
-                if now.cuda_stream == self._raw:
-                    status = f(self.h, *args)
-                else:
-                    self.stream.wait_stream(now)
-                    status = f(self.h, *args)
-                    now.wait_stream(self.stream)
-                    for t in tensors:
-                        t.record_stream(self.stream)
+            status = self._call_from_elsewhere(f, args, chain(*tensors))
         if status:
             _check(status)
+
+    def _call_from_elsewhere(self, f, args, tensors) -> int:
+        """The same with the handle's device current, and in order with the current stream."""
+        with torch.cuda.device(self._index):
+            now = torch.cuda.current_stream()
+            if now.cuda_stream == self._raw:
+                return f(self.h, *args)
+            self.stream.wait_stream(now)
+            status = f(self.h, *args)
+            now.wait_stream(self.stream)
+            for t in tensors:
+                t.record_stream(self.stream)
+            return status
 
     def _on_device(self, t, what: str) -> None:
         if not isinstance(t, torch.Tensor):
@@ -250,7 +254,7 @@ class GradNorm(_Handle):
             self._on_device(out, "out")
             if out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
                 _refuse("out is two contiguous float32 values")
-        self._call(self._L.ea_grad_norm, (g._ptrs, grad_scale, max_norm, out.data_ptr()), chain((out,), g.tensors))
+        self._call(self._L.ea_grad_norm, (g._ptrs, grad_scale, max_norm, out.data_ptr()), (out,), g.tensors)
         return out
 
 
@@ -334,7 +338,7 @@ class AdamW(_Handle):
             if clip.dtype != torch.float32 or clip.numel() != 2 or not clip.is_contiguous():
                 _refuse("clip is two contiguous float32 values")
         self._call(self._L.ea_adamw_step, (g._ptrs, lr, None if clip is None else clip.data_ptr()),
-                   chain(self._touched, g.tensors, () if clip is None else (clip,)))
+                   self._touched, g.tensors, () if clip is None else (clip,))
 
     @property
     def t(self) -> int:
