@@ -11,7 +11,8 @@ vector [E, M, b], as EARound takes it.  A worker's step is
     clip = norm([g])                        the gradient's norm and clipping factor
 
 and the parameters move either by AdamW on the clipped mean gradient (32- or 8-bit states), or by a round of
-Efficient-Adam, in which every worker compresses its clipped gradient's Adam step.
+Efficient-Adam, in which every worker compresses its clipped gradient's Adam step.  A gradient that is not finite is not
+used: AdamW skips the step, a worker of the round takes part with a gradient of zeros.
 
     python -m paper_2205_14473_gb300.bigram --optimizer adamw8
     python -m paper_2205_14473_gb300.bigram --optimizer round --workers 4
@@ -87,7 +88,7 @@ def train(optimizer: str = "adamw", vocab: int = 512, dim: int = 64, sequences: 
     norm, clip = ea.GradNorm([d]), torch.empty(2, device=device)
     if optimizer == "round":
         cfg = ea.EAConfig(d=d, n=workers, qw=W.uniform_q(4, 4096, True), qs=W.uniform_q(8, 4096), alpha=lr, adam_form=1, seed=seed)
-        rnd = ea.EARound(cfg)
+        rnd, zero = ea.EARound(cfg), torch.zeros((), device=device)
     else:
         # the bias is a vector: no decay
         opt = ea.AdamW(list(model.x.split(model.sizes)), state_bits=8 if optimizer == "adamw8" else 32, weight_decay=[0.01, 0.01, 0.0],
@@ -97,8 +98,9 @@ def train(optimizer: str = "adamw", vocab: int = 512, dim: int = 64, sequences: 
     for t in range(steps):
         step_losses = [model.gradient(corpus.batch(sequences, length, 1 + t * workers + i), grads[i]) for i in range(workers)]
         if optimizer == "round":
-            for g in grads:
-                g.mul_(norm([g], max_norm=max_norm, out=clip)[1])
+            for g in grads:  # a factor of NaN in the workers' moments and residuals would stay there
+                factor = norm([g], max_norm=max_norm, out=clip)[1]
+                torch.where(factor.isnan(), zero, g * factor, out=g)
             rnd.step(grads, model.x)
         else:
             torch.mean(torch.stack(grads), 0, out=mean)

@@ -45,3 +45,22 @@ def test_every_optimizer_learns(optimizer):
     losses = train(optimizer, steps=150)
     assert abs(losses[0] - np.log(512)) < 0.1
     assert np.mean(losses[-10:]) < 0.5 * np.log(512)
+
+
+@pytest.mark.parametrize("optimizer", ["adamw", "adamw8", "round"])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_gradient_that_is_not_finite_does_not_stay(monkeypatch, optimizer, bad):
+    """Every worker's gradient of the fourth step holds a value that is not finite: the training goes on and learns."""
+    calls, gradient = [], Bigram.gradient
+
+    def poisoned(self, batch, g):
+        loss = gradient(self, batch, g)
+        calls.append(1)
+        if 3 * 4 < len(calls) <= 4 * 4:
+            g[5] = bad
+        return loss
+
+    monkeypatch.setattr(Bigram, "gradient", poisoned)
+    losses = train(optimizer, steps=60)
+    assert len(calls) == 60 * 4 and np.isfinite(losses).all()
+    assert np.mean(losses[-5:]) < 0.9 * np.log(512)
