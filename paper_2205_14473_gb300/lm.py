@@ -13,6 +13,10 @@ As with EARound, the calls only marshal arguments, a handle is bound to one stre
 where it is made), and every call is asynchronous on it.  A call made while another stream of the handle's device is
 current is ordered after the work of that stream so far, and that stream's later work after the call; which device is
 current does not matter.
+
+None of them is an autograd operation: a result has no graph, whether or not an input requires a gradient (Embedding.grad
+is lookup's backward pass, for the caller to run).  A tensor that a call writes to counts as modified in place, so a
+backward pass that had saved it fails instead of using the new values.
 """
 from __future__ import annotations
 
@@ -20,6 +24,7 @@ import ctypes
 from itertools import chain
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import EA_E_INVAL, EAError, _check, lib
 from .lm_abi import (EA_ADAMW_BLOCK, EA_T_BF16, EA_T_F16, EA_T_F32, EA_T_I32, EA_T_I64, _i64, _P,
@@ -171,9 +176,9 @@ class Embedding(_Handle):
 
     def lookup(self, tokens, weight, out=None, dtype=None):
         """scale * weight[tokens], of shape tokens.shape + (dim,), in `dtype` (default: weight's) or into `out`."""
-        ids = self._tokens(tokens)
+        ids, given = self._tokens(tokens), out is not None
         self._table(weight, "weight")
-        if out is None:
+        if not given:
             out = torch.empty((*tokens.shape, self.dim), dtype=dtype or weight.dtype, device=self.device)
             self._c.row_outer, self._c.row_inner = self._c.inner * self.dim, self.dim
             self._row_type(out.dtype, "out")
@@ -182,13 +187,15 @@ class Embedding(_Handle):
             if dtype is not None and out.dtype != dtype:
                 _refuse(f"out is {out.dtype}, not {dtype}")
         self._call(self._L.ea_embed_lookup, (self._c, ids.data_ptr(), weight.data_ptr(), out.data_ptr()), (ids, weight, out))
+        if given:
+            increment_version(out)
         return out
 
     def grad(self, tokens, dy, out=None, accumulate: bool = False, dtype=torch.float32):
         """The gradient of weight, of shape (vocab, dim), from dy = the gradient of lookup's result, into `out`
         or, with accumulate, added to it."""
-        ids = self._tokens(tokens)
-        if out is None:
+        ids, given = self._tokens(tokens), out is not None
+        if not given:
             if accumulate:
                 _refuse("accumulate needs out")
             out = torch.empty(self._shape, dtype=dtype, device=self.device)
@@ -197,6 +204,8 @@ class Embedding(_Handle):
             dy = dy.contiguous()
         self._rows(dy, tokens, "dy")
         self._call(self._L.ea_embed_grad, (self._c, ids.data_ptr(), dy.data_ptr(), out.data_ptr(), int(accumulate)), (ids, dy, out))
+        if given:
+            increment_version(out)
         return out
 
     def sync(self) -> None:
@@ -247,14 +256,16 @@ class GradNorm(_Handle):
     def __call__(self, grads, max_norm: float = float("inf"), grad_scale: float = 1.0, out=None):
         """A float32 tensor of two: the norm N of grad_scale * grads, and grad_scale * min(1, max_norm / N), NaN where
         N is not finite.  AdamW.step takes it as `clip`."""
-        g = _grad_list(self, grads)
-        if out is None:
+        g, given = _grad_list(self, grads), out is not None
+        if not given:
             out = torch.empty(2, dtype=torch.float32, device=self.device)
         else:
             self._on_device(out, "out")
             if out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
                 _refuse("out is two contiguous float32 values")
         self._call(self._L.ea_grad_norm, (g._ptrs, grad_scale, max_norm, out.data_ptr()), (out,), g.tensors)
+        if given:
+            increment_version(out)
         return out
 
 
@@ -328,6 +339,8 @@ class AdamW(_Handle):
         self._open(config, stream, device)
         self._touched = (*self.params.tensors, *[c for c in self.copies if c is not None],
                          *[t for v in self.states.values() for t in v])
+        # one tensor for each count of modifications (pieces of a flat vector have one between them)
+        self._modified = tuple({id(b): b for b in (t if t._base is None else t._base for t in self._touched)}.values())
 
     def step(self, grads, lr: float, clip=None) -> None:
         """One step.  clip: GradNorm's result (the gradients are multiplied by its second value, on the device; a
@@ -339,6 +352,7 @@ class AdamW(_Handle):
                 _refuse("clip is two contiguous float32 values")
         self._call(self._L.ea_adamw_step, (g._ptrs, lr, None if clip is None else clip.data_ptr()),
                    self._touched, g.tensors, () if clip is None else (clip,))
+        increment_version(self._modified)
 
     @property
     def t(self) -> int:

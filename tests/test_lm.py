@@ -180,7 +180,7 @@ def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
     seen("ea_embed_grad", 3, lambda: table.grad(ids, torch.ones(2, 2)))
     norm = handle(lm.GradNorm, sizes=[8], dtype=torch.float32)
     seen("ea_grad_norm", 2, lambda: norm([g]))
-    opt = handle(lm.AdamW, sizes=[8], dtype=torch.float32, _touched=(g, g, g))
+    opt = handle(lm.AdamW, sizes=[8], dtype=torch.float32, _touched=(g, g, g), _modified=(g,))
     seen("ea_adamw_step", 5, lambda: opt.step([g], lr=1e-3, clip=torch.ones(2)))
     log.clear()
     table.sync()

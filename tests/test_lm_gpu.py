@@ -648,6 +648,39 @@ def test_another_current_stream():
     assert all(torch.equal(x, y) for x, y in zip(run(None), run(torch.cuda.Stream())))
 
 
+def test_written_tensors_count_as_modified():
+    """A backward pass that saved what a call then writes to is refused, as after torch's own operations in place."""
+    vocab, dim = 10, 8
+    w, ids, dy = _randn(vocab, dim, seed=77), torch.tensor([1, 2], device="cuda"), _randn(2, dim, seed=78)
+    table, norm = ea.Embedding(vocab, dim, 2), ea.GradNorm([5])
+    p, c, g = torch.nn.Parameter(_randn(5, seed=79)), torch.zeros(5, device="cuda", dtype=BF16), _randn(5, seed=80)
+    opt = ea.AdamW([p], copies=[c], grad_dtype=F32)
+    row, dw, out = torch.empty(2, dim, device="cuda"), torch.zeros(vocab, dim, device="cuda"), torch.empty(2, device="cuda")
+    flat = torch.zeros(9, device="cuda")
+    pieces = ea.AdamW(list(flat.split([4, 5])), state_bits=8)
+    for f, written in ((lambda: opt.step([g], lr=1e-3), (p, c, opt.states["m"][0])),
+                       (lambda: pieces.step([g[:4], g], lr=1e-3), (flat, pieces.params.tensors[1])),
+                       (lambda: table.lookup(ids, w, out=row), (row,)),
+                       (lambda: table.grad(ids, dy, out=dw, accumulate=True), (dw,)), (lambda: norm([g], out=out), (out,))):
+        for t in written:
+            x = torch.ones_like(t, requires_grad=True)
+            loss = (x * t).sum()
+            f()
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+    with torch.inference_mode():                             # tensors that have no count
+        dw = torch.zeros(vocab, dim, device="cuda")
+        assert torch.equal(table.grad(ids, dy, out=dw), table.grad(ids, dy))
+        q = torch.zeros(5, device="cuda")
+        ea.AdamW([q]).step([g], lr=1e-3)
+
+
+def test_a_lookup_has_no_graph():
+    w = torch.nn.Parameter(_randn(10, 8, seed=81))
+    y = ea.Embedding(10, 8, 2).lookup(torch.tensor([1, 2], device="cuda"), w)
+    assert not y.requires_grad and torch.equal(y, w.detach()[[1, 2]])
+
+
 def test_graph_replays_count_steps():
     vocab, dim, n = 500, 32, 600
     ids, dy, p = _tokens((n,), vocab, 74), _randn(n, dim, seed=75), _randn(vocab * dim, seed=76)
