@@ -39,6 +39,11 @@ def _refuse(msg: str, status: int = EA_E_INVAL):
     raise EAError(status, msg)
 
 
+def _need_cuda(device) -> None:
+    if device.type != "cuda":
+        _refuse(f"the device is {device}: these operators run on CUDA devices")
+
+
 class _Handle:
     """A library handle with its workspace, on one stream of one device."""
 
@@ -46,8 +51,7 @@ class _Handle:
 
     def _open(self, config, stream, device) -> None:
         self.device = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
-        if self.device.type != "cuda":
-            _refuse(f"the device is {self.device}: these operators run on CUDA devices")
+        _need_cuda(self.device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
@@ -223,7 +227,9 @@ class TensorList:
             _refuse("no tensors")
         first = self.tensors[0]
         for i, t in enumerate(self.tensors):
-            if not isinstance(t, torch.Tensor) or t.dtype != first.dtype or t.device != first.device or not t.is_contiguous():
+            if not isinstance(t, torch.Tensor):
+                _refuse(f"tensor {i} is a {type(t).__name__}")
+            if t.dtype != first.dtype or t.device != first.device or not t.is_contiguous():
                 _refuse(f"tensor {i} is not a contiguous tensor of {first.dtype} on {first.device}")
         self.dtype, self.device = first.dtype, first.device
         self.sizes = [t.numel() for t in self.tensors]
@@ -289,7 +295,8 @@ class AdamW(_Handle):
         self.dtype = grad_dtype or self.param_dtype
         if self.param_dtype not in _TYPE or self.dtype not in _TYPE:
             _refuse(f"parameters and gradients are float32, bfloat16 or float16, not {self.param_dtype} and {self.dtype}")
-        device, stream = self.params.device, stream
+        device = self.params.device
+        _need_cuda(device)
         names = {32: ("m", "v"), 8: ("m", "r", "m_scale", "r_scale")}.get(state_bits)
         if names is None:
             _refuse("state_bits is 32 or 8")
@@ -304,13 +311,15 @@ class AdamW(_Handle):
         self.states = {k: list(v) for k, v in states.items()}
         for k in names:
             for i, t in enumerate(self.states[k]):
-                if t.dtype != dtypes[k] or t.device != device or not t.is_contiguous():
+                if not isinstance(t, torch.Tensor) or t.dtype != dtypes[k] or t.device != device or not t.is_contiguous():
                     _refuse(f"{k}[{i}] is not a contiguous tensor of {dtypes[k]} on {device}")
             if [t.numel() for t in self.states[k]] != lengths[k]:
                 _refuse(f"{k} does not have the sizes of the parameters' states")
         self.copies = [None] * n if copies is None else list(copies)
         if len(self.copies) != n:
             _refuse(f"{len(self.copies)} copies for {n} tensors")
+        if not all(c is None or isinstance(c, torch.Tensor) for c in self.copies):
+            _refuse("a copy is not a tensor")
         types = {c.dtype for c in self.copies if c is not None}
         if len(types) > 1 or types - {torch.bfloat16, torch.float16}:
             _refuse("copies are all bfloat16 or all float16")

@@ -185,3 +185,17 @@ def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
     log.clear()
     table.sync()
     assert opt.t == 0 and log == [("ea_embed_sync_status", 1), ("ea_adamw_step_index", 1)] and device[0] == here
+
+
+def test_refusals_of_what_is_not_a_cuda_tensor(ea_lib):
+    """Host tensors and things that are no tensors are refused as every other argument is, by EAError."""
+    import torch
+
+    p = torch.zeros(3)
+    for f in (lambda: ea.AdamW([p]), lambda: ea.AdamW([p], state_bits=8), lambda: ea.AdamW([1.0]), lambda: ea.AdamW([p, None]),
+              lambda: ea.TensorList([None]), lambda: ea.TensorList(["a", p]), lambda: ea.GradNorm([3], device="cpu"),
+              lambda: ea.Embedding(3, 4, 5, device="cpu"), lambda: ea.AdamW([p], copies=[1.0]),
+              lambda: ea.AdamW([p], states={"m": [1.0], "v": [1.0]})):
+        with pytest.raises(ea.EAError) as ex:
+            f()
+        assert ex.value.status == ea.EA_E_INVAL and str(ex.value)

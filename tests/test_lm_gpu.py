@@ -765,3 +765,11 @@ def test_refusals():
     no(ea.EA_E_INVAL, ea.AdamW, [])
     no(ea.EA_E_INVAL, ea.AdamW, [p, _randn(4, seed=1, dtype=BF16)])
     assert torch.equal(table.lookup(ids, w), w[ids])
+
+
+def test_refusals_of_copies_and_states_that_are_no_tensors():
+    p = _randn(10, seed=84)
+    for bad in (dict(copies=[1.0]), dict(states={"m": [1.0], "v": [p.clone()]}), dict(states={"m": [p.clone()], "v": [None]})):
+        with pytest.raises(ea.EAError) as ex:
+            ea.AdamW([p], **bad)
+        assert ex.value.status == ea.EA_E_INVAL and str(ex.value)
