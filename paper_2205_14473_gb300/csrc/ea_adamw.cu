@@ -124,24 +124,17 @@ struct alignas(4 * sizeof(T)) Quad {
     T x[4];
 };
 
-// Those from p on, where `whole`, else the ones below n (the others are 0).
+// Those from p on below n; the others are 0.
 template <class T>
-__device__ __forceinline__ Quad<T> load_quad(const T *p, int n, bool whole)
+__device__ __forceinline__ Quad<T> load_quad(const T *p, int n)
 {
-    using Word = typename std::conditional<sizeof(T) == 4, uint4, typename std::conditional<sizeof(T) == 2, uint2, uint32_t>::type>::type;
-    union {
-        Word w;
-        Quad<T> q;
-    } v{};
-    if (whole) {
-        v.w = *reinterpret_cast<const Word *>(p);
-    } else {
+    Quad<T> q{};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) v.q.x[i] = p[i];
-    }
-    return v.q;
+    for (int i = 0; i < 4; ++i)
+        if (i < n) q.x[i] = p[i];
+    return q;
 }
+// Those from p on, where `whole`, else the ones below n.
 template <class T>
 __device__ __forceinline__ void store_quad(T *p, int n, bool whole, const Quad<T> &q)
 {
@@ -337,10 +330,10 @@ __device__ __forceinline__ void adam_load(const AdamPlace<P, G, C, S> &at, int n
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        b.p[h] = load_quad(at.p + 128 * h, n - 128 * h, false);
-        b.g[h] = load_quad(at.g + 128 * h, n - 128 * h, false);
-        b.m[h] = load_quad(at.m + 128 * h, n - 128 * h, false);
-        b.v[h] = load_quad(at.v + 128 * h, n - 128 * h, false);
+        b.p[h] = load_quad(at.p + 128 * h, n - 128 * h);
+        b.g[h] = load_quad(at.g + 128 * h, n - 128 * h);
+        b.m[h] = load_quad(at.m + 128 * h, n - 128 * h);
+        b.v[h] = load_quad(at.v + 128 * h, n - 128 * h);
     }
 }
 

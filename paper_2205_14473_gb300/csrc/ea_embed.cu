@@ -15,7 +15,6 @@
 namespace ea {
 
 constexpr uint32_t kStatusToken = 4u;  // a token outside the table
-constexpr int kEmbedThreads = 256;
 
 struct EmbedArgs {
     int64_t n;                   // tokens
