@@ -4,7 +4,7 @@
  * by which gradients are clipped, and an AdamW step over many tensors with moments in 32 or in 8 bits.
  *
  * As in ea.h: every call is asynchronous on the stream given to the init call and never synchronizes,
- * except the *_sync_status calls and ea_adamw_step_index; the library allocates no device memory, the
+ * except the *_sync_status and *_selftest_* calls and ea_adamw_step_index; the library allocates no device memory, the
  * caller passes one workspace (256-byte aligned, *_workspace_bytes() bytes, untouched by anyone else until
  * the destroy call) and owns it, the stream and every tensor.  A handle belongs to the device that was
  * current at its init call, and to one host thread at a time.  All calls but the init and synchronizing ones
@@ -155,6 +155,10 @@ int ea_adamw_step(ea_adamw *h, const void *const *grads, float lr, const float *
 /* Steps taken, skipped ones not counted (synchronizes the stream). */
 int ea_adamw_step_index(ea_adamw *h, int64_t *t);
 int ea_adamw_destroy(ea_adamw *h);
+
+/* Self-test of the 8-bit step's square root against the correctly rounded one, for every binary32 value below 2^60:
+ * the number of values for which they differ.  Synchronizes the stream. */
+int ea_adamw_selftest_sqrt(void *stream, uint64_t *unequal);
 
 #ifdef __cplusplus
 }

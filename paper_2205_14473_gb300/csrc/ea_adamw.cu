@@ -81,10 +81,12 @@ __device__ __forceinline__ float recip_normal(float x)
     return r;
 }
 
+constexpr uint32_t kLiftBelow = (127u + 60u) << 23;  // 2^60: the values that sqrt_lifted is used for
+
 // The square roots of 2^64 v for two v, zero or at least 2^-149, rounded to nearest: from y ~ 1 / sqrt(x), the
 // remainder x - g^2 of g = x y, exact in a fused operation, corrects g to its last bit (Markstein, "Computation of
 // elementary functions on the IBM RISC System/6000 processor", 1990; without the refinement of y and g that the paper
-// has in between).  Compared with sqrtf for every mantissa in both parities of the exponent, and for subnormal v: equal.
+// has in between).  Equal to sqrtf, times 2^32, for every v below 2^60 (ea_adamw_selftest_sqrt).
 // It is a third of the call's instructions, and no branch stands between a lane's coordinates.
 __device__ __forceinline__ F2 sqrt_lifted(F2 v, F2 none)
 {
@@ -427,7 +429,7 @@ __device__ __forceinline__ void adam_block(const AdamArgs &a, const AdamStep &s,
         vmax = __reduce_max_sync(0xffffffffu, vmax);
     }
     // roots are taken 2^32 times as large, so that subnormal values have one, where none overflows
-    const bool lift = finite && vmax < (127u + 60u) << 23;
+    const bool lift = finite && vmax < kLiftBelow;
     const F2 unit = both(lift ? 0x1p-32f : 1.0f);
     const int km = scale_exponent(mmax), kv = scale_exponent(bits(__fsqrt_rn(__uint_as_float(vmax))));
     const F2 im = both(power_of_two(-km)), iv = mul2(both(power_of_two(-kv)), unit, s.none);
@@ -569,6 +571,21 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtasPerSm)
         }
     }
 }
+
+// Counts the v in [0, 2^kLiftBelow) whose sqrt_lifted is not sqrtf's result times 2^32: all of them, two at a time.
+constexpr int kSqrtCtas = 152 * 8, kSqrtThreads = 256;
+__global__ void __launch_bounds__(kSqrtThreads) sqrt_selftest_kernel(float minus_zero, unsigned long long *unequal)
+{
+    unsigned long long bad = 0;
+    for (uint32_t i = (blockIdx.x * kSqrtThreads + threadIdx.x) * 2; i < kLiftBelow; i += gridDim.x * kSqrtThreads * 2) {
+        const float v[2] = {__uint_as_float(i), __uint_as_float(i + 1)};
+        float root[2];
+        unpack2(sqrt_lifted(pack2(v[0], v[1]), both(minus_zero)), root[0], root[1]);
+        for (int k = 0; k < 2; ++k) bad += bits(root[k]) != bits(__fmul_rn(__fsqrt_rn(v[k]), 0x1p32f));
+    }
+    if (bad) atomicAdd(unequal, bad);
+}
+__device__ unsigned long long g_sqrt_unequal;
 
 }  // namespace ea
 
@@ -791,6 +808,25 @@ int ea_adamw_step_index(ea_adamw *h, int64_t *t)
     if (!h || !t) return lm_fail(EA_E_INVAL, "NULL argument");
     int r = lm_cuda(cudaMemcpyAsync(t, &h->d_state->t, 8, cudaMemcpyDeviceToHost, h->stream), "step read");
     if (r == EA_OK) r = lm_cuda(cudaStreamSynchronize(h->stream), "stream synchronize");
+    return r;
+}
+
+int ea_adamw_selftest_sqrt(void *stream, uint64_t *unequal)
+{
+    if (!unequal) return lm_fail(EA_E_INVAL, "unequal is NULL");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const unsigned long long zero = 0;
+    unsigned long long n = 0;
+    void *at = nullptr;
+    int r = lm_cuda(cudaGetSymbolAddress(&at, g_sqrt_unequal), "counter");
+    if (r == EA_OK) r = lm_cuda(cudaMemcpyAsync(at, &zero, sizeof zero, cudaMemcpyHostToDevice, s), "counter clear");
+    if (r == EA_OK) {
+        sqrt_selftest_kernel<<<kSqrtCtas, kSqrtThreads, 0, s>>>(-0.0f, static_cast<unsigned long long *>(at));
+        r = lm_cuda(cudaGetLastError(), "launch");
+    }
+    if (r == EA_OK) r = lm_cuda(cudaMemcpyAsync(&n, at, sizeof n, cudaMemcpyDeviceToHost, s), "counter read");
+    if (r == EA_OK) r = lm_cuda(cudaStreamSynchronize(s), "stream synchronize");
+    if (r == EA_OK) *unequal = n;
     return r;
 }
 

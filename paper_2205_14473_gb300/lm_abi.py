@@ -47,7 +47,9 @@ def declare(L) -> None:
     L.ea_grad_norm.argtypes = [_P, _P, _f32, _f32, _P]
     L.ea_adamw_step.argtypes = [_P, _P, _f32, _P]
     L.ea_adamw_step_index.argtypes = [_P, ctypes.POINTER(_i64)]
+    L.ea_adamw_selftest_sqrt.argtypes = [_P, ctypes.POINTER(ctypes.c_uint64)]
 
 
 EXPORTED = [f"{n}_{f}" for n in ("ea_embed", "ea_grad_norm", "ea_adamw") for f in ("workspace_bytes", "init", "destroy")] + [
-    "ea_embed_lookup", "ea_embed_grad", "ea_embed_sync_status", "ea_grad_norm", "ea_adamw_step", "ea_adamw_step_index"]
+    "ea_embed_lookup", "ea_embed_grad", "ea_embed_sync_status", "ea_grad_norm", "ea_adamw_step", "ea_adamw_step_index",
+    "ea_adamw_selftest_sqrt"]

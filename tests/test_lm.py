@@ -199,3 +199,23 @@ def test_refusals_of_what_is_not_a_cuda_tensor(ea_lib):
         with pytest.raises(ea.EAError) as ex:
             f()
         assert ex.value.status == ea.EA_E_INVAL and str(ex.value)
+
+
+def test_selftest_refuses_null(ea_lib):
+    assert ea_lib.ea_adamw_selftest_sqrt(None, None) == ea.EA_E_INVAL
+
+
+@pytest.mark.parametrize("kind,config,edge,past", [
+    ("ea_embed", _embed, dict(vocab=2 ** 31 - 2), dict(vocab=2 ** 31 - 1)), ("ea_embed", _embed, dict(dim=2 ** 20), dict(dim=2 ** 20 + 1)),
+    ("ea_embed", _embed, dict(max_tokens=2 ** 30), dict(max_tokens=2 ** 30 + 1)), ("ea_embed", _embed, dict(max_tokens=0), dict(max_tokens=-1)),
+    ("ea_embed", _embed, dict(padding=99), dict(padding=100)), ("ea_embed", _embed, dict(padding=-1), dict(padding=-2)),
+    ("ea_grad_norm", _norm, dict(sizes=(2 ** 40,)), dict(sizes=(2 ** 40 + 1,))),
+    ("ea_grad_norm", _norm, dict(sizes=(0,) * 2 ** 20), dict(sizes=(0,) * (2 ** 20 + 1))),
+    ("ea_adamw", _adamw, dict(tensor=dict(size=2 ** 40)), dict(tensor=dict(size=2 ** 40 + 1))),
+    ("ea_adamw", _adamw, dict(beta1=0.0), dict(beta1=-1e-45)), ("ea_adamw", _adamw, dict(eps=1.1e-30), dict(eps=0.9e-30)),
+    ("ea_adamw", _adamw, dict(step=2 ** 32 - 1), dict(step=2 ** 32)), ("ea_adamw", _adamw, dict(beta2=1 - 2.0 ** -24), dict(beta2=1.0)),
+])
+def test_limits_on_both_sides(ea_lib, kind, config, edge, past):
+    n, query = ctypes.c_size_t(0), getattr(ea_lib, kind + "_workspace_bytes")
+    assert query(config(**edge), ctypes.byref(n)) == ea.EA_OK and n.value >= 256
+    assert query(config(**past), ctypes.byref(n)) == ea.EA_E_INVAL

@@ -522,6 +522,16 @@ def test_adamw_8_states_are_binary32(ptype, gtype, mag):
             assert torch.equal(got, q), (k, t, int((got != q).sum()))
 
 
+def test_adamw_8_square_root():
+    """The 8-bit step's square root is the correctly rounded one for every value that it is taken of: a root of a block's
+    maximum that came out one unit too large would have no code."""
+    import ctypes
+
+    unequal = ctypes.c_uint64(1)
+    assert ea.lib().ea_adamw_selftest_sqrt(torch.cuda.current_stream().cuda_stream, ctypes.byref(unequal)) == ea.EA_OK
+    assert unequal.value == 0
+
+
 def test_adamw_8_rounding_is_unbiased():
     """The mean of the held first moment over many coordinates with the same value: within 6 standard deviations
     of that value (a deviation is at most half the grid's spacing)."""
