@@ -632,6 +632,57 @@ def test_adamw_agrees_with_torch():
     _inside(_np(p), _np(q.data), np.abs(_np(q.data)) * 20 * 2 * U + 20 * 0.33 * 20 * 10 * U, "p")
 
 
+# ------------------------------------------------------------------------- offsets beyond 2^31 elements
+
+FAR = 2 ** 31 + 4096
+
+
+def test_far_rows_of_tables_and_outputs():
+    """A table of more than 2^31 elements, and rows that lie as far apart."""
+    dim = 1024
+    vocab = FAR // dim
+    w = torch.empty(vocab, dim, device="cuda", dtype=BF16)
+    ids = torch.tensor([[vocab - 1, 0, vocab - 2], [vocab // 2, vocab - 1, 1]], device="cuda")
+    rows = _randn(2, 3, dim, seed=100, dtype=BF16)
+    w[ids] = rows
+    rows = w[ids]
+    table, flat = ea.Embedding(vocab, dim, 6), torch.empty(FAR + 3 * dim, device="cuda", dtype=BF16)
+    assert torch.equal(table.lookup(ids, w), rows)
+    far = flat.as_strided((2, 3, dim), (2 ** 31, dim, 1))
+    assert torch.equal(table.lookup(ids, w, out=far), rows)
+    narrow, few = ea.Embedding(FAR // 64, 64, 6), ids * 16
+    assert torch.equal(narrow.lookup(few, w.view(-1, 64)), w.view(-1, 64)[few])
+    # the gradient of that table, from rows that lie far apart
+    w.fill_(float("nan"))
+    table.grad(ids, far, out=w)
+    want = far.reshape(6, dim).clone()
+    want[0] = (want[0].float() + want[4].float()).to(BF16)
+    got = w[ids].view(6, dim)
+    assert torch.equal(got[[0, 1, 2, 3, 5]], want[[0, 1, 2, 3, 5]])
+    assert int(torch.count_nonzero(w)) == int(torch.count_nonzero(got[[0, 1, 2, 3, 5]]))
+
+
+@pytest.mark.parametrize("off", [0, 1])
+def test_far_coordinates_of_the_norm(off):
+    x = torch.zeros(FAR + off, device="cuda", dtype=BF16)[off:]
+    x[:1000], x[-1000:] = _randn(1000, seed=101, dtype=BF16), _randn(1000, seed=102, dtype=BF16)
+    _check_norm(ea.GradNorm([FAR], BF16)([x], max_norm=1.0), [torch.cat([x[:1000], x[-1000:]])], 1.0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_far_coordinates_of_adamw(bits):
+    """The first step moves a coordinate by lr g / (|g| + eps), wherever it lies, and nothing else: with eps far below
+    |g|, by lr within the step's roundings (and the parameter's) of either sign."""
+    p, g = torch.zeros(FAR, device="cuda", dtype=BF16), torch.zeros(FAR, device="cuda", dtype=BF16)
+    for part in (slice(0, 1000), slice(2 ** 31 - 500, 2 ** 31 + 500), slice(FAR - 1000, FAR)):
+        g[part] = torch.sign(_randn(1000, seed=103))
+    opt = ea.AdamW([p], state_bits=bits, weight_decay=0.1)
+    opt.step([g], lr=0.5)
+    assert int(torch.count_nonzero(p)) == 3000 and int(torch.count_nonzero(opt.states["m"][0].view(torch.uint8))) >= 3000
+    for part in (slice(0, 1000), slice(2 ** 31 - 500, 2 ** 31 + 500), slice(FAR - 1000, FAR)):
+        _inside(_np(p[part]), -0.5 * _np(g[part]), 0.5 * (20 * U + 1e-6 + HALF_ULP[BF16]), "p")
+
+
 # ------------------------------------------------------------------------- streams, graphs, refusals
 
 def test_another_current_stream():
