@@ -89,7 +89,8 @@ int ea_grad_norm_init(const ea_grad_norm_config *cfg, void *workspace, size_t wo
 /* out[0] = N = |grad_scale| * the 2-norm of all gradients together, out[1] = grad_scale * min(1, max_norm / N)
  * (grad_scale where N = 0), the factor that takes gradients held as multiples 1 / grad_scale of themselves to
  * clipped ones.  Where N is not finite (an infinite or NaN gradient), out[1] is NaN, which ea_adamw_step takes
- * as a step to be skipped.  Values of any magnitude count: N overflows only where it exceeds binary32.
+ * as a step to be skipped; a gradient multiplied by it would make a round's moments and residuals NaN for good.
+ * Values of any magnitude count: N overflows only where it exceeds binary32.
  * grads: n_tensors device addresses in host memory, read before this returns, each aligned to its element
  * (those of empty tensors are ignored).  grad_scale: finite, not 0.  max_norm: >= 0, may be infinite.  out:
  * device, two binary32.  The same bits on every run. */
@@ -140,14 +141,16 @@ int ea_adamw_init(const ea_adamw_config *cfg, void *workspace, size_t workspace_
  *   p <- p - (l weight_decay p + a m / (sqrt(v) + e)),  l = lr lr_scale,
  *   a = l sqrt(1 - beta2^t) / (1 - beta1^t),  e = eps sqrt(1 - beta2^t)
  * which is lr_scale lr ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p), in binary32
- * with one rounding per operation (the quotient to within two units in the last place).  p is rounded to the parameters' type, and the unrounded binary32 p to the
- * copy's.  With 8-bit states the step uses m and v as just formed; then each is scaled by the smallest power
- * of two (>= 2^-126) that brings its block's largest finite magnitude to at most 448 and rounded to e4m3
- * stochastically (up with the probability of the remainder, in 2^-16): coordinate j of tensor i draws word
+ * with one rounding per operation, but that the quotient is m times a reciprocal within one unit in the last place
+ * (three units together; the reciprocal of a denominator above 2^126 is 0) and a's product is fused with the sum
+ * after it.  p is rounded to the parameters' type, and the unrounded binary32 p to the copy's.  With 8-bit states
+ * the step uses m and v as just formed; then each is scaled by the smallest power of two (>= 2^-126) that brings
+ * its block's largest finite magnitude to at most 448 and rounded to e4m3 stochastically (up with the probability of the remainder, in 2^-16): coordinate j of tensor i draws word
  * j mod 4 of Philox4x32-10 at the counter (j/4 low, j/4 high, i, t - 1) under the key seed, its low half for
  * m and its high half for v; a nonzero root is never rounded to zero, and a value that is not finite is held
  * as NaN.
- * grads: n_tensors device addresses in host memory, as in ea_grad_norm.  lr: finite.  clip: device, what
+ * grads: n_tensors device addresses in host memory, as in ea_grad_norm.  lr: finite; an argument of the launches, so a
+ * captured step is replayed with the lr of its capture (and with the device's own t and clip).  clip: device, what
  * ea_grad_norm writes, or NULL for a factor of 1.  Where clip[1] is NaN the step is skipped: nothing is
  * written and t does not advance. */
 int ea_adamw_step(ea_adamw *h, const void *const *grads, float lr, const float *clip);

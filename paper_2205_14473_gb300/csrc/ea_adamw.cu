@@ -3,12 +3,14 @@
 // moments in binary32 or in 8 bits.
 //
 // Measured on one GB300 (us a step, GB/s of the bytes that it cannot do without, against a copy's 6,800):
-//   354 M binary32 parameters, bfloat16 gradients and copy, 32-bit states  1,512 to 1,540 us, 6,430 GB/s: HBM
+//   354 M binary32 parameters, bfloat16 gradients and copy, 32-bit states  1,506 to 1,540 us, 6,580 GB/s: HBM
 //   ResNet-18's 62 tensors, all binary32                                   60 us, 5,440 GB/s: launch and first loads
-//   108 M bfloat16 parameters and gradients, 8-bit states                  337 us, 3,240 GB/s: instruction issue
-// An 8-bit step is about 70 instructions per coordinate (ten rounds of the generator for four coordinates are ten of
-// them, a fifth of the time); with the arithmetic taken out the same kernel takes 334 us where each block's scales go
-// by themselves, and 185 where eight blocks' go together, but that costs the full step more than it saves.
+//   108 M bfloat16 parameters and gradients, 8-bit states                  336 us, 3,250 GB/s: two limits, below
+// An 8-bit step is 80 instructions per coordinate at 14 warps per SM: 65% of the issue slots, the ALU 49% busy, DRAM at a
+// third of its rate.  Nine of the generator's ten rounds taken out save 45 us.  But the accesses alone, in the same order
+// and with the arithmetic taken out, take 334 us too, where each block's two scales are loaded one block ahead and stored
+// by themselves: fewer instructions alone would not make it faster.  With eight blocks' scales moved together the accesses
+// take 185 us and the whole step 353.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -73,7 +75,8 @@ __device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
 // after it would be merged into one rounding, whatever their PTX says.
 __device__ __forceinline__ F2 mul2(F2 a, F2 b, F2 minus_zero) { return fma2(a, b, minus_zero); }
 
-// Within 2^-23 relative of the reciprocal of a normal number.
+// Within 2^-23 relative of the reciprocal of a normal number (0 for one above 2^126).  With a correctly rounded quotient
+// instead, 8-bit steps of 40 M coordinates take 141 us for 130, 32-bit ones of ResNet-18 61.3 for 59.9.
 __device__ __forceinline__ float recip_normal(float x)
 {
     float r;

@@ -4,8 +4,12 @@
 // Both move rows and do next to no arithmetic.  Measured on one GB300 (us a call, calls one behind another; GB/s of the
 // bytes that a call cannot do without, against a copy's 6,800):
 //   lookup, 16,384 of 50,257 x 1600, 32 to 16 bits   19.2 us, 4,840 GB/s (a plain copy of as many bytes: 25.8 us)
-//   gradient of that batch, 32 bits written          86 us, 4,350 GB/s: the sort and the zero rows (52 us), sums, joins
-//   gradient, 260,096 tokens, 768 wide, half padding 94 us, 3,160 GB/s: six launches of sort (38 us), sums at 7 TB/s (41)
+//     the table off a 16-byte boundary, or 1601 wide 24.8 us
+//   gradient of that batch, 32 bits written          85 us, 4,400 GB/s: the sort and the zero rows (52 us), sums, joins
+//     added to a tied one                            56 us
+//     the table off a 16-byte boundary, or 1601 wide 99 us
+//   gradient, 260,096 tokens, 768 wide, half padding 94 us, 3,140 GB/s: six launches of sort (38 us), sums (41; 4.7 TB/s)
+//     the table off a 16-byte boundary, or 769 wide  143, 159 us
 #include <cooperative_groups.h>
 #include <type_traits>
 
@@ -76,7 +80,8 @@ __device__ __forceinline__ void store_pack(Y *p, Pack<Y, VEC> &x) { move_pack<Y,
 //   rows of kWideRow packs or more: a warp takes a piece of one row, so that its addresses are formed once for all of
 //     its packs; one token's row is still spread over as many warps as it has pieces;
 //   narrower ones: the packs of all tokens are dealt out in order, so that no lane idles.
-// The index arithmetic decides: dealt out in order, 16,384 rows of 400 packs took 23.8 us; a piece per warp takes 19.2.
+// The index arithmetic decides: dealt out in order, 16,384 rows of 400 packs took 23.8 us; a piece per warp takes 19.2.  In
+// 16 bits, dealt out or by pieces: 48 packs 6.4 and 7.0 us, 64 packs 8.2 either way, 96 10.5 and 10.2, 127 14.4 and 12.3.
 
 constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;  // narrow rows
@@ -220,8 +225,15 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256;                 // of one radix pass
 constexpr int kCluster = 8;                  // CTAs that sort together
 constexpr int kMaxItems = 16;                // keys per thread of a sorting CTA
-constexpr int kZeroCtasPerSm = 3;          // that write zero rows beside it
+// CTAs per SM that write zero rows beside it: 16,384 tokens of 50,257 x 1600 85.3 us, with two of them 95.2, with four 85.5;
+// 16-bit rows 1024 wide 47.0, 47.3 and 48.8.
+constexpr int kZeroCtasPerSm = 3;
+// One CTA or a cluster, tokens of 30,522 x 768: overwritten, 1,024 tokens 29.2 and 30.6 us, 2,048 29.4 and 30.7, 4,096 32.9
+// and 32.0; added to what is there, where the sort is all of the first launch, 16.4 each, 20.5 and 17.4, 26.7 and 18.8.
 constexpr int kOneCtaTokens = kSortThreads * 4;
+// A cluster or the longer sorts, tokens of 50,257 x 1024: 16,384 64 and 85 us, 32,768 81 and 91, 40,000 106 and 93, 65,536
+// 139 and 103; added to what is there 46 and 51, 69 and 68, 89 and 73, 110 and 95.  It is as many as a cluster holds; above
+// 32,768, where a CTA's 16 keys per thread leave room for no second one on an SM, the longer sorts would be faster.
 constexpr int kClusterTokens = kSortThreads * kMaxItems * kCluster;
 constexpr int kTileItems = 2;                // keys per thread of a tile of the longer sorts
 constexpr int kTile1 = kSortThreads * kTileItems;
@@ -769,6 +781,7 @@ int64_t most_chunks(int64_t dim)
 }
 
 // Entries per chunk, no fewer than kMinChunk (a chunk may write two partial sums, as many bytes as 4 rows in 16 bits).
+// With 4, 8 and 16: 384 tokens x 768 in 32 bits 12.4, 12.4 and 15.1 us; 2,000 x 1600 in 16 bits 24.9, 21.0 and 22.6.
 int64_t chunk_length(int64_t n, int64_t dim) { return std::max<int64_t>(kMinChunk, over(n, most_chunks(dim))); }
 
 struct EmbedLayout {

@@ -353,7 +353,7 @@ class AdamW(_Handle):
 
     def step(self, grads, lr: float, clip=None) -> None:
         """One step.  clip: GradNorm's result (the gradients are multiplied by its second value, on the device; a
-        step whose factor is NaN is skipped), or None."""
+        step whose factor is NaN is skipped), or None.  A step in a CUDA graph keeps the lr that it was captured with."""
         g = _grad_list(self, grads)
         if clip is not None:
             self._on_device(clip, "clip")
