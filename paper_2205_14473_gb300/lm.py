@@ -24,7 +24,6 @@ import ctypes
 from itertools import chain
 
 import torch
-from torch.autograd.graph import increment_version
 
 from . import EA_E_INVAL, EAError, _check, lib
 from .lm_abi import (EA_ADAMW_BLOCK, EA_T_BF16, EA_T_F16, EA_T_F32, EA_T_I32, EA_T_I64, _i64, _P,
@@ -48,6 +47,7 @@ class _Handle:
     """A library handle with its workspace, on one stream of one device."""
 
     _kind = ""
+    _only = False  # whether there is no other device, which need not be looked at then
 
     def _open(self, config, stream, device) -> None:
         self.device = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
@@ -57,6 +57,7 @@ class _Handle:
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         self._raw = self.stream.cuda_stream
         self._index = self.device.index
+        self._only = torch.cuda.device_count() == 1
         self._L = lib()
         n, h = ctypes.c_size_t(0), _P()
         _check(getattr(self._L, self._kind + "_workspace_bytes")(ctypes.byref(config), ctypes.byref(n)))
@@ -75,7 +76,7 @@ class _Handle:
 
     def _call(self, f, args, *tensors) -> None:
         """f, a call of the library on this handle that reads or writes `tensors` (lists of them)."""
-        if _C._cuda_getDevice() == self._index and _C._cuda_getCurrentRawStream(self._index) == self._raw:
+        if (self._only or _C._cuda_getDevice() == self._index) and _C._cuda_getCurrentRawStream(self._index) == self._raw:
             status = f(self.h, *args)
         else:
             status = self._call_from_elsewhere(f, args, chain(*tensors))
@@ -192,7 +193,7 @@ class Embedding(_Handle):
                 _refuse(f"out is {out.dtype}, not {dtype}")
         self._call(self._L.ea_embed_lookup, (self._c, ids.data_ptr(), weight.data_ptr(), out.data_ptr()), (ids, weight, out))
         if given:
-            increment_version(out)
+            _C._increment_version((out,))
         return out
 
     def grad(self, tokens, dy, out=None, accumulate: bool = False, dtype=torch.float32):
@@ -209,7 +210,7 @@ class Embedding(_Handle):
         self._rows(dy, tokens, "dy")
         self._call(self._L.ea_embed_grad, (self._c, ids.data_ptr(), dy.data_ptr(), out.data_ptr(), int(accumulate)), (ids, dy, out))
         if given:
-            increment_version(out)
+            _C._increment_version((out,))
         return out
 
     def sync(self) -> None:
@@ -271,7 +272,7 @@ class GradNorm(_Handle):
                 _refuse("out is two contiguous float32 values")
         self._call(self._L.ea_grad_norm, (g._ptrs, grad_scale, max_norm, out.data_ptr()), (out,), g.tensors)
         if given:
-            increment_version(out)
+            _C._increment_version((out,))
         return out
 
 
@@ -361,7 +362,7 @@ class AdamW(_Handle):
                 _refuse("clip is two contiguous float32 values")
         self._call(self._L.ea_adamw_step, (g._ptrs, lr, None if clip is None else clip.data_ptr()),
                    self._touched, g.tensors, () if clip is None else (clip,))
-        increment_version(self._modified)
+        _C._increment_version(self._modified)
 
     @property
     def t(self) -> int:
