@@ -1,0 +1,383 @@
+"""The operators inside a residual block of a language model (include/ea_block.h): layer norm, a gated linear
+recurrence along each sequence and dropout from a counter, each with its gradient.
+
+    norm, scan, drop = LayerNorm(dim, max_rows), GatedScan(dim), Dropout(0.1, seed=7)
+    y, stats = norm.forward(x, weight, bias)
+    ...                                                  # z and v, products of y
+    h, _ = scan.forward(z, v)
+    ...                                                  # o, a product of h
+    out = drop(o, counter, residual=x)                   # x + dropped-out o
+
+    do = drop.grad(dout, counter)
+    dz, dv, _ = scan.grad(dh, z, v, h)
+    dx, dw, db = norm.grad(dy, x, stats, weight, add=dout, dw=True, db=True)
+
+Handles, streams, devices and what counts as modified are as in lm.py, and as there nothing has an autograd graph.
+Tensors are rows of dim values, with any strides between the rows; a tensor that is read and whose rows are not
+contiguous, or that has more than three dimensions and is not contiguous, is copied first.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import EA_E_INVAL, _check  # noqa: F401
+from .block_abi import (ea_dropout_call, ea_dropout_config, ea_layernorm_call, ea_layernorm_config, ea_scan_call,
+                        ea_scan_config)
+from .lm import _C, _TOKEN, _TYPE, _Handle, _refuse
+
+_F32 = torch.float32
+
+
+def _type(dtype, what) -> int:
+    kind = _TYPE.get(dtype)
+    if kind is None:
+        _refuse(f"{what} is float32, bfloat16 or float16, not {dtype}")
+    return kind
+
+
+class _Block(_Handle):
+    """What the three share: checks of rows."""
+
+    def _read(self, t, shape, what):
+        """(t or a copy of it, its outer stride, its inner stride) for a tensor of rows that is read."""
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        if t.shape != shape:
+            _refuse(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+        n = t.dim()
+        if n > 3:
+            t = t.contiguous()
+            return t, 0, t.shape[-1]
+        stride = t.stride()
+        if n and stride[-1] != 1 and t.shape[-1] > 1:
+            t = t.contiguous()
+            stride = t.stride()
+        return t, stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0
+
+    def _written(self, t, shape, dtype, what):
+        """The same for one that is written."""
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        if t.shape != shape:
+            _refuse(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+        if t.dtype != dtype:
+            _refuse(f"{what} is {t.dtype}, not {dtype}")
+        n, stride = t.dim(), t.stride()
+        if n > 3 and not t.is_contiguous() or n and stride[-1] != 1 and t.shape[-1] > 1:
+            _refuse(f"the rows of {what} are not contiguous")
+        return (0, t.shape[-1]) if n > 3 else (stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0)
+
+    def _values(self, t, shape, dtype, what) -> int:
+        """The address of contiguous values of one type."""
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            _refuse(f"{what} is not a contiguous tensor {tuple(shape)} of {dtype}")
+        return t.data_ptr()
+
+
+def _counts(shape):
+    """(outer, inner): rows of a tensor of this shape."""
+    n = len(shape)
+    if n == 3:
+        return shape[0], shape[1]
+    if n == 2:
+        return 1, shape[0]
+    if n == 1:
+        return 1, 1
+    rows = 1
+    for k in shape[:-1]:
+        rows *= k
+    return 1, rows
+
+
+class LayerNorm(_Block):
+    """Layer norm over rows of dim values, up to max_rows of them a call, and its gradient.
+
+    x, dx and the residual's gradient are of one type; y and dy of the same, or of 16 bits where x is float32; weights
+    and their gradients of any of the three types.  Sums and statistics are in 32 bits."""
+
+    _kind = "ea_layernorm"
+
+    def __init__(self, dim: int, max_rows: int, eps: float = 1e-5, stream=None, device=None):
+        self.dim, self.max_rows, self.eps = int(dim), int(max_rows), float(eps)
+        self._c, self._row = ea_layernorm_call(), torch.Size((self.dim,))
+        self._open(ea_layernorm_config(self.dim, self.max_rows, self.eps), stream, device)
+
+    def _x(self, x):
+        if not isinstance(x, torch.Tensor) or x.device != self.device:
+            self._on_device(x, "x")
+        shape, c = x.shape, self._c
+        if not shape or shape[-1] != self.dim:
+            _refuse(f"x is {tuple(shape)}: its rows are not {self.dim} long")
+        c.outer, c.inner = _counts(shape)
+        c.x_type = _type(x.dtype, "x")
+        x, c.x_outer, c.x_inner = self._read(x, shape, "x")
+        return x
+
+    def _weight(self, t, dtype, what):
+        """The address of a weight (None: 0)."""
+        if t is None:
+            return None
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        if dtype is not None and t.dtype != dtype:
+            _refuse(f"{what} is {t.dtype}, the other one {dtype}")
+        self._c.weight_type = _type(t.dtype, what)
+        return self._values(t, self._row, t.dtype, what)
+
+    def forward(self, x, weight=None, bias=None, out=None, dtype=None, stats=None):
+        """(y, stats): y of x's shape in `dtype` (default: x's) or in `out` (which may be x); stats, of shape
+        x.shape[:-1] + (2,), each row's mean and 1 / sqrt(variance + eps), which grad takes, or into `stats`."""
+        given = [t for t in (out, stats) if t is not None]
+        shape, x = getattr(x, "shape", None), self._x(x)
+        c = self._c
+        w = self._weight(weight, None, "weight")
+        b = self._weight(bias, weight.dtype if w is not None else None, "bias")
+        if out is None:
+            out = torch.empty(shape, dtype=dtype or x.dtype, device=self.device)
+            c.y_outer, c.y_inner = (c.inner * self.dim, self.dim)
+        else:
+            c.y_outer, c.y_inner = self._written(out, shape, dtype or getattr(out, "dtype", None), "out")
+        c.y_type = _type(out.dtype, "out")
+        pairs = torch.Size((*shape[:-1], 2))
+        if stats is None:
+            stats = torch.empty(pairs, dtype=_F32, device=self.device)
+        else:
+            self._values(stats, pairs, _F32, "stats")
+        self._call(self._L.ea_layernorm_forward, (c, x.data_ptr(), w, b, out.data_ptr(), stats.data_ptr()),
+                   [t for t in (x, weight, bias, out, stats) if t is not None])
+        if given:
+            _C._increment_version(given)
+        return out, stats
+
+    def _sums(self, t, what):
+        """A weight's gradient: None (not asked for), True (a new one in 32 bits) or a tensor."""
+        if t is None or t is False:
+            return None
+        if t is True:
+            return torch.empty(self._row, dtype=_F32, device=self.device)
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        self._values(t, self._row, t.dtype, what)
+        return t
+
+    def grad(self, dy, x, stats, weight=None, add=None, out=None, dw=None, db=None, accumulate: bool = False):
+        """(dx, dw, db) from dy = the gradient of forward's y, with its x, stats and weight.  add: rows of x's shape and type
+        that are added to dx (the gradient that passes the block by).  dx: into `out` (which may be dy, x or add) or new.
+        dw, db: None (not computed), True (new, in 32 bits) or tensors of one type that are written to or, with accumulate, added
+        to."""
+        given = [t for t in (out, dw, db) if isinstance(t, torch.Tensor)]
+        if accumulate and (dw is True or db is True):
+            _refuse("accumulate needs dw's and db's tensors")
+        shape, x = getattr(x, "shape", None), self._x(x)
+        c = self._c
+        dy, c.y_outer, c.y_inner = self._read(dy, shape, "dy")
+        c.y_type = _type(dy.dtype, "dy")
+        at = self._values(stats, torch.Size((*shape[:-1], 2)), _F32, "stats")
+        w = self._weight(weight, None, "weight")
+        if add is not None:
+            add, c.add_outer, c.add_inner = self._read(add, shape, "add")
+            if add.dtype != x.dtype:
+                _refuse(f"add is {add.dtype}, x {x.dtype}")
+        dw, db = self._sums(dw, "dw"), self._sums(db, "db")
+        if dw is not None and db is not None and dw.dtype != db.dtype:
+            _refuse(f"dw is {dw.dtype}, db {db.dtype}")
+        for t in (dw, db):
+            if t is not None:
+                c.grad_type = _type(t.dtype, "a weight's gradient")
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=self.device)
+            c.dx_outer, c.dx_inner = c.inner * self.dim, self.dim
+        else:
+            c.dx_outer, c.dx_inner = self._written(out, shape, x.dtype, "out")
+        self._call(self._L.ea_layernorm_backward,
+                   (c, dy.data_ptr(), x.data_ptr(), at, w, None if add is None else add.data_ptr(), out.data_ptr(),
+                    None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), int(accumulate)),
+                   [t for t in (dy, x, stats, weight, add, out, dw, db) if t is not None])
+        if given:
+            _C._increment_version(given)
+        return out, dw, db
+
+
+class GatedScan(_Block):
+    """The gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) v_t, f = sigmoid(z), in every column of sequences of rows of
+    dim values, and its gradient.  z, v, h and their gradients are of one type; states are float32, of shape (batch, dim)."""
+
+    _kind = "ea_scan"
+
+    def __init__(self, dim: int, stream=None, device=None):
+        self.dim = int(dim)
+        self._c = ea_scan_call()
+        self._open(ea_scan_config(self.dim), stream, device)
+
+    def _begin(self, z, lengths):
+        if not isinstance(z, torch.Tensor) or z.device != self.device:
+            self._on_device(z, "z")
+        if z.dim() != 3 or z.shape[2] != self.dim:
+            _refuse(f"z is {tuple(z.shape)}, not (batch, length, {self.dim})")
+        c = self._c
+        c.batch, c.length = z.shape[:2]
+        c.type = _type(z.dtype, "z")
+        if lengths is None:
+            return None
+        if not isinstance(lengths, torch.Tensor) or lengths.device != self.device:
+            self._on_device(lengths, "lengths")
+        kind = _TOKEN.get(lengths.dtype)
+        if kind is None:
+            _refuse(f"lengths are int32 or int64, not {lengths.dtype}")
+        c.length_type = kind
+        if lengths.shape != z.shape[:1]:
+            _refuse(f"lengths is {tuple(lengths.shape)}, not ({z.shape[0]},)")
+        return lengths.contiguous()
+
+    def _rows(self, t, like, what):
+        t, outer, inner = self._read(t, like.shape, what)
+        if t.dtype != like.dtype:
+            _refuse(f"{what} is {t.dtype}, z {like.dtype}")
+        return t, outer, inner
+
+    def _state(self, t, what):
+        """(tensor or None, its address or None) of states that are read, or written: None or False, True for a new one."""
+        if t is None or t is False:
+            return None, None
+        shape = torch.Size((self._c.batch, self.dim))
+        if t is True:
+            t = torch.empty(shape, dtype=_F32, device=self.device)
+            return t, t.data_ptr()
+        return t, self._values(t, shape, _F32, what)
+
+    def forward(self, z, v, initial=None, lengths=None, out=None, final=None):
+        """(h, final): h of z's shape and type, into `out` (which may be z or v) or new.  initial: the state before the first
+        row (None: zeros).  lengths: of the sequences (int32 or int64 on the device; None: all rows): rows behind them get zeros,
+        and the state stays as it was.  final: None, True (a new tensor) or a tensor (which may be initial) that receives
+        the states after the last rows.  A length outside [0, length] counts as the nearest of the two, and sync() raises for it."""
+        given = [t for t in (out, final) if isinstance(t, torch.Tensor)]
+        c, n = self._c, self._begin(z, lengths)
+        shape = z.shape
+        z, c.z_batch, c.z_row = self._read(z, shape, "z")
+        v, c.v_batch, c.v_row = self._rows(v, z, "v")
+        initial, first = self._state(initial, "initial")
+        final, last = self._state(final, "final")
+        if out is None:
+            out = torch.empty(shape, dtype=z.dtype, device=self.device)
+            c.h_batch, c.h_row = shape[1] * self.dim, self.dim
+        else:
+            c.h_batch, c.h_row = self._written(out, shape, z.dtype, "out")
+        self._call(self._L.ea_scan_forward,
+                   (c, z.data_ptr(), v.data_ptr(), first, None if n is None else n.data_ptr(), out.data_ptr(), last),
+                   [t for t in (z, v, initial, n, out, final) if t is not None])
+        if given:
+            _C._increment_version(given)
+        return out, final
+
+    def step(self, z, v, state, out=None):
+        """One row each of the sequences: z and v of shape (batch, dim).  Updates state (float32) in place and returns h."""
+        if not isinstance(z, torch.Tensor) or not isinstance(v, torch.Tensor) or z.dim() != 2 or v.dim() != 2:
+            _refuse("z and v are (batch, dim)")
+        if out is not None and (not isinstance(out, torch.Tensor) or out.dim() != 2):
+            _refuse("out is (batch, dim)")
+        if not isinstance(state, torch.Tensor):
+            _refuse("state is not a tensor")
+        h, _ = self.forward(z[:, None], v[:, None], initial=state, out=None if out is None else out[:, None], final=state)
+        return h[:, 0] if out is None else out
+
+    def grad(self, dh, z, v, h, initial=None, lengths=None, d_final=None, dz=None, dv=None, d_initial=None):
+        """(dz, dv, d_initial) from dh = the gradient of forward's h and d_final = that of its final states (None: zeros), with
+        its z, v, h, initial and lengths.  dz (which may be z or dh) and dv (v or dh) are written to, or new.  d_initial: None,
+        True (a new tensor) or a tensor (which may be d_final)."""
+        given = [t for t in (dz, dv, d_initial) if isinstance(t, torch.Tensor)]
+        c, n = self._c, self._begin(z, lengths)
+        shape = z.shape
+        z, c.z_batch, c.z_row = self._read(z, shape, "z")
+        dh, c.dh_batch, c.dh_row = self._rows(dh, z, "dh")
+        v, c.v_batch, c.v_row = self._rows(v, z, "v")
+        h, c.h_batch, c.h_row = self._rows(h, z, "h")
+        initial, first = self._state(initial, "initial")
+        d_final, last = self._state(d_final, "d_final")
+        d_initial, d_first = self._state(d_initial, "d_initial")
+        if dz is None:
+            dz = torch.empty(shape, dtype=z.dtype, device=self.device)
+            c.dz_batch, c.dz_row = shape[1] * self.dim, self.dim
+        else:
+            c.dz_batch, c.dz_row = self._written(dz, shape, z.dtype, "dz")
+        if dv is None:
+            dv = torch.empty(shape, dtype=z.dtype, device=self.device)
+            c.dv_batch, c.dv_row = shape[1] * self.dim, self.dim
+        else:
+            c.dv_batch, c.dv_row = self._written(dv, shape, z.dtype, "dv")
+        self._call(self._L.ea_scan_backward,
+                   (c, dh.data_ptr(), z.data_ptr(), v.data_ptr(), h.data_ptr(), first, None if n is None else n.data_ptr(), last,
+                    dz.data_ptr(), dv.data_ptr(), d_first),
+                   [t for t in (dh, z, v, h, initial, n, d_final, dz, dv, d_initial) if t is not None])
+        if given:
+            _C._increment_version(given)
+        return dz, dv, d_initial
+
+    def sync(self) -> None:
+        with torch.cuda.device(self._index):
+            _check(self._L.ea_scan_sync_status(self.h))
+
+
+class Dropout(_Block):
+    """Dropout whose mask is a function of (seed, counter, element) and is stored nowhere: the gradient draws it again.
+
+    p: the probability that an element is dropped, as the nearest multiple of 2^-16 (self.p).  The mask of a call goes by
+    `counter`, an integer in [0, 2^64) or an int64 tensor of one value on the device, which a captured graph reads at every
+    replay: another one for every call of a training step (step * layers + layer, say).  Use another seed than an optimizer's."""
+
+    _kind = "ea_dropout"
+
+    def __init__(self, p: float, seed: int = 0, stream=None, device=None):
+        self.seed = int(seed)
+        if not 0 <= self.seed < 1 << 64:
+            _refuse("seed is outside [0, 2^64)")
+        self._c = ea_dropout_call()
+        self._open(ea_dropout_config(float(p), self.seed), stream, device)
+        self.p = round(65536 * float(p)) / 65536
+
+    def __call__(self, x, counter, residual=None, out=None, dtype=None):
+        """residual + x / (1 - p) where an element is kept, residual (or 0) where it is not, of x's shape, in `dtype` (default:
+        the residual's type, or x's) or into `out` (which may be x or residual).  x and the result are of one type, or one of them
+        float32; residual is of the result's."""
+        c, given = self._c, out is not None
+        if not isinstance(x, torch.Tensor) or x.device != self.device:
+            self._on_device(x, "x")
+        shape = x.shape
+        if not shape:
+            _refuse("x has no dimensions")
+        c.x_type = _type(x.dtype, "x")
+        c.outer, c.inner = _counts(shape)
+        c.dim = shape[-1]
+        x, c.x_outer, c.x_inner = self._read(x, shape, "x")
+        if dtype is None:
+            dtype = (out if given else residual if residual is not None else x).dtype
+        if residual is not None:
+            residual, c.add_outer, c.add_inner = self._read(residual, shape, "residual")
+            if residual.dtype != dtype:
+                _refuse(f"residual is {residual.dtype}, the result {dtype}")
+        c.y_type = _type(dtype, "the result")
+        if not given:
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+            c.y_outer, c.y_inner = c.inner * c.dim, c.dim
+        else:
+            c.y_outer, c.y_inner = self._written(out, shape, dtype, "out")
+        if isinstance(counter, torch.Tensor):
+            if counter.device != self.device or counter.dtype != torch.int64 or counter.numel() != 1:
+                _refuse(f"counter is an integer or an int64 tensor of one value on {self.device}")
+            number, at = 0, counter.data_ptr()
+        else:
+            number, at = int(counter), None
+            if not 0 <= number < 1 << 64:
+                _refuse("counter is outside [0, 2^64)")
+        self._call(self._L.ea_dropout_apply,
+                   (c, x.data_ptr(), None if residual is None else residual.data_ptr(), number, at, out.data_ptr()),
+                   [t for t in (x, residual, out, counter if at is not None else None) if t is not None])
+        if given:
+            _C._increment_version((out,))
+        return out
+
+    def grad(self, dy, counter, out=None, dtype=None):
+        """The gradient of x from dy = that of the result of the call with this counter, in `dtype` (x's; default: dy's) or into
+        `out`.  The residual's gradient is dy."""
+        return self(dy, counter, out=out, dtype=dtype)

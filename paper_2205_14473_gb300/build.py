@@ -1,4 +1,4 @@
-"""Build libea.so (the C-ABI of include/ea.h and include/ea_lm.h) in-tree for sm_103a with nvcc.
+"""Build libea.so (the C-ABI of include/ea.h, include/ea_lm.h and include/ea_block.h) in-tree for sm_103a with nvcc.
 
 The translation units compile in parallel; the result lands in paper_2205_14473_gb300/_lib/.
 Usage: python -m paper_2205_14473_gb300.build [--verbose]
@@ -16,8 +16,10 @@ CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libea.so")
 LM_SOURCES = ["ea_embed.cu", "ea_norm.cu", "ea_adamw.cu"]  # the units of include/ea_lm.h
-LM_HEADERS = ["ea_lm.cuh"]                                 # read by those alone
-SOURCES = ["ea_api.cu", "ea_worker.cu", "ea_noalloc.cu", "ea_selftest.cu", *LM_SOURCES] + [
+LM_HEADERS = ["ea_lm.cuh"]                                 # read by those and the next alone
+BLOCK_SOURCES = ["ea_layernorm.cu", "ea_scan.cu", "ea_dropout.cu"]  # the units of include/ea_block.h
+BLOCK_HEADERS = ["ea_block.cuh"]                                    # read by those alone
+SOURCES = ["ea_api.cu", "ea_worker.cu", "ea_noalloc.cu", "ea_selftest.cu", *LM_SOURCES, *BLOCK_SOURCES] + [
     f"ea_server_{part}{m}_q{q}.cu" for q in (2, 1, 3, 0) for part in ("", "general_") for m in "sw"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 # binary32 per operation: no FMA contraction, IEEE division and square root, denormals kept
@@ -32,14 +34,16 @@ def _stale(obj: str, deps: list[str]) -> bool:
 
 def build(verbose: bool = False, force: bool = False) -> str:
     os.makedirs(LIBDIR, exist_ok=True)
-    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh")) and f not in LM_HEADERS]
+    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh")) and f not in (*LM_HEADERS, *BLOCK_HEADERS)]
     headers.append(os.path.join(ROOT, "include", "ea.h"))
     lm_headers = [os.path.join(CSRC, f) for f in LM_HEADERS] + [os.path.join(ROOT, "include", "ea_lm.h")]
+    block_headers = [*lm_headers, *[os.path.join(CSRC, f) for f in BLOCK_HEADERS], os.path.join(ROOT, "include", "ea_block.h")]
+    more = {**dict.fromkeys(LM_SOURCES, lm_headers), **dict.fromkeys(BLOCK_SOURCES, block_headers)}
     jobs = []
     for src in SOURCES:
         path = os.path.join(CSRC, src)
         obj = os.path.join(LIBDIR, src.replace(".cu", ".o"))
-        if force or _stale(obj, [path, *headers, *(lm_headers if src in LM_SOURCES else [])]):
+        if force or _stale(obj, [path, *headers, *more.get(src, [])]):
             cmd = [NVCC, *FLAGS, *(["-Xptxas", "-v"] if verbose else []), "-c", path, "-o", obj]
             jobs.append(cmd)
 
