@@ -47,30 +47,6 @@ struct AdamArgs {
     float minus_zero;              // -0 (see mul2)
 };
 
-// Two binary32 values in one 64-bit register: one instruction slot for two operations, each rounded by itself.
-struct F2 {
-    unsigned long long v;
-};
-__device__ __forceinline__ F2 pack2(float a, float b)
-{
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpack2(F2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
-__device__ __forceinline__ F2 add2(F2 a, F2 b)
-{
-    F2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
-{
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
 // a b as a b + (-0), the same value, with a -0 that the compiler does not know: a packed product and the packed sum
 // after it would be merged into one rounding, whatever their PTX says.
 __device__ __forceinline__ F2 mul2(F2 a, F2 b, F2 minus_zero) { return fma2(a, b, minus_zero); }

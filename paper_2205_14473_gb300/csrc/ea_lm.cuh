@@ -35,6 +35,31 @@ __device__ __forceinline__ bf16 from_f32<bf16>(float x) { return __float2bfloat1
 template <>
 __device__ __forceinline__ f16 from_f32<f16>(float x) { return __float2half_rn(x); }
 
+// Two binary32 values in one 64-bit register: one instruction slot for two operations, each rounded by itself.
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 pack2(float a, float b)
+{
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(F2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pack2(a, a); }
+
 inline size_t type_bytes(int32_t type) { return type == EA_T_F32 || type == EA_T_I32 ? 4 : type == EA_T_I64 ? 8 : 2; }
 inline bool is_float_type(int32_t type) { return type == EA_T_F32 || type == EA_T_BF16 || type == EA_T_F16; }
 

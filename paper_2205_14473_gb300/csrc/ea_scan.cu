@@ -12,7 +12,7 @@ namespace ea {
 
 constexpr uint32_t kStatusLength = 8u;  // a length outside [0, length]
 constexpr int kWalkThreads = 128;
-constexpr int kTileThreads = 128, kTileWarps = kTileThreads / 32;
+constexpr int kTileThreads = 128;
 constexpr int kMaxCluster = 16;
 
 // A tensor: element 0 of row t of sequence i at p + i * batch + t * row.
@@ -39,12 +39,88 @@ __device__ __forceinline__ int64_t scan_length(const ScanArgs &a, int64_t i)
     return n < 0 ? 0 : n > a.length ? a.length : n;
 }
 
-// f = 1 / (1 + e^-z) and 1 - f = e^-z / (1 + e^-z), each with a small relative error at either end.
-__device__ __forceinline__ void gate(float z, float &f, float &shut)
+constexpr float kMinusLog2e = -1.44269504088896340736f;
+
+// 2^x and 1 / x by the hardware's approximations, within 2^-22 relative (x above 2^126 gives 0).
+__device__ __forceinline__ float exp2_fast(float x)
 {
-    const float e = __expf(-fabsf(z)), big = __fdividef(1.0f, __fadd_rn(1.0f, e)), small = __fmul_rn(e, big);
-    f = z >= 0.0f ? big : small;
-    shut = z >= 0.0f ? small : big;
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float recip_fast(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// At most 126, so that neither 2^x nor its reciprocal leaves the normal numbers; NaN stays.
+__device__ __forceinline__ float below_126(float x)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(126.0f));
+    return r;
+}
+
+// V values of a thread's columns, in pairs where there are two or more.
+template <int V>
+struct Lanes {
+    F2 x[V / 2];
+    __device__ __forceinline__ void set(float a)
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) x[i] = both(a);
+    }
+    __device__ __forceinline__ void get(float (&y)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) unpack2(x[i], y[2 * i], y[2 * i + 1]);
+    }
+    __device__ __forceinline__ void put(const float (&y)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) x[i] = pack2(y[2 * i], y[2 * i + 1]);
+    }
+};
+template <>
+struct Lanes<1> {
+    float x[1];
+    __device__ __forceinline__ void set(float a) { x[0] = a; }
+    __device__ __forceinline__ void get(float (&y)[1]) const { y[0] = x[0]; }
+    __device__ __forceinline__ void put(const float (&y)[1]) { x[0] = y[0]; }
+};
+__device__ __forceinline__ float fma2(float a, float b, float c) { return __fmaf_rn(a, b, c); }
+__device__ __forceinline__ float add2(float a, float b) { return __fadd_rn(a, b); }
+__device__ __forceinline__ float times2(float a, float b) { return __fmul_rn(a, b); }
+__device__ __forceinline__ F2 times2(F2 a, F2 b)
+{
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+template <int V>
+__device__ __forceinline__ Lanes<V> fma(const Lanes<V> &a, const Lanes<V> &b, const Lanes<V> &c)
+{
+    Lanes<V> r;
+#pragma unroll
+    for (int i = 0; i < (V + 1) / 2; ++i) r.x[i] = fma2(a.x[i], b.x[i], c.x[i]);
+    return r;
+}
+template <int V>
+__device__ __forceinline__ Lanes<V> operator*(const Lanes<V> &a, const Lanes<V> &b)
+{
+    Lanes<V> r;
+#pragma unroll
+    for (int i = 0; i < (V + 1) / 2; ++i) r.x[i] = times2(a.x[i], b.x[i]);
+    return r;
+}
+template <int V>
+__device__ __forceinline__ Lanes<V> operator+(const Lanes<V> &a, const Lanes<V> &b)
+{
+    Lanes<V> r;
+#pragma unroll
+    for (int i = 0; i < (V + 1) / 2; ++i) r.x[i] = add2(a.x[i], b.x[i]);
+    return r;
 }
 
 // V consecutive elements in one access.
@@ -52,6 +128,104 @@ template <class T, int V>
 struct alignas(V * sizeof(T)) Vec {
     T x[V];
 };
+
+template <class T, int V>
+__device__ __forceinline__ Lanes<V> lanes(const Vec<T, V> &v)
+{
+    Lanes<V> r;
+    float y[V];
+    if constexpr (std::is_same<T, bf16>::value && V > 1) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(v.x);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) y[2 * i] = __uint_as_float(w[i] << 16), y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else if constexpr (std::is_same<T, f16>::value && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(v.x + 2 * i));
+            y[2 * i] = p.x, y[2 * i + 1] = p.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = to_f32(v.x[i]);
+    }
+    r.put(y);
+    return r;
+}
+template <class T, int V>
+__device__ __forceinline__ Vec<T, V> rounded(const Lanes<V> &a)
+{
+    Vec<T, V> r;
+    float y[V];
+    a.get(y);
+    if constexpr (std::is_same<T, bf16>::value && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) *reinterpret_cast<__nv_bfloat162 *>(r.x + 2 * i) = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+    } else if constexpr (std::is_same<T, f16>::value && V > 1) {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) *reinterpret_cast<__half2 *>(r.x + 2 * i) = __floats2half2_rn(y[2 * i], y[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r.x[i] = from_f32<T>(y[i]);
+    }
+    return r;
+}
+template <class T, int V>
+__device__ __forceinline__ Vec<T, V> filled(float a)
+{
+    Lanes<V> x;
+    x.set(a);
+    return rounded<T, V>(x);
+}
+
+// V states, on a 16-byte boundary where V > 1.
+template <int V>
+__device__ __forceinline__ Lanes<V> load_states(const float *p)
+{
+    Lanes<V> r;
+    alignas(16) float y[V];
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(y + i) = *reinterpret_cast<const float4 *>(p + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = p[i];
+    }
+    r.put(y);
+    return r;
+}
+template <int V>
+__device__ __forceinline__ void store_states(float *p, const Lanes<V> &a)
+{
+    alignas(16) float y[V];
+    a.get(y);
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = *reinterpret_cast<const float4 *>(y + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) p[i] = y[i];
+    }
+}
+
+// With e = 2^(-z log2 e), at most 2^126:  f = 1 / (1 + e) and 1 - f = e f, each with a small relative error at either end.
+// 2^-126 less makes f 0 where e is at its limit and does not change an f of 2^-101 or more.
+template <int V>
+__device__ __forceinline__ void gate(const Lanes<V> &z, Lanes<V> &f, Lanes<V> &shut)
+{
+    Lanes<V> scale, one, least, e;
+    float y[V];
+    scale.set(kMinusLog2e), one.set(1.0f), least.set(-0x1p-126f);
+    (z * scale).get(y);
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = exp2_fast(below_126(y[i]));
+    e.put(y);
+    (e + one).get(y);
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = recip_fast(y[i]);
+    f.put(y);
+    shut = e * f;
+    f = f + least;
+}
 
 // ---------------------------------------------------------------------------------------------- short sequences
 // A thread takes V columns of a sequence from its first row to its last, the loads of kAhead rows before their arithmetic.
@@ -65,11 +239,11 @@ __global__ void __launch_bounds__(kWalkThreads) scan_walk_kernel(const ScanArgs 
     const int64_t i = k / packs, c = (k - i * packs) * V, n = scan_length(a, i);
     const T *z = zs.p + i * zs.batch + c, *v = vs.p + i * vs.batch + c;
     T *h = hs.p + i * hs.batch + c;
-    float state[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) state[j] = a.initial ? a.initial[i * a.dim + c + j] : 0.0f;
+    Lanes<V> state;
+    state.set(0.0f);
+    if (a.initial) state = load_states<V>(a.initial + i * a.dim + c);
     for (int64_t t = 0; t < a.length; t += kAhead) {
-        Vec<T, V> zv[kAhead], vv[kAhead], out;
+        Vec<T, V> zv[kAhead], vv[kAhead];
 #pragma unroll
         for (int r = 0; r < kAhead; ++r)
             if (t + r < n) {
@@ -79,21 +253,15 @@ __global__ void __launch_bounds__(kWalkThreads) scan_walk_kernel(const ScanArgs 
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) {
             if (t + r >= a.length) break;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float f, shut;
-                if (t + r < n) {
-                    gate(to_f32(zv[r].x[j]), f, shut);
-                    state[j] = __fmaf_rn(f, state[j], __fmul_rn(shut, to_f32(vv[r].x[j])));
-                }
-                out.x[j] = from_f32<T>(t + r < n ? state[j] : 0.0f);
+            if (t + r < n) {
+                Lanes<V> f, shut;
+                gate(lanes(zv[r]), f, shut);
+                state = fma(f, state, shut * lanes(vv[r]));
             }
-            *reinterpret_cast<Vec<T, V> *>(h + (t + r) * hs.row) = out;
+            *reinterpret_cast<Vec<T, V> *>(h + (t + r) * hs.row) = t + r < n ? rounded<T, V>(state) : filled<T, V>(0.0f);
         }
     }
-    if (final)
-#pragma unroll
-        for (int j = 0; j < V; ++j) final[i * a.dim + c + j] = state[j];
+    if (final) store_states(final + i * a.dim + c, state);
 }
 
 // A gradient's tensors.
@@ -114,64 +282,53 @@ __global__ void __launch_bounds__(kWalkThreads) scan_walk_back_kernel(const Scan
     using W = Vec<T, V>;
     auto at = [&](const Seq<const T> &s, int64_t t) { return *reinterpret_cast<const W *>(s.p + i * s.batch + t * s.row + c); };
     auto to = [&](const Seq<T> &s, int64_t t) -> W & { return *reinterpret_cast<W *>(s.p + i * s.batch + t * s.row + c); };
-    W zero;
-    float carry[V];  // f_{t+1} g_{t+1}
-#pragma unroll
-    for (int j = 0; j < V; ++j) carry[j] = g.d_final ? g.d_final[i * a.dim + c + j] : 0.0f, zero.x[j] = from_f32<T>(0.0f);
+    const W zero = filled<T, V>(0.0f);
+    Lanes<V> carry, minus, first;  // carry: f_{t+1} g_{t+1}
+    carry.set(0.0f), minus.set(-1.0f), first.set(0.0f);
+    if (g.d_final) carry = load_states<V>(g.d_final + i * a.dim + c);
+    if (a.initial) first = load_states<V>(a.initial + i * a.dim + c);
     for (int64_t t = a.length - 1; t >= 0; --t) {
         if (t >= n) {
             to(g.dz, t) = zero;
             to(g.dv, t) = zero;
             continue;
         }
-        const W z = at(g.z, t), dh = at(g.dh, t), v = at(g.v, t), h = t ? at(g.h, t - 1) : zero;
-        W dz, dv;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float before = t ? to_f32(h.x[j]) : a.initial ? a.initial[i * a.dim + c + j] : 0.0f;
-            float f, shut;
-            gate(to_f32(z.x[j]), f, shut);
-            const float gt = __fadd_rn(to_f32(dh.x[j]), carry[j]), d = __fmul_rn(shut, gt);
-            carry[j] = __fmul_rn(f, gt);
-            dv.x[j] = from_f32<T>(d);
-            dz.x[j] = from_f32<T>(__fmul_rn(__fmul_rn(f, d), __fsub_rn(before, to_f32(v.x[j]))));
-        }
-        to(g.dz, t) = dz;
-        to(g.dv, t) = dv;
+        const W z = at(g.z, t), dh = at(g.dh, t), v = at(g.v, t);
+        const Lanes<V> before = t ? lanes(at(g.h, t - 1)) : first;
+        Lanes<V> f, shut;
+        gate(lanes(z), f, shut);
+        const Lanes<V> gt = lanes(dh) + carry, d = shut * gt;
+        carry = f * gt;
+        to(g.dv, t) = rounded<T, V>(d);
+        to(g.dz, t) = rounded<T, V>((f * d) * fma(lanes(v), minus, before));
     }
-    if (g.d_initial)
-#pragma unroll
-        for (int j = 0; j < V; ++j) g.d_initial[i * a.dim + c + j] = carry[j];
+    if (g.d_initial) store_states(g.d_initial + i * a.dim + c, carry);
 }
 
 // ---------------------------------------------------------------------------------------------- tiles
-// A thread's V columns are 16 bytes where rows allow it (a warp's lanes then cover 128-byte pieces of 4 rows), else one element
-// (a warp covers 32 columns), and its rows 64 bytes of each tensor, or 16 elements.
-template <class T, int V>
+// A thread's V columns are 16 bytes where rows allow it (eight lanes then cover a 128-byte piece of a row), else one element
+// (a warp covers 32 columns).  S: its rows.
+template <class T, int V, int S>
 struct Tile {
     static constexpr int kLanes = V == 1 ? 32 : 8;            // lanes across a row
     static constexpr int kColumns = kLanes * V;
-    static constexpr int kRows = V == 1 ? 16 : 4;             // of a thread
-    static constexpr int kSegs = kTileThreads / kLanes;
+    static constexpr int kRows = S;
+    static constexpr int kSegs = kTileThreads / kLanes;       // threads along the rows
     static constexpr int kChunk = kSegs * kRows;              // rows of a CTA in a step
-    static constexpr bool kRing = V * sizeof(T) >= 4;         // what asynchronous copies can move
-    static constexpr int kPack = V * sizeof(T);
+    static constexpr bool kRing = V > 1;                      // rows come through shared memory, else through registers
+    static constexpr int kGroups = kTileThreads / kColumns;   // threads that compose a column's pieces, adjacent lanes
+    static constexpr int kPieces = kSegs / kGroups;           // of each of them
 };
 
-// What a tile's CTA shares, behind its ring of copies.
-template <int C>
+// What a tile's CTA shares, behind its ring of copies.  A piece's columns are turned around within 32 lanes' worth by its group,
+// so that the lanes that read a column's pieces fall into different banks.
+template <class L>
 struct TileShared {
-    float2 warp[kTileWarps][C];           // each warp's composition
-    float start[kTileWarps][C];           // the state that each warp starts with
-    float2 rank[2][kMaxCluster][C];       // the CTAs' compositions, of this step and the last
+    uint64_t arrived[2];                                       // barriers of `rank`
+    float a[L::kSegs][L::kColumns], b[L::kSegs][L::kColumns];  // each thread's composition, then in b the state it starts with
+    float2 rank[2][kMaxCluster][L::kColumns];                  // the CTAs' compositions, of this step and the last
+    static __device__ __forceinline__ int at(int seg, int column) { return column ^ (seg / L::kPieces * (32 / L::kGroups)); }
 };
-
-template <int BYTES>
-__device__ __forceinline__ void cp_async(void *dst, const void *src)
-{
-    if constexpr (BYTES == 16) cp_async16(dst, src);
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(dst)), "l"(src), "n"(BYTES) : "memory");
-}
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -185,279 +342,290 @@ __device__ __forceinline__ uint32_t cluster_size()
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// A store to the shared memory of another CTA of the cluster, at the place that `p` is in this one.
-__device__ __forceinline__ void store_remote(float2 *p, uint32_t rank, float2 v)
+__device__ __forceinline__ void cluster_sync()
 {
-    uint32_t to;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Stores to the shared memory of a CTA of the cluster, at the place that `p` is in this one, and counts the 8 bytes on its
+// barrier at the place that `bar` is.
+__device__ __forceinline__ void store_remote(float2 *p, uint64_t *bar, uint32_t rank, float2 v)
+{
+    uint32_t to, at;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(p)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(to), "f"(v.x), "f"(v.y), "r"(at)
+                 : "memory");
 }
 
-// From each thread's composition (A, B) of its rows to the state that it starts with.  carry: in the first kColumns threads,
-// the state before the step of this thread's column, and the one after it on return.
-template <class L>
-__device__ __forceinline__ void tile_start(float (&A)[L::kColumns / L::kLanes], float (&B)[L::kColumns / L::kLanes], float &carry,
-                                           TileShared<L::kColumns> &sh, uint32_t rank, uint32_t ranks, int parity)
+// A CTA's place in its cluster, and the step that its exchange is at.
+struct Exchange {
+    uint32_t rank = 0, ranks = 1, step = 0;
+    bool late = false;  // whether a wait has run out
+
+    template <class S>
+    __device__ __forceinline__ void begin(S &sh)
+    {
+        rank = cluster_rank(), ranks = cluster_size();
+        if (threadIdx.x == 0) {
+            mbar_init(&sh.arrived[0], 1);
+            mbar_init(&sh.arrived[1], 1);
+            mbar_init_fence();
+        }
+        cluster_sync();  // before any CTA stores into another
+    }
+};
+
+template <int V>
+__device__ __forceinline__ void to_shared(float *p, const Lanes<V> &a)
 {
-    constexpr int V = L::kColumns / L::kLanes;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = lane % L::kLanes * V;
-#pragma unroll
-    for (int o = L::kLanes; o < 32; o *= 2)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float a = __shfl_up_sync(0xffffffffu, A[j], o), b = __shfl_up_sync(0xffffffffu, B[j], o);
-            if (lane >= o) {
-                B[j] = __fmaf_rn(A[j], b, B[j]);
-                A[j] = __fmul_rn(A[j], a);
-            }
-        }
-    if (lane >= 32 - L::kLanes)
-#pragma unroll
-        for (int j = 0; j < V; ++j) sh.warp[warp][c0 + j] = make_float2(A[j], B[j]);
-    if constexpr (L::kLanes < 32) {  // what the lanes before this one's make
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            A[j] = __shfl_up_sync(0xffffffffu, A[j], L::kLanes);
-            B[j] = __shfl_up_sync(0xffffffffu, B[j], L::kLanes);
-        }
-    }
-    if (lane < L::kLanes)
-#pragma unroll
-        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
-    __syncthreads();
-    float2 before[kTileWarps], all = make_float2(1.0f, 0.0f);
-    const bool column = threadIdx.x < L::kColumns;
-    if (column) {
-#pragma unroll
-        for (int w = 0; w < kTileWarps; ++w) {
-            const float2 x = sh.warp[w][threadIdx.x];
-            before[w] = all;
-            all = make_float2(__fmul_rn(x.x, all.x), __fmaf_rn(x.x, all.y, x.y));
-        }
-        if (ranks > 1)
-            for (uint32_t r = 0; r < ranks; ++r) store_remote(&sh.rank[parity][rank][threadIdx.x], r, all);
-    }
-    if (ranks > 1) {
-        cluster_arrive();
-        cluster_wait();
-    }
-    if (column) {
-        float mine = carry;
-        if (ranks > 1) {
-            float x = carry;
-            for (uint32_t r = 0; r < ranks; ++r) {
-                if (r == rank) mine = x;
-                const float2 y = sh.rank[parity][r][threadIdx.x];
-                x = __fmaf_rn(y.x, x, y.y);
-            }
-            carry = x;
-        } else {
-            carry = __fmaf_rn(all.x, carry, all.y);
-        }
-#pragma unroll
-        for (int w = 0; w < kTileWarps; ++w) sh.start[w][threadIdx.x] = __fmaf_rn(before[w].x, mine, before[w].y);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < V; ++j) B[j] = __fmaf_rn(A[j], sh.start[warp][c0 + j], B[j]);
+    store_states<V>(p, a);
 }
 
-// blockIdx.x: tile of columns x sequence, in clusters along the rows (blockIdx.x / ranks is the tile).
-template <class T, int V, int DEPTH>
+// From each thread's composition (A, B) of its rows to the state that it starts with.  carry: the state before the step of
+// column threadIdx.x / kGroups, and the one after it on return.  A CTA's composition goes to all CTAs of its cluster, into one
+// of two buffers: a CTA sends the next but one after it has waited for the next, which the others send after this one is read.
+template <bool CLUSTER, class L, int V>
+__device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V> &B, float &carry, TileShared<L> &sh, Exchange &x, uint32_t *status)
+{
+    constexpr int G = L::kGroups;
+    const int seg = threadIdx.x / L::kLanes, c0 = threadIdx.x % L::kLanes * V;
+    const int column = threadIdx.x / G, group = threadIdx.x % G;
+    to_shared(&sh.a[seg][sh.at(seg, c0)], A);
+    to_shared(&sh.b[seg][sh.at(seg, c0)], B);
+    __syncthreads();
+    float pa[L::kPieces], pb[L::kPieces], m = 1.0f, y = 0.0f;  // what the pieces before each of the group's make of a state
+#pragma unroll
+    for (int k = 0; k < L::kPieces; ++k) {
+        const int s = group * L::kPieces + k, at = sh.at(s, column);
+        const float a = sh.a[s][at], b = sh.b[s][at];
+        pa[k] = m, pb[k] = y;
+        y = __fmaf_rn(a, y, b);
+        m = __fmul_rn(a, m);
+    }
+#pragma unroll
+    for (int o = 1; o < G; o *= 2) {  // the groups before this one's, and it
+        const float a = __shfl_up_sync(0xffffffffu, m, o, G), b = __shfl_up_sync(0xffffffffu, y, o, G);
+        if (group >= o) {
+            y = __fmaf_rn(m, b, y);
+            m = __fmul_rn(m, a);
+        }
+    }
+    const float2 all = make_float2(__shfl_sync(0xffffffffu, m, G - 1, G), __shfl_sync(0xffffffffu, y, G - 1, G));
+    m = __shfl_up_sync(0xffffffffu, m, 1, G);
+    y = __shfl_up_sync(0xffffffffu, y, 1, G);
+    float state = carry;
+    if constexpr (CLUSTER) {
+        const uint32_t buffer = x.step & 1;
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.arrived[buffer], x.ranks * L::kColumns * 8);
+        for (uint32_t r = group; r < x.ranks; r += G) store_remote(&sh.rank[buffer][x.rank][column], &sh.arrived[buffer], r, all);
+        if (!x.late && !mbar_wait(&sh.arrived[buffer], x.step >> 1 & 1)) {
+            x.late = true;
+            report_status(status, kStatusTimeout);
+        }
+        for (uint32_t r = 0; r < x.ranks; ++r) {
+            if (r == x.rank) state = carry;
+            const float2 c = sh.rank[buffer][r][column];
+            carry = __fmaf_rn(c.x, carry, c.y);
+        }
+        ++x.step;
+    } else {
+        carry = __fmaf_rn(all.x, carry, all.y);
+    }
+    if (group) state = __fmaf_rn(m, state, y);
+#pragma unroll
+    for (int k = 0; k < L::kPieces; ++k) {
+        const int s = group * L::kPieces + k;
+        sh.b[s][sh.at(s, column)] = __fmaf_rn(pa[k], state, pb[k]);
+    }
+    __syncthreads();
+    return load_states<V>(&sh.b[seg][sh.at(seg, c0)]);
+}
+
+// blockIdx.x: sequence and tile of columns, in clusters along the rows (blockIdx.x / ranks is the tile).
+template <class T, int V, int S, int DEPTH, bool CLUSTER>
 __global__ void __launch_bounds__(kTileThreads) scan_tile_kernel(const ScanArgs a, const Seq<const T> zs, const Seq<const T> vs, const Seq<T> hs, float *final)
 {
-    using L = Tile<T, V>;
+    using L = Tile<T, V, S>;
     using W = Vec<T, V>;
-    constexpr int S = L::kRows;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ TileShared<L::kColumns> sh;
-    const uint32_t rank = cluster_rank(), ranks = cluster_size();
-    const uint32_t tile = blockIdx.x / ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
+    __shared__ __align__(16) TileShared<L> sh;
+    Exchange x;
+    if constexpr (CLUSTER) x.begin(sh);
+    const uint32_t tile = blockIdx.x / x.ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
     const int64_t i = tile / tiles, c0 = static_cast<int64_t>(tile % tiles) * L::kColumns;
     const int64_t c = c0 + threadIdx.x % L::kLanes * V;
     const bool inside = c < a.dim;
-    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(ranks) * L::kChunk;
+    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk;
     const T *z = zs.p + i * zs.batch + c, *v = vs.p + i * vs.batch + c;
     T *h = hs.p + i * hs.batch + c;
-    if (ranks > 1) cluster_arrive();  // every CTA runs before any stores into another
-    const int64_t column = c0 + threadIdx.x;  // of the state that this thread carries
-    const bool carries = threadIdx.x < L::kColumns && column < a.dim;
-    float carry = carries && a.initial ? a.initial[i * a.dim + column] : 0.0f;
-    const int64_t first = rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;  // this thread's first row
+    const int64_t column = c0 + threadIdx.x / L::kGroups;  // of the state that this thread carries
+    float carry = column < a.dim && a.initial ? a.initial[i * a.dim + column] : 0.0f;
+    const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;  // this thread's first row
+    // Rows that are not there have z of infinity and v of 0: the state passes through them.
+    const W closed = filled<T, V>(__int_as_float(0x7f800000)), zero = filled<T, V>(0.0f);
     W *ring = reinterpret_cast<W *>(smem) + threadIdx.x;  // a stage: S of z, then S of v, one per thread each
+    W zv[S], vv[S];
     auto fetch = [&](int64_t t, int stage) {
+        const T *from_z = z + t * zs.row, *from_v = v + t * vs.row;
         if constexpr (L::kRing) {
-#pragma unroll
-            for (int r = 0; r < S; ++r)
-                if (inside && t + r < n) {
-                    cp_async<L::kPack>(ring + (stage * 2 * S + r) * kTileThreads, z + (t + r) * zs.row);
-                    cp_async<L::kPack>(ring + ((stage * 2 + 1) * S + r) * kTileThreads, v + (t + r) * vs.row);
-                }
-            cp_async_commit();
-        }
-    };
-    if constexpr (L::kRing)
-        for (int d = 0; d < DEPTH; ++d) fetch(first + d * stride, d);
-    if (ranks > 1) cluster_wait();
-    int stage = 0, parity = 0;
-    for (int64_t base = 0; base < a.length; base += stride) {
-        const int64_t t = first + base;
-        float f[S][V], u[S][V], A[V], B[V];
-        W zv[S], vv[S];
-        if constexpr (L::kRing) {
-            cp_async_wait<DEPTH - 1>();
+            W *to = ring + stage * (2 * S * kTileThreads);
 #pragma unroll
             for (int r = 0; r < S; ++r) {
-                zv[r] = ring[(stage * 2 * S + r) * kTileThreads];
-                vv[r] = ring[((stage * 2 + 1) * S + r) * kTileThreads];
+                if (inside && t + r < n) {
+                    cp_async16(to + r * kTileThreads, from_z + r * zs.row);
+                    cp_async16(to + (S + r) * kTileThreads, from_v + r * vs.row);
+                } else {
+                    to[r * kTileThreads] = closed;
+                    to[(S + r) * kTileThreads] = zero;
+                }
             }
+            cp_async_commit();
         } else {
 #pragma unroll
-            for (int r = 0; r < S; ++r)
-                if (inside && t + r < n) {
-                    zv[r] = *reinterpret_cast<const W *>(z + (t + r) * zs.row);
-                    vv[r] = *reinterpret_cast<const W *>(v + (t + r) * vs.row);
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
-#pragma unroll
-        for (int r = 0; r < S; ++r) {
-            const bool on = inside && t + r < n;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float shut;
-                gate(to_f32(zv[r].x[j]), f[r][j], shut);
-                u[r][j] = on ? __fmul_rn(shut, to_f32(vv[r].x[j])) : 0.0f;
-                f[r][j] = on ? f[r][j] : 1.0f;
-                B[j] = __fmaf_rn(f[r][j], B[j], u[r][j]);
-                A[j] = __fmul_rn(f[r][j], A[j]);
+            for (int r = 0; r < S; ++r) {
+                const bool on = inside && t + r < n;
+                zv[r] = on ? *reinterpret_cast<const W *>(from_z + r * zs.row) : closed;
+                vv[r] = on ? *reinterpret_cast<const W *>(from_v + r * vs.row) : zero;
             }
         }
-        if constexpr (L::kRing) fetch(t + DEPTH * stride, stage);
-        tile_start<L>(A, B, carry, sh, rank, ranks, parity);
+    };
+    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(first + d * stride, d);
+    int stage = 0;
+    for (int64_t base = 0; base < n; base += stride) {
+        const int64_t t = first + base;
+        if constexpr (L::kRing) {
+            cp_async_wait<DEPTH - 1>();
+            const W *from = ring + stage * (2 * S * kTileThreads);
+#pragma unroll
+            for (int r = 0; r < S; ++r) zv[r] = from[r * kTileThreads], vv[r] = from[(S + r) * kTileThreads];
+        }
+        Lanes<V> f[S], u[S], A, B;
 #pragma unroll
         for (int r = 0; r < S; ++r) {
-            W out;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                B[j] = __fmaf_rn(f[r][j], B[j], u[r][j]);
-                out.x[j] = from_f32<T>(t + r < n ? B[j] : 0.0f);
-            }
-            if (inside && t + r < a.length) *reinterpret_cast<W *>(h + (t + r) * hs.row) = out;
+            Lanes<V> shut;
+            gate(lanes(zv[r]), f[r], shut);
+            u[r] = shut * lanes(vv[r]);
+            B = r ? fma(f[r], B, u[r]) : u[r];
+            A = r ? f[r] * A : f[r];
         }
+        fetch(t + (L::kRing ? DEPTH : 1) * stride, stage);
+        Lanes<V> state = tile_start<CLUSTER>(A, B, carry, sh, x, a.status);
+        T *to = h + t * hs.row;
+        if (inside)
+#pragma unroll
+            for (int r = 0; r < S; ++r) {
+                state = fma(f[r], state, u[r]);
+                if (t + r < n) *reinterpret_cast<W *>(to + r * hs.row) = rounded<T, V>(state);
+            }
         stage = stage + 1 == DEPTH ? 0 : stage + 1;
-        parity ^= 1;
     }
-    if (final && carries && rank == 0) final[i * a.dim + column] = carry;
+    if (inside)
+        for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs) *reinterpret_cast<W *>(h + t * hs.row) = zero;
+    if (final && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) final[i * a.dim + column] = carry;
 }
 
-// The same from the last row to the first: q counts rows from the end.
-template <class T, int V, int DEPTH>
+// The same from the last row to the first: q counts rows from the sequence's end.
+template <class T, int V, int S, int DEPTH, bool CLUSTER>
 __global__ void __launch_bounds__(kTileThreads) scan_tile_back_kernel(const ScanArgs a, const ScanGrads<T> g)
 {
-    using L = Tile<T, V>;
+    using L = Tile<T, V, S>;
     using W = Vec<T, V>;
-    constexpr int S = L::kRows;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ TileShared<L::kColumns> sh;
-    const uint32_t rank = cluster_rank(), ranks = cluster_size();
-    const uint32_t tile = blockIdx.x / ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
+    __shared__ __align__(16) TileShared<L> sh;
+    Exchange x;
+    if constexpr (CLUSTER) x.begin(sh);
+    const uint32_t tile = blockIdx.x / x.ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
     const int64_t i = tile / tiles, c0 = static_cast<int64_t>(tile % tiles) * L::kColumns;
     const int64_t c = c0 + threadIdx.x % L::kLanes * V;
     const bool inside = c < a.dim;
-    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(ranks) * L::kChunk, end = a.length - 1;
+    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk, end = n - 1;
     const T *z = g.z.p + i * g.z.batch + c, *v = g.v.p + i * g.v.batch + c, *h = g.h.p + i * g.h.batch + c, *dh = g.dh.p + i * g.dh.batch + c;
     T *dz = g.dz.p + i * g.dz.batch + c, *dv = g.dv.p + i * g.dv.batch + c;
-    if (ranks > 1) cluster_arrive();
-    const int64_t column = c0 + threadIdx.x;
-    const bool carries = threadIdx.x < L::kColumns && column < a.dim;
-    float carry = carries && g.d_final ? g.d_final[i * a.dim + column] : 0.0f;
-    const int64_t first = rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;
+    const int64_t column = c0 + threadIdx.x / L::kGroups;
+    float carry = column < a.dim && g.d_final ? g.d_final[i * a.dim + column] : 0.0f;
+    const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;
+    const W closed = filled<T, V>(__int_as_float(0x7f800000)), zero = filled<T, V>(0.0f);
     W *ring = reinterpret_cast<W *>(smem) + threadIdx.x;  // a stage: S of z, of dh, of v and of h
     auto slot = [&](int stage, int what, int r) -> W & { return ring[((stage * 4 + what) * S + r) * kTileThreads]; };
+    constexpr int R = L::kRing ? 1 : S;
+    W zr[R], dr[R], vr[R], hr[R], zn[R], dn[R], vn[R], hn[R];  // without the ring: this step's and the next one's
     auto fetch = [&](int64_t q, int stage) {
-        if constexpr (L::kRing) {
 #pragma unroll
-            for (int r = 0; r < S; ++r) {
-                const int64_t t = end - q - r;
-                if (inside && t >= 0 && t < n) {
-                    cp_async<L::kPack>(&slot(stage, 0, r), z + t * g.z.row);
-                    cp_async<L::kPack>(&slot(stage, 1, r), dh + t * g.dh.row);
-                    cp_async<L::kPack>(&slot(stage, 2, r), v + t * g.v.row);
-                    if (t) cp_async<L::kPack>(&slot(stage, 3, r), h + (t - 1) * g.h.row);
+        for (int r = 0; r < S; ++r) {
+            const int64_t t = end - q - r;
+            const bool on = inside && t >= 0;
+            if constexpr (L::kRing) {
+                if (on) {
+                    cp_async16(&slot(stage, 0, r), z + t * g.z.row);
+                    cp_async16(&slot(stage, 1, r), dh + t * g.dh.row);
+                    cp_async16(&slot(stage, 2, r), v + t * g.v.row);
+                    if (t) cp_async16(&slot(stage, 3, r), h + (t - 1) * g.h.row);
+                } else {
+                    slot(stage, 0, r) = closed;
+                    slot(stage, 1, r) = zero;
                 }
+            } else {
+                zn[r] = on ? *reinterpret_cast<const W *>(z + t * g.z.row) : closed;
+                dn[r] = on ? *reinterpret_cast<const W *>(dh + t * g.dh.row) : zero;
+                vn[r] = on ? *reinterpret_cast<const W *>(v + t * g.v.row) : zero;
+                hn[r] = on && t ? *reinterpret_cast<const W *>(h + (t - 1) * g.h.row) : zero;
             }
-            cp_async_commit();
         }
+        if constexpr (L::kRing) cp_async_commit();
     };
-    if constexpr (L::kRing)
-        for (int d = 0; d < DEPTH; ++d) fetch(first + d * stride, d);
-    if (ranks > 1) cluster_wait();
-    int stage = 0, parity = 0;
-    for (int64_t base = 0; base < a.length; base += stride) {
+    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(first + d * stride, d);
+    Lanes<V> minus;
+    minus.set(-1.0f);
+    int stage = 0;
+    for (int64_t base = 0; base < n; base += stride) {
         const int64_t q = first + base;
-        float f[S][V], shut[S][V], A[V], B[V];
-        W zr[L::kRing ? 1 : S], dr[L::kRing ? 1 : S], vr[L::kRing ? 1 : S], hr[L::kRing ? 1 : S];
         if constexpr (L::kRing) {
             cp_async_wait<DEPTH - 1>();
         } else {
 #pragma unroll
+            for (int r = 0; r < S; ++r) zr[r] = zn[r], dr[r] = dn[r], vr[r] = vn[r], hr[r] = hn[r];
+            fetch(q + stride, 0);
+        }
+        Lanes<V> f[S], shut[S], A, B;
+#pragma unroll
+        for (int r = 0; r < S; ++r) {
+            Lanes<V> d;
+            if constexpr (L::kRing) gate(lanes(slot(stage, 0, r)), f[r], shut[r]), d = lanes(slot(stage, 1, r));
+            else gate(lanes(zr[r]), f[r], shut[r]), d = lanes(dr[r]);
+            B = f[r] * (r ? d + B : d);
+            A = r ? f[r] * A : f[r];
+        }
+        Lanes<V> later = tile_start<CLUSTER>(A, B, carry, sh, x, a.status);
+        if (inside)
+#pragma unroll
             for (int r = 0; r < S; ++r) {
                 const int64_t t = end - q - r;
-                if (inside && t >= 0 && t < n) {
-                    zr[r] = *reinterpret_cast<const W *>(z + t * g.z.row);
-                    dr[r] = *reinterpret_cast<const W *>(dh + t * g.dh.row);
-                    vr[r] = *reinterpret_cast<const W *>(v + t * g.v.row);
-                    if (t) hr[r] = *reinterpret_cast<const W *>(h + (t - 1) * g.h.row);
+                if (t < 0) continue;
+                W d, vv, hv;
+                if constexpr (L::kRing) d = slot(stage, 1, r), vv = slot(stage, 2, r), hv = slot(stage, 3, r);
+                else d = dr[r], vv = vr[r], hv = hr[r];
+                Lanes<V> before = lanes(hv);
+                if (t == 0) {
+                    float y[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) y[j] = a.initial ? a.initial[i * a.dim + c + j] : 0.0f;
+                    before.put(y);
                 }
+                const Lanes<V> gt = lanes(d) + later, dvt = shut[r] * gt;
+                later = f[r] * gt;
+                *reinterpret_cast<W *>(dv + t * g.dv.row) = rounded<T, V>(dvt);
+                *reinterpret_cast<W *>(dz + t * g.dz.row) = rounded<T, V>((f[r] * dvt) * fma(lanes(vv), minus, before));
             }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
-#pragma unroll
-        for (int r = 0; r < S; ++r) {
-            const int64_t t = end - q - r;
-            const bool on = inside && t >= 0 && t < n;
-            W zv, d;
-            if constexpr (L::kRing) zv = slot(stage, 0, r), d = slot(stage, 1, r);
-            else zv = zr[r], d = dr[r];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                gate(to_f32(zv.x[j]), f[r][j], shut[r][j]);
-                const float dht = on ? to_f32(d.x[j]) : 0.0f;
-                f[r][j] = on ? f[r][j] : 1.0f;
-                B[j] = __fmul_rn(f[r][j], __fadd_rn(dht, B[j]));
-                A[j] = __fmul_rn(f[r][j], A[j]);
-            }
-        }
-        tile_start<L>(A, B, carry, sh, rank, ranks, parity);
-#pragma unroll
-        for (int r = 0; r < S; ++r) {
-            const int64_t t = end - q - r;
-            const bool on = t < n;
-            if (!inside || t < 0) continue;
-            W d, vv, hv, oz, ov;
-            if constexpr (L::kRing) d = slot(stage, 1, r), vv = slot(stage, 2, r), hv = slot(stage, 3, r);
-            else d = dr[r], vv = vr[r], hv = hr[r];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float before = t ? to_f32(hv.x[j]) : a.initial ? a.initial[i * a.dim + c + j] : 0.0f;
-                const float gt = __fadd_rn(to_f32(d.x[j]), B[j]), dvt = __fmul_rn(shut[r][j], gt);
-                if (on) B[j] = __fmul_rn(f[r][j], gt);
-                ov.x[j] = from_f32<T>(on ? dvt : 0.0f);
-                oz.x[j] = from_f32<T>(on ? __fmul_rn(__fmul_rn(f[r][j], dvt), __fsub_rn(before, to_f32(vv.x[j]))) : 0.0f);
-            }
-            *reinterpret_cast<W *>(dz + t * g.dz.row) = oz;
-            *reinterpret_cast<W *>(dv + t * g.dv.row) = ov;
-        }
         if constexpr (L::kRing) fetch(q + DEPTH * stride, stage);
         stage = stage + 1 == DEPTH ? 0 : stage + 1;
-        parity ^= 1;
     }
-    if (g.d_initial && carries && rank == 0) g.d_initial[i * a.dim + column] = carry;
+    if (inside)
+        for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs) {
+            *reinterpret_cast<W *>(dz + t * g.dz.row) = zero;
+            *reinterpret_cast<W *>(dv + t * g.dv.row) = zero;
+        }
+    if (g.d_initial && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) g.d_initial[i * a.dim + column] = carry;
 }
 
 }  // namespace ea
@@ -501,22 +669,35 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
 }
 
 constexpr int64_t kWalkRows = 16;  // sequences up to this length are walked along
-constexpr int kDepth = 3, kBackDepth = 2;
-constexpr int kTileCtasPerSm = 3;
+constexpr int kDepth = 3, kClusterDepth = 2, kBackDepth = 2;  // stages of the rings
+// A thread's rows: of 16-byte accesses without and within a cluster, of single elements, and the same of the gradient.
+constexpr int kRows = 4, kClusterRows = 8, kRowsOfOne = 16, kBackRows = 4, kBackRowsOfOne = 8;
 
-// Launches a kernel of tiles: as many CTAs of a cluster along a sequence as it takes to fill the device, and no more than
-// the sequence has chunks.
-template <class L, class... KArgs, class... Args>
-cudaError_t launch_tiles(const ea_scan *s, const ScanArgs &a, void (*kernel)(KArgs...), size_t smem, Args &&...args)
+// CTAs of a cluster along a sequence: 1 where the tiles alone occupy `fill` quarters of the SMs (an exchange costs as much as
+// a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes, and no more than the
+// sequence has chunks.  Clusters of 16 are for what occupies a part of the device even so (2 x 65,536 x 1024: 146 us in
+// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61).
+template <class L>
+int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
 {
-    const int64_t tiles = a.batch * over<int64_t>(a.dim, L::kColumns), chunks = over<int64_t>(a.length, L::kChunk);
+    const int64_t tiles = a.batch * over<int64_t>(a.dim, L::kColumns), chunks = over<int64_t>(a.length, L::kChunk), sms = s->dev.sms;
     int ranks = 1;
-    while (ranks < kMaxCluster && ranks < chunks && tiles * ranks < static_cast<int64_t>(s->dev.sms) * kTileCtasPerSm) ranks *= 2;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    while (ranks < kMaxCluster && ranks < chunks && tiles * ranks * 4 < sms * fill && (ranks < 8 || tiles * 16 <= sms)) ranks *= 2;
+    return ranks;
+}
+
+template <class L, class... KArgs, class... Args>
+cudaError_t launch_tiles(const ea_scan *s, const ScanArgs &a, int ranks, int stages, void (*kernel)(KArgs...), Args &&...args)
+{
+    const size_t ring = L::kRing ? static_cast<size_t>(stages) * L::kRows * kTileThreads * 16 : 0;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(ring));
     if (e == cudaSuccess && ranks > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
-    return launch_lm(kernel, dim3(static_cast<unsigned>(tiles * ranks)), kTileThreads, smem, s->stream, false, ranks, a, std::forward<Args>(args)...);
+    const int64_t tiles = a.batch * over<int64_t>(a.dim, L::kColumns);
+    return launch_lm(kernel, dim3(static_cast<unsigned>(tiles * ranks)), kTileThreads, ring, s->stream, false, ranks, a, std::forward<Args>(args)...);
 }
+
+bool states_on_16(const void *p, const void *q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) % 16 == 0; }
 
 // f(std::integral_constant<int, V>) for the columns that an access of this call's tensors takes: 16 bytes of them or one.
 template <class T, class F>
@@ -573,7 +754,8 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
     }
     if (r != EA_OK || !a.batch || (!a.length && !final)) return r;
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
-    const bool all = wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) && wide(h, c->h_batch, c->h_row);
+    const bool all = wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) && wide(h, c->h_batch, c->h_row) &&
+                     (a.length > kWalkRows || states_on_16(initial, final));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
@@ -581,14 +763,17 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
         const Seq<T> hs{static_cast<T *>(h), c->h_batch, c->h_row};
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
-            using L = Tile<T, V>;
+            constexpr int S = V == 1 ? kRowsOfOne : kRows, SC = V == 1 ? kRowsOfOne : kClusterRows;
+            using L = Tile<T, V, S>;
+            using LC = Tile<T, V, SC>;
             if (a.length <= kWalkRows) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, zs, vs, hs, final);
                 e = cudaGetLastError();
             } else {
-                const size_t ring = L::kRing ? kDepth * 2 * L::kRows * kTileThreads * L::kPack : 0;
-                e = launch_tiles<L>(s, a, scan_tile_kernel<T, V, kDepth>, ring, zs, vs, hs, final);
+                const int ranks = scan_ranks<LC>(s, a, 5);
+                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kClusterDepth * 2, scan_tile_kernel<T, V, SC, kClusterDepth, true>, zs, vs, hs, final);
+                else e = launch_tiles<L>(s, a, 1, kDepth * 2, scan_tile_kernel<T, V, S, kDepth, false>, zs, vs, hs, final);
             }
         });
     });
@@ -615,7 +800,8 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
     if (r != EA_OK || !a.batch || (!a.length && !d_initial)) return r;
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
     const bool all = wide(dh, c->dh_batch, c->dh_row) && wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) &&
-                     wide(h, c->h_batch, c->h_row) && wide(dz, c->dz_batch, c->dz_row) && wide(dv, c->dv_batch, c->dv_row);
+                     wide(h, c->h_batch, c->h_row) && wide(dz, c->dz_batch, c->dz_row) && wide(dv, c->dv_batch, c->dv_row) &&
+                     (a.length > kWalkRows || (states_on_16(initial, d_final) && states_on_16(d_initial, nullptr)));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
@@ -625,14 +811,16 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
                              out(dz, c->dz_batch, c->dz_row), out(dv, c->dv_batch, c->dv_row), d_final,                     d_initial};
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
-            using L = Tile<T, V>;
+            constexpr int S = V == 1 ? kBackRowsOfOne : kBackRows;
+            using L = Tile<T, V, S>;
             if (a.length <= kWalkRows) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_back_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, g);
                 e = cudaGetLastError();
             } else {
-                const size_t ring = L::kRing ? kBackDepth * 4 * L::kRows * kTileThreads * L::kPack : 0;
-                e = launch_tiles<L>(s, a, scan_tile_back_kernel<T, V, kBackDepth>, ring, g);
+                const int ranks = scan_ranks<L>(s, a, 9);
+                if (ranks > 1) e = launch_tiles<L>(s, a, ranks, kBackDepth * 4, scan_tile_back_kernel<T, V, S, kBackDepth, true>, g);
+                else e = launch_tiles<L>(s, a, 1, kBackDepth * 4, scan_tile_back_kernel<T, V, S, kBackDepth, false>, g);
             }
         });
     });
@@ -647,6 +835,7 @@ int ea_scan_sync_status(ea_scan *s)
     if (r == EA_OK) r = lm_cuda(cudaMemsetAsync(s->status, 0, 4, s->stream), "status clear");
     if (r == EA_OK) r = lm_cuda(cudaStreamSynchronize(s->stream), "stream synchronize");
     if (r != EA_OK) return r;
+    if (st & kStatusTimeout) return lm_fail(EA_E_TIMEOUT, "a wait within a cluster ran out");
     if (st & kStatusLength) return lm_fail(EA_E_DEVICE_CHECK, "a sequence's length lay outside its rows");
     return EA_OK;
 }
