@@ -52,6 +52,93 @@ __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropArg
     }
 }
 
+// Eight elements as they lie in memory, in accesses of 16 bytes, or of 32 for binary32.
+template <class T>
+struct alignas(8 * sizeof(T)) Eight {
+    T x[8];
+};
+__device__ __forceinline__ Eight<float> load_eight(const float *p)
+{
+    Eight<float> r;
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(r.x[0]), "=f"(r.x[1]), "=f"(r.x[2]), "=f"(r.x[3]), "=f"(r.x[4]), "=f"(r.x[5]), "=f"(r.x[6]), "=f"(r.x[7])
+                 : "l"(p)
+                 : "memory");
+    return r;
+}
+template <class T>
+__device__ __forceinline__ Eight<T> load_eight(const T *p)
+{
+    return *reinterpret_cast<const Eight<T> *>(p);
+}
+__device__ __forceinline__ void store_eight(float *p, const float (&x)[8])
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]),
+                 "f"(x[6]), "f"(x[7])
+                 : "memory");
+}
+__device__ __forceinline__ void store_eight(bf16 *p, const float (&x)[8])
+{
+    Eight<bf16> r;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) *reinterpret_cast<__nv_bfloat162 *>(r.x + i) = __floats2bfloat162_rn(x[i], x[i + 1]);
+    *reinterpret_cast<Eight<bf16> *>(p) = r;
+}
+__device__ __forceinline__ void store_eight(f16 *p, const float (&x)[8])
+{
+    Eight<f16> r;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) *reinterpret_cast<__half2 *>(r.x + i) = __floats2half2_rn(x[i], x[i + 1]);
+    *reinterpret_cast<Eight<f16> *>(p) = r;
+}
+
+constexpr int kDropUnroll = 2;
+
+// Rows that are whole blocks of eight, each on its boundary, `packs` of them a row (0: all in one); limit below 2^16.  The
+// random words are formed while the loads are on their way.
+template <class X, class Y, bool ADD>
+__global__ void __launch_bounds__(kDropThreads) dropout_packs_kernel(const DropArgs a, const Rows packs, const RowsOf<const X> xs, const RowsOf<const Y> adds,
+                                                                     const RowsOf<Y> ys)
+{
+    const uint2 counter = drop_counter(a);
+    const int64_t blocks = a.n / kDropVec, stride = static_cast<int64_t>(gridDim.x) * (kDropThreads * kDropUnroll);
+    const uint32_t limit = a.limit << 16;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * (kDropThreads * kDropUnroll) + threadIdx.x; first < blocks; first += stride) {
+        Eight<X> x[kDropUnroll];
+        Eight<Y> add[kDropUnroll];
+        Y *to[kDropUnroll];
+#pragma unroll
+        for (int k = 0; k < kDropUnroll; ++k) {
+            const int64_t q = first + k * kDropThreads;
+            if (q >= blocks) break;
+            uint32_t r = 0;
+            int64_t column = q * kDropVec;
+            if (packs.inner) {
+                r = packs.outer_of(static_cast<uint32_t>(q));
+                column = static_cast<int64_t>(static_cast<uint32_t>(q) - r * packs.inner) * kDropVec;
+            }
+            x[k] = load_eight(xs.row(a.rows, r) + column);
+            if constexpr (ADD) add[k] = load_eight(adds.row(a.rows, r) + column);
+            to[k] = ys.row(a.rows, r) + column;
+        }
+#pragma unroll
+        for (int k = 0; k < kDropUnroll; ++k) {
+            const int64_t q = first + k * kDropThreads;
+            if (q >= blocks) break;
+            const uint4 w = drop_words(a, q, counter);
+            const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool kept = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) >= limit;
+                y[i] = kept ? __fmul_rn(to_f32(x[k].x[i]), a.scale) : 0.0f;
+                if constexpr (ADD) y[i] = __fadd_rn(y[i], to_f32(add[k].x[i]));
+            }
+            store_eight(to[k], y);
+        }
+    }
+}
+
 }  // namespace ea
 
 using namespace ea;
@@ -65,6 +152,14 @@ struct ea_dropout {
 };
 
 namespace {
+
+constexpr int kDropCtasPerSm = 8;
+
+// Whether a tensor's rows lie one behind another.
+bool follows(const ea_dropout_call *c, int64_t outer, int64_t inner)
+{
+    return (c->inner <= 1 || inner == c->dim) && (c->outer <= 1 || outer == c->inner * c->dim);
+}
 
 int validate(const ea_dropout_config *cfg)
 {
@@ -144,8 +239,22 @@ int ea_dropout_apply(ea_dropout *h, const ea_dropout_call *c, const void *x, con
         const RowsOf<const X> xs{static_cast<const X *>(x), c->x_outer, one ? c->x_outer : c->x_inner};
         const RowsOf<const Y> adds{static_cast<const Y *>(add), c->add_outer, one ? c->add_outer : c->add_inner};
         const RowsOf<Y> ys{static_cast<Y *>(y), c->y_outer, one ? c->y_outer : c->y_inner};
-        const int64_t ctas = over<int64_t>(over<int64_t>(a.n, kDropVec), kDropThreads);
-        dropout_any_kernel<X, Y><<<static_cast<unsigned>(std::min<int64_t>(ctas, h->dev.sms * 8)), kDropThreads, 0, h->stream>>>(a, xs, adds, ys);
+        // all rows one behind another are one row
+        const bool flat = follows(c, c->x_outer, c->x_inner) && follows(c, c->y_outer, c->y_inner) && (!add || follows(c, c->add_outer, c->add_inner));
+        const int64_t dim = flat ? a.n : a.dim, outer = flat ? 1 : c->outer, inner = flat ? 1 : c->inner, blocks = over<int64_t>(a.n, kDropVec);
+        auto whole = [&](const void *p, int32_t type, int64_t o, int64_t i) { return rows_on(8 * type_bytes(type), p, type, dim, outer, inner, o, i); };
+        const bool wide = whole(x, c->x_type, c->x_outer, c->x_inner) && whole(y, c->y_type, c->y_outer, c->y_inner) &&
+                          (!add || whole(add, c->y_type, c->add_outer, c->add_inner));
+        if (wide && (flat || (blocks < kMaxRows && dim > kDropVec)) && a.limit < 65536) {
+            if (flat) a.rows = Rows{};
+            const Rows packs = flat ? Rows{} : rows_of(dim / kDropVec);
+            const int64_t ctas = std::min<int64_t>(over<int64_t>(blocks, kDropThreads * kDropUnroll), h->dev.sms * kDropCtasPerSm);
+            auto kernel = add ? dropout_packs_kernel<X, Y, true> : dropout_packs_kernel<X, Y, false>;
+            kernel<<<static_cast<unsigned>(ctas), kDropThreads, 0, h->stream>>>(a, packs, xs, adds, ys);
+            return;
+        }
+        const int64_t ctas = over<int64_t>(blocks, kDropThreads);
+        dropout_any_kernel<X, Y><<<static_cast<unsigned>(std::min<int64_t>(ctas, h->dev.sms * kDropCtasPerSm)), kDropThreads, 0, h->stream>>>(a, xs, adds, ys);
     });
     return lm_cuda(cudaGetLastError(), "launch");
 }
