@@ -20,12 +20,12 @@ from __future__ import annotations
 
 import torch
 
-from . import EA_E_INVAL, _check  # noqa: F401
+from . import _check
 from .block_abi import (ea_dropout_call, ea_dropout_config, ea_layernorm_call, ea_layernorm_config, ea_scan_call,
                         ea_scan_config)
 from .lm import _C, _TOKEN, _TYPE, _Handle, _refuse
 
-_F32 = torch.float32
+_F32, _Tensor, _ROWS = torch.float32, torch.Tensor, torch.contiguous_format
 
 
 def _type(dtype, what) -> int:
@@ -36,44 +36,57 @@ def _type(dtype, what) -> int:
 
 
 class _Block(_Handle):
-    """What the three share: checks of rows."""
+    """What the three share: checks of rows, and calls that name their tensors only where another stream needs them."""
 
     def _read(self, t, shape, what):
         """(t or a copy of it, its outer stride, its inner stride) for a tensor of rows that is read."""
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
         if t.shape != shape:
             _refuse(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
-        n = t.dim()
-        if n > 3:
-            t = t.contiguous()
-            return t, 0, t.shape[-1]
         stride = t.stride()
-        if n and stride[-1] != 1 and t.shape[-1] > 1:
+        n = len(stride)
+        if n == 3 and stride[2] == 1:
+            return t, stride[0], stride[1]
+        if n > 3:
+            return t.contiguous(), 0, shape[-1]
+        if n and stride[-1] != 1 and shape[-1] > 1:
             t = t.contiguous()
             stride = t.stride()
         return t, stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0
 
     def _written(self, t, shape, dtype, what):
-        """The same for one that is written."""
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        """(Its outer stride, its inner stride) for one that is written."""
+        if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
         if t.shape != shape:
             _refuse(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
         if t.dtype != dtype:
             _refuse(f"{what} is {t.dtype}, not {dtype}")
-        n, stride = t.dim(), t.stride()
-        if n > 3 and not t.is_contiguous() or n and stride[-1] != 1 and t.shape[-1] > 1:
+        stride = t.stride()
+        n = len(stride)
+        if n == 3 and stride[2] == 1:
+            return stride[0], stride[1]
+        if n > 3 and not t.is_contiguous() or n and stride[-1] != 1 and shape[-1] > 1:
             _refuse(f"the rows of {what} are not contiguous")
-        return (0, t.shape[-1]) if n > 3 else (stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0)
+        return (0, shape[-1]) if n > 3 else (stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0)
 
     def _values(self, t, shape, dtype, what) -> int:
         """The address of contiguous values of one type."""
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
         if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
             _refuse(f"{what} is not a contiguous tensor {tuple(shape)} of {dtype}")
         return t.data_ptr()
+
+    def _run(self, f, args, tensors) -> None:
+        """As _call; `tensors` may hold None."""
+        if (self._only or _C._cuda_getDevice() == self._index) and _C._cuda_getCurrentRawStream(self._index) == self._raw:
+            status = f(self.h, *args)
+        else:
+            status = self._call_from_elsewhere(f, args, [t for t in tensors if t is not None])
+        if status:
+            _check(status)
 
 
 def _counts(shape):
@@ -105,48 +118,56 @@ class LayerNorm(_Block):
         self._open(ea_layernorm_config(self.dim, self.max_rows, self.eps), stream, device)
 
     def _x(self, x):
-        if not isinstance(x, torch.Tensor) or x.device != self.device:
+        if not isinstance(x, _Tensor) or x.device != self.device:
             self._on_device(x, "x")
         shape, c = x.shape, self._c
         if not shape or shape[-1] != self.dim:
             _refuse(f"x is {tuple(shape)}: its rows are not {self.dim} long")
-        c.outer, c.inner = _counts(shape)
-        c.x_type = _type(x.dtype, "x")
-        x, c.x_outer, c.x_inner = self._read(x, shape, "x")
+        c.x_type = _TYPE.get(x.dtype) or _type(x.dtype, "x")
+        stride = x.stride()
+        if len(shape) == 3 and stride[2] == 1:
+            c.outer, c.inner = shape[0], shape[1]
+            c.x_outer, c.x_inner = stride[0], stride[1]
+        else:
+            c.outer, c.inner = _counts(shape)
+            x, c.x_outer, c.x_inner = self._read(x, shape, "x")
         return x
 
     def _weight(self, t, dtype, what):
         """The address of a weight (None: 0)."""
         if t is None:
             return None
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
-        if dtype is not None and t.dtype != dtype:
-            _refuse(f"{what} is {t.dtype}, the other one {dtype}")
-        self._c.weight_type = _type(t.dtype, what)
-        return self._values(t, self._row, t.dtype, what)
+        own = t.dtype
+        if dtype is not None and own != dtype:
+            _refuse(f"{what} is {own}, the other one {dtype}")
+        self._c.weight_type = _TYPE.get(own) or _type(own, what)
+        if t.shape != self._row or not t.is_contiguous():
+            _refuse(f"{what} is not a contiguous tensor of {self.dim}")
+        return t.data_ptr()
 
     def forward(self, x, weight=None, bias=None, out=None, dtype=None, stats=None):
         """(y, stats): y of x's shape in `dtype` (default: x's) or in `out` (which may be x); stats, of shape
         x.shape[:-1] + (2,), each row's mean and 1 / sqrt(variance + eps), which grad takes, or into `stats`."""
-        given = [t for t in (out, stats) if t is not None]
+        given = None if out is None and stats is None else [t for t in (out, stats) if t is not None]
         shape, x = getattr(x, "shape", None), self._x(x)
         c = self._c
         w = self._weight(weight, None, "weight")
         b = self._weight(bias, weight.dtype if w is not None else None, "bias")
         if out is None:
-            out = torch.empty(shape, dtype=dtype or x.dtype, device=self.device)
-            c.y_outer, c.y_inner = (c.inner * self.dim, self.dim)
+            kind = dtype or x.dtype
+            c.y_type = _TYPE.get(kind) or _type(kind, "out")
+            out = torch.empty_like(x, dtype=kind, memory_format=_ROWS)
+            c.y_outer, c.y_inner = c.inner * self.dim, self.dim
         else:
             c.y_outer, c.y_inner = self._written(out, shape, dtype or getattr(out, "dtype", None), "out")
-        c.y_type = _type(out.dtype, "out")
-        pairs = torch.Size((*shape[:-1], 2))
+            c.y_type = _type(out.dtype, "out")
         if stats is None:
-            stats = torch.empty(pairs, dtype=_F32, device=self.device)
+            stats = x.new_empty((*shape[:-1], 2), dtype=_F32)
         else:
-            self._values(stats, pairs, _F32, "stats")
-        self._call(self._L.ea_layernorm_forward, (c, x.data_ptr(), w, b, out.data_ptr(), stats.data_ptr()),
-                   [t for t in (x, weight, bias, out, stats) if t is not None])
+            self._values(stats, (*shape[:-1], 2), _F32, "stats")
+        self._run(self._L.ea_layernorm_forward, (c, x.data_ptr(), w, b, out.data_ptr(), stats.data_ptr()), (x, weight, bias, out, stats))
         if given:
             _C._increment_version(given)
         return out, stats
@@ -157,7 +178,7 @@ class LayerNorm(_Block):
             return None
         if t is True:
             return torch.empty(self._row, dtype=_F32, device=self.device)
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
         self._values(t, self._row, t.dtype, what)
         return t
@@ -167,14 +188,14 @@ class LayerNorm(_Block):
         that are added to dx (the gradient that passes the block by).  dx: into `out` (which may be dy, x or add) or new.
         dw, db: None (not computed), True (new, in 32 bits) or tensors of one type that are written to or, with accumulate, added
         to."""
-        given = [t for t in (out, dw, db) if isinstance(t, torch.Tensor)]
+        given = [t for t in (out, dw, db) if isinstance(t, _Tensor)]
         if accumulate and (dw is True or db is True):
             _refuse("accumulate needs dw's and db's tensors")
         shape, x = getattr(x, "shape", None), self._x(x)
         c = self._c
         dy, c.y_outer, c.y_inner = self._read(dy, shape, "dy")
         c.y_type = _type(dy.dtype, "dy")
-        at = self._values(stats, torch.Size((*shape[:-1], 2)), _F32, "stats")
+        at = self._values(stats, (*shape[:-1], 2), _F32, "stats")
         w = self._weight(weight, None, "weight")
         if add is not None:
             add, c.add_outer, c.add_inner = self._read(add, shape, "add")
@@ -187,14 +208,14 @@ class LayerNorm(_Block):
             if t is not None:
                 c.grad_type = _type(t.dtype, "a weight's gradient")
         if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=self.device)
+            out = torch.empty_like(x, memory_format=_ROWS)
             c.dx_outer, c.dx_inner = c.inner * self.dim, self.dim
         else:
             c.dx_outer, c.dx_inner = self._written(out, shape, x.dtype, "out")
-        self._call(self._L.ea_layernorm_backward,
-                   (c, dy.data_ptr(), x.data_ptr(), at, w, None if add is None else add.data_ptr(), out.data_ptr(),
-                    None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), int(accumulate)),
-                   [t for t in (dy, x, stats, weight, add, out, dw, db) if t is not None])
+        self._run(self._L.ea_layernorm_backward,
+                  (c, dy.data_ptr(), x.data_ptr(), at, w, None if add is None else add.data_ptr(), out.data_ptr(),
+                   None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), int(accumulate)),
+                  (dy, x, stats, weight, add, out, dw, db))
         if given:
             _C._increment_version(given)
         return out, dw, db
@@ -212,7 +233,7 @@ class GatedScan(_Block):
         self._open(ea_scan_config(self.dim), stream, device)
 
     def _begin(self, z, lengths):
-        if not isinstance(z, torch.Tensor) or z.device != self.device:
+        if not isinstance(z, _Tensor) or z.device != self.device:
             self._on_device(z, "z")
         if z.dim() != 3 or z.shape[2] != self.dim:
             _refuse(f"z is {tuple(z.shape)}, not (batch, length, {self.dim})")
@@ -221,7 +242,7 @@ class GatedScan(_Block):
         c.type = _type(z.dtype, "z")
         if lengths is None:
             return None
-        if not isinstance(lengths, torch.Tensor) or lengths.device != self.device:
+        if not isinstance(lengths, _Tensor) or lengths.device != self.device:
             self._on_device(lengths, "lengths")
         kind = _TOKEN.get(lengths.dtype)
         if kind is None:
@@ -241,7 +262,7 @@ class GatedScan(_Block):
         """(tensor or None, its address or None) of states that are read, or written: None or False, True for a new one."""
         if t is None or t is False:
             return None, None
-        shape = torch.Size((self._c.batch, self.dim))
+        shape = (self._c.batch, self.dim)
         if t is True:
             t = torch.empty(shape, dtype=_F32, device=self.device)
             return t, t.data_ptr()
@@ -252,7 +273,7 @@ class GatedScan(_Block):
         row (None: zeros).  lengths: of the sequences (int32 or int64 on the device; None: all rows): rows behind them get zeros,
         and the state stays as it was.  final: None, True (a new tensor) or a tensor (which may be initial) that receives
         the states after the last rows.  A length outside [0, length] counts as the nearest of the two, and sync() raises for it."""
-        given = [t for t in (out, final) if isinstance(t, torch.Tensor)]
+        given = [t for t in (out, final) if isinstance(t, _Tensor)]
         c, n = self._c, self._begin(z, lengths)
         shape = z.shape
         z, c.z_batch, c.z_row = self._read(z, shape, "z")
@@ -260,33 +281,44 @@ class GatedScan(_Block):
         initial, first = self._state(initial, "initial")
         final, last = self._state(final, "final")
         if out is None:
-            out = torch.empty(shape, dtype=z.dtype, device=self.device)
+            out = torch.empty_like(z, memory_format=_ROWS)
             c.h_batch, c.h_row = shape[1] * self.dim, self.dim
         else:
             c.h_batch, c.h_row = self._written(out, shape, z.dtype, "out")
-        self._call(self._L.ea_scan_forward,
-                   (c, z.data_ptr(), v.data_ptr(), first, None if n is None else n.data_ptr(), out.data_ptr(), last),
-                   [t for t in (z, v, initial, n, out, final) if t is not None])
+        self._run(self._L.ea_scan_forward, (c, z.data_ptr(), v.data_ptr(), first, None if n is None else n.data_ptr(), out.data_ptr(), last),
+                  (z, v, initial, n, out, final))
         if given:
             _C._increment_version(given)
         return out, final
 
     def step(self, z, v, state, out=None):
         """One row each of the sequences: z and v of shape (batch, dim).  Updates state (float32) in place and returns h."""
-        if not isinstance(z, torch.Tensor) or not isinstance(v, torch.Tensor) or z.dim() != 2 or v.dim() != 2:
-            _refuse("z and v are (batch, dim)")
-        if out is not None and (not isinstance(out, torch.Tensor) or out.dim() != 2):
-            _refuse("out is (batch, dim)")
-        if not isinstance(state, torch.Tensor):
-            _refuse("state is not a tensor")
-        h, _ = self.forward(z[:, None], v[:, None], initial=state, out=None if out is None else out[:, None], final=state)
-        return h[:, 0] if out is None else out
+        if not isinstance(z, _Tensor) or z.device != self.device:
+            self._on_device(z, "z")
+        shape, c, given = z.shape, self._c, out is not None
+        if len(shape) != 2 or shape[1] != self.dim:
+            _refuse(f"z is {tuple(shape)}, not (batch, {self.dim})")
+        kind = z.dtype
+        c.type = _TYPE.get(kind) or _type(kind, "z")
+        c.batch, c.length = shape[0], 1
+        z, _, c.z_batch = self._read(z, shape, "z")
+        v, _, c.v_batch = self._rows(v, z, "v")
+        at = self._values(state, shape, _F32, "state")
+        if not given:
+            out = torch.empty_like(z, memory_format=_ROWS)
+            c.h_batch = self.dim
+        else:
+            _, c.h_batch = self._written(out, shape, kind, "out")
+        c.z_row = c.v_row = c.h_row = self.dim
+        self._run(self._L.ea_scan_forward, (c, z.data_ptr(), v.data_ptr(), at, None, out.data_ptr(), at), (z, v, state, out))
+        _C._increment_version((out, state) if given else (state,))
+        return out
 
     def grad(self, dh, z, v, h, initial=None, lengths=None, d_final=None, dz=None, dv=None, d_initial=None):
         """(dz, dv, d_initial) from dh = the gradient of forward's h and d_final = that of its final states (None: zeros), with
         its z, v, h, initial and lengths.  dz (which may be z or dh) and dv (v or dh) are written to, or new.  d_initial: None,
         True (a new tensor) or a tensor (which may be d_final)."""
-        given = [t for t in (dz, dv, d_initial) if isinstance(t, torch.Tensor)]
+        given = [t for t in (dz, dv, d_initial) if isinstance(t, _Tensor)]
         c, n = self._c, self._begin(z, lengths)
         shape = z.shape
         z, c.z_batch, c.z_row = self._read(z, shape, "z")
@@ -297,19 +329,19 @@ class GatedScan(_Block):
         d_final, last = self._state(d_final, "d_final")
         d_initial, d_first = self._state(d_initial, "d_initial")
         if dz is None:
-            dz = torch.empty(shape, dtype=z.dtype, device=self.device)
+            dz = torch.empty_like(z, memory_format=_ROWS)
             c.dz_batch, c.dz_row = shape[1] * self.dim, self.dim
         else:
             c.dz_batch, c.dz_row = self._written(dz, shape, z.dtype, "dz")
         if dv is None:
-            dv = torch.empty(shape, dtype=z.dtype, device=self.device)
+            dv = torch.empty_like(z, memory_format=_ROWS)
             c.dv_batch, c.dv_row = shape[1] * self.dim, self.dim
         else:
             c.dv_batch, c.dv_row = self._written(dv, shape, z.dtype, "dv")
-        self._call(self._L.ea_scan_backward,
-                   (c, dh.data_ptr(), z.data_ptr(), v.data_ptr(), h.data_ptr(), first, None if n is None else n.data_ptr(), last,
-                    dz.data_ptr(), dv.data_ptr(), d_first),
-                   [t for t in (dh, z, v, h, initial, n, d_final, dz, dv, d_initial) if t is not None])
+        self._run(self._L.ea_scan_backward,
+                  (c, dh.data_ptr(), z.data_ptr(), v.data_ptr(), h.data_ptr(), first, None if n is None else n.data_ptr(), last,
+                   dz.data_ptr(), dv.data_ptr(), d_first),
+                  (dh, z, v, h, initial, n, d_final, dz, dv, d_initial))
         if given:
             _C._increment_version(given)
         return dz, dv, d_initial
@@ -341,7 +373,7 @@ class Dropout(_Block):
         the residual's type, or x's) or into `out` (which may be x or residual).  x and the result are of one type, or one of them
         float32; residual is of the result's."""
         c, given = self._c, out is not None
-        if not isinstance(x, torch.Tensor) or x.device != self.device:
+        if not isinstance(x, _Tensor) or x.device != self.device:
             self._on_device(x, "x")
         shape = x.shape
         if not shape:
@@ -358,11 +390,11 @@ class Dropout(_Block):
                 _refuse(f"residual is {residual.dtype}, the result {dtype}")
         c.y_type = _type(dtype, "the result")
         if not given:
-            out = torch.empty(shape, dtype=dtype, device=self.device)
+            out = torch.empty_like(x, dtype=dtype, memory_format=_ROWS)
             c.y_outer, c.y_inner = c.inner * c.dim, c.dim
         else:
             c.y_outer, c.y_inner = self._written(out, shape, dtype, "out")
-        if isinstance(counter, torch.Tensor):
+        if isinstance(counter, _Tensor):
             if counter.device != self.device or counter.dtype != torch.int64 or counter.numel() != 1:
                 _refuse(f"counter is an integer or an int64 tensor of one value on {self.device}")
             number, at = 0, counter.data_ptr()
@@ -370,9 +402,8 @@ class Dropout(_Block):
             number, at = int(counter), None
             if not 0 <= number < 1 << 64:
                 _refuse("counter is outside [0, 2^64)")
-        self._call(self._L.ea_dropout_apply,
-                   (c, x.data_ptr(), None if residual is None else residual.data_ptr(), number, at, out.data_ptr()),
-                   [t for t in (x, residual, out, counter if at is not None else None) if t is not None])
+        self._run(self._L.ea_dropout_apply, (c, x.data_ptr(), None if residual is None else residual.data_ptr(), number, at, out.data_ptr()),
+                  (x, residual, out, counter if at is not None else None))
         if given:
             _C._increment_version((out,))
         return out

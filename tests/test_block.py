@@ -151,7 +151,7 @@ def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
     seen("ea_layernorm_backward", 8, lambda: norm.grad(x, x, stats, w, add=x, dw=True, db=True))
     scan, z, state = handle(block.GatedScan, dim=4, _c=A.ea_scan_call()), torch.ones(2, 3, 4), torch.ones(2, 4)
     seen("ea_scan_forward", 6, lambda: scan.forward(z, z, initial=state, lengths=torch.tensor([1, 2]), final=True))
-    seen("ea_scan_forward", 5, lambda: scan.step(z[:, 0], z[:, 0], state))
+    seen("ea_scan_forward", 4, lambda: scan.step(z[:, 0], z[:, 0], state))
     seen("ea_scan_backward", 10, lambda: scan.grad(z, z, z, z, initial=state, lengths=torch.tensor([1, 2]), d_final=state, d_initial=True))
     drop = handle(block.Dropout, _c=A.ea_dropout_call())
     seen("ea_dropout_apply", 4, lambda: drop(x, torch.tensor([5]), residual=x))
