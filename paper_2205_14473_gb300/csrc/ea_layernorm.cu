@@ -145,6 +145,16 @@ __global__ void __launch_bounds__(kColumnLanes *kColumnRows) ln_join_kernel(cons
 // ---------------------------------------------------------------------------------------------- rows in registers
 constexpr int kHeld = 16;                // elements of a thread
 constexpr int kBackThreads = 512;
+constexpr int kForwardDepth = 4;         // rows on their way
+// Of the gradient: what 192 KB hold of x, dy and the added rows.
+template <class X, class Y>
+constexpr int kBackDepth = 192 * 1024 / (kBackThreads * kHeld * (2 * static_cast<int>(sizeof(X)) + static_cast<int>(sizeof(Y))));
+
+// An 8-byte asynchronous copy global -> shared.
+__device__ __forceinline__ void cp_async8(void *dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
 
 // A thread's 16 elements of a row: packs of VEC, pack k of lane l of a group of G being pack l + k G of the row.
 template <class T, int VEC>
@@ -155,6 +165,29 @@ struct Held {
     static constexpr int kPacks = kHeld / VEC;
     Pack p[kPacks];
 
+    // Packs k of a row on their way to `slots` (one of them to every kStep-th), none of those outside the row.
+    template <int G, int kStep>
+    static __device__ __forceinline__ void fetch(Pack *slots, const T *row, int lane, int packs)
+    {
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k)
+            if (lane + k * G < packs) {
+                if constexpr (sizeof(Pack) == 16) cp_async16(slots + k * kStep, row + (lane + k * G) * VEC);
+                else cp_async8(slots + k * kStep, row + (lane + k * G) * VEC);
+            }
+    }
+    template <int kStep>
+    static __device__ __forceinline__ void clear(Pack *slots)
+    {
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) slots[k * kStep] = Pack{};
+    }
+    template <int kStep>
+    __device__ __forceinline__ void take(const Pack *slots)
+    {
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) p[k] = slots[k * kStep];
+    }
     template <int G>
     __device__ __forceinline__ void load(const T *row, int lane, int packs)
     {
@@ -245,15 +278,31 @@ __device__ __forceinline__ void group_sync(int group)
 template <class X, class Y, int VEC, int G>
 __global__ void __launch_bounds__(G > 32 ? G : 128) ln_forward_kernel(const LnArgs a, const RowsOf<const X> xs, const RowsOf<Y> ys, float *stats)
 {
-    constexpr int kThreads = G > 32 ? G : 128, kGroups = kThreads / G, W = G / 32;
+    constexpr int kThreads = G > 32 ? G : 128, kGroups = kThreads / G, W = G / 32, kDepth = kForwardDepth;
+    constexpr bool kRing = VEC > 1;
+    using H = Held<X, VEC>;
+    using Pack = typename H::Pack;
+    extern __shared__ __align__(16) unsigned char memory[];
+    Pack *ring = reinterpret_cast<Pack *>(memory) + threadIdx.x;  // a stage: kPacks, one per thread each
     __shared__ float2 parts[2][W > 1 ? W : 1];  // each warp's mean and squares about it, of this row and the last
     __shared__ float share[W > 1 ? W : 1], counts[W > 1 ? W : 1];  // each warp's elements, and their share of the row's
     const int lane = threadIdx.x % G, packs = static_cast<int>(a.dim / VEC), warp = threadIdx.x / 32;
     const uint32_t stride = gridDim.x * kGroups;
     uint32_t r = blockIdx.x * kGroups + threadIdx.x / G;
     F2 w[kHeld / 2], b[kHeld / 2];
-    Held<X, VEC> next;
-    if (r < a.n) next.template load<G>(xs.row(a.rows, r), lane, packs);
+    H next;
+    auto fetch = [&](uint32_t row, int stage) {
+        if constexpr (kRing) {
+            if (row < a.n) H::template fetch<G, kThreads>(ring + stage * (H::kPacks * kThreads), xs.row(a.rows, row), lane, packs);
+            cp_async_commit();
+        } else {
+            next.template load<G>(xs.row(a.rows, row), lane, row < a.n ? packs : 0);
+        }
+    };
+    if constexpr (kRing)
+        for (int d = 0; d < kDepth; ++d) H::template clear<kThreads>(ring + d * (H::kPacks * kThreads));
+    for (int d = 0; d < (kRing ? kDepth : 1); ++d) fetch(r + d * stride, d);
+    int stage = 0;
     load_weight<VEC, G>(a.w, a.weight_type, lane, packs, 1.0f, w);
     load_weight<VEC, G>(a.b, a.weight_type, lane, packs, 0.0f, b);
     // elements of this thread's warp (or group), of the packs that lie inside the row
@@ -273,8 +322,13 @@ __global__ void __launch_bounds__(G > 32 ? G : 128) ln_forward_kernel(const LnAr
     // whole warps go on until all of their rows are done
     for (uint32_t first = r - (G < 32 ? threadIdx.x % 32 / G : 0); first < a.n; first += stride, r += stride, buffer ^= 1) {
         F2 x[kHeld / 2];
+        if constexpr (kRing) {
+            cp_async_wait<kDepth - 1>();
+            next.template take<kThreads>(ring + stage * (H::kPacks * kThreads));
+        }
         next.values(x);
-        if (r + stride < a.n && r + stride >= r) next.template load<G>(xs.row(a.rows, r + stride), lane, packs);
+        fetch(r + (kRing ? kDepth : 1) * stride, stage);
+        stage = stage + 1 == kDepth ? 0 : stage + 1;
         F2 s = x[0];
 #pragma unroll
         for (int i = 1; i < kHeld / 2; ++i) s = add2(s, x[i]);
@@ -328,37 +382,66 @@ template <class X, class Y, int VEC, int G>
 __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnArgs a, const RowsOf<const Y> dys, const RowsOf<const X> xs, const float *stats,
                                                                       const RowsOf<const X> adds, const RowsOf<X> dxs, float *partial)
 {
-    constexpr int kGroups = kBackThreads / G, W = G / 32;
-    constexpr bool kAhead = sizeof(X) == 2 && VEC > 1;  // registers hold the next row too
-    extern __shared__ __align__(16) float sums[];  // at the end: each group's dw, then its db
+    constexpr int kGroups = kBackThreads / G, W = G / 32, T = kBackThreads, kDepth = kBackDepth<X, Y>;
+    constexpr bool kRing = VEC > 1;
+    using HX = Held<X, VEC>;
+    using HY = Held<Y, VEC>;
+    extern __shared__ __align__(16) unsigned char memory[];
+    float *sums = reinterpret_cast<float *>(memory);  // at the end: each group's dw, then its db
+    // A stage: packs of x, of dy and of the added rows, one per thread each.
+    typename HX::Pack *ring_x = reinterpret_cast<typename HX::Pack *>(memory) + threadIdx.x, *ring_add = ring_x + kDepth * HX::kPacks * T;
+    typename HY::Pack *ring_y = reinterpret_cast<typename HY::Pack *>(memory + 2 * sizeof(X) * kHeld * T * kDepth) + threadIdx.x;
     __shared__ float2 parts[2][kBackThreads / 32];
     const int lane = threadIdx.x % G, group = threadIdx.x / G, packs = static_cast<int>(a.dim / VEC), warp = threadIdx.x / 32;
     const uint32_t stride = gridDim.x * kGroups;
     uint32_t r = blockIdx.x * kGroups + group;
     F2 w[kHeld / 2], dw[kHeld / 2], db[kHeld / 2];
-    Held<X, VEC> nx, na;
-    Held<Y, VEC> ny;
-    float2 st = make_float2(0.0f, 0.0f);
-    auto fetch = [&](uint32_t row) {  // zeros where there is no such row
-        const int there = row < a.n ? packs : 0;
-        nx.template load<G>(xs.row(a.rows, row), lane, there);
-        ny.template load<G>(dys.row(a.rows, row), lane, there);
-        st = row < a.n ? *reinterpret_cast<const float2 *>(stats + 2 * static_cast<int64_t>(row)) : make_float2(0.0f, 0.0f);
+    HX nx, na;
+    HY ny;
+    float2 st[kRing ? kDepth : 1];  // of the rows on their way
+    auto fetch = [&](uint32_t row, int stage, float2 &s) {  // zeros where there is no such row
+        s = row < a.n ? *reinterpret_cast<const float2 *>(stats + 2 * static_cast<int64_t>(row)) : make_float2(0.0f, 0.0f);
+        if constexpr (kRing) {
+            if (row < a.n) {
+                HX::template fetch<G, T>(ring_x + stage * (HX::kPacks * T), xs.row(a.rows, row), lane, packs);
+                HY::template fetch<G, T>(ring_y + stage * (HY::kPacks * T), dys.row(a.rows, row), lane, packs);
+                if (adds.p) HX::template fetch<G, T>(ring_add + stage * (HX::kPacks * T), adds.row(a.rows, row), lane, packs);
+            } else {
+                HX::template clear<T>(ring_x + stage * (HX::kPacks * T));
+                HY::template clear<T>(ring_y + stage * (HY::kPacks * T));
+            }
+            cp_async_commit();
+        } else {
+            const int there = row < a.n ? packs : 0;
+            nx.template load<G>(xs.row(a.rows, row), lane, there);
+            ny.template load<G>(dys.row(a.rows, row), lane, there);
+        }
     };
-    if (kAhead) fetch(r);
+    if constexpr (kRing)
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            HX::template clear<T>(ring_x + d * (HX::kPacks * T));
+            HY::template clear<T>(ring_y + d * (HY::kPacks * T));
+            HX::template clear<T>(ring_add + d * (HX::kPacks * T));
+            fetch(r + d * stride, d, st[d]);
+        }
     load_weight<VEC, G>(a.w, a.weight_type, lane, packs, 1.0f, w);
 #pragma unroll
     for (int i = 0; i < kHeld / 2; ++i) dw[i] = db[i] = both(0.0f);
-    int buffer = 0;
+    int buffer = 0, stage = 0;
     for (uint32_t first = r - (G < 32 ? threadIdx.x % 32 / G : 0); first < a.n; first += stride, r += stride, buffer ^= 1) {
         const bool on = r < a.n;
-        if (!kAhead) fetch(r);
         F2 t[kHeld / 2], q[kHeld / 2];
-        const F2 minus = both(-st.x), scale = both(st.y);
+        if constexpr (kRing) {
+            cp_async_wait<kDepth - 1>();
+            nx.template take<T>(ring_x + stage * (HX::kPacks * T));
+            ny.template take<T>(ring_y + stage * (HY::kPacks * T));
+        } else {
+            fetch(r, 0, st[0]);
+        }
+        const F2 minus = both(-st[0].x), scale = both(st[0].y);
         nx.values(t);
         ny.values(q);
-        if (kAhead && adds.p) na.template load<G>(adds.row(a.rows, r), lane, on ? packs : 0);
-        if (kAhead) fetch(r + stride);
 #pragma unroll
         for (int i = 0; i < kHeld / 2; ++i) {
             t[i] = times2(add2(t[i], minus), scale);
@@ -366,8 +449,17 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
             db[i] = add2(db[i], q[i]);
             q[i] = times2(q[i], w[i]);
         }
+        if (adds.p) {
+            if constexpr (kRing) na.template take<T>(ring_add + stage * (HX::kPacks * T));
+            else na.template load<G>(adds.row(a.rows, r), lane, on ? packs : 0);
+        }
+        if constexpr (kRing) {
+#pragma unroll
+            for (int d = 0; d + 1 < kDepth; ++d) st[d] = st[d + 1];
+            fetch(r + kDepth * stride, stage, st[kDepth - 1]);
+            stage = stage + 1 == kDepth ? 0 : stage + 1;
+        }
         if (!dxs.p) continue;
-        if (!kAhead && adds.p) na.template load<G>(adds.row(a.rows, r), lane, on ? packs : 0);
         F2 s2 = q[0], p2 = times2(q[0], t[0]);
 #pragma unroll
         for (int i = 1; i < kHeld / 2; ++i) s2 = add2(s2, q[i]), p2 = fma2(q[i], t[i], p2);
@@ -394,6 +486,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
         if (on) Held<X, VEC>::template store<G>(dxs.row(a.rows, r), lane, packs, t);
     }
     if (!partial) return;
+    cp_async_wait<0>();
+    __syncthreads();  // the sums take the ring's place
     // column c of a row is element c % VEC of pack c / VEC
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
@@ -547,6 +641,7 @@ int ea_layernorm_forward(ea_layernorm *h, const ea_layernorm_call *c, const void
     if (r == EA_OK) r = check_rows_apart(c->outer, c->inner, c->y_outer, c->y_inner, a.dim, "y");
     if (r == EA_OK && stats && reinterpret_cast<uintptr_t>(stats) % 8) r = lm_fail(EA_E_ALIGN, "stats is not aligned to its pairs");
     if (r != EA_OK || a.n == 0) return r;
+    cudaError_t e = cudaSuccess;
     with_pair(c->x_type, c->y_type, [&](auto *xt, auto *yt) {
         using X = std::remove_reference_t<decltype(*xt)>;
         using Y = std::remove_reference_t<decltype(*yt)>;
@@ -564,11 +659,13 @@ int ea_layernorm_forward(ea_layernorm *h, const ea_layernorm_call *c, const void
                 constexpr int G = decltype(group)::value, kThreads = G > 32 ? G : 128;
                 const uint32_t ctas = over<uint32_t>(a.n, kThreads / G), most = h->dev.sms * (kForwardThreads / kThreads);
                 auto kernel = wide ? ln_forward_kernel<X, Y, kVec, G> : ln_forward_kernel<X, Y, 1, G>;
-                kernel<<<std::min(ctas, most), kThreads, 0, h->stream>>>(a, xs, ys, stats);
+                const int ring = wide ? kForwardDepth * kThreads * kHeld * static_cast<int>(sizeof(X)) : 0;
+                if (ring > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring);
+                if (e == cudaSuccess) kernel<<<std::min(ctas, most), kThreads, ring, h->stream>>>(a, xs, ys, stats);
             });
         }
     });
-    return lm_cuda(cudaGetLastError(), "launch");
+    return lm_cuda(e == cudaSuccess ? cudaGetLastError() : e, "launch");
 }
 
 int ea_layernorm_backward(ea_layernorm *h, const ea_layernorm_call *c, const void *dy, const void *x, const float *stats, const void *w,
@@ -622,8 +719,9 @@ int ea_layernorm_backward(ea_layernorm *h, const ea_layernorm_call *c, const voi
                 float *partial = dw || db ? h->partial : nullptr;
                 if (partial) parts = static_cast<int>(ctas);
                 auto kernel = wide ? ln_backward_kernel<X, Y, kVec, G> : ln_backward_kernel<X, Y, 1, G>;
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSumsBytes);
-                if (e == cudaSuccess) kernel<<<ctas, kBackThreads, kSumsBytes, h->stream>>>(a, dys, xs, stats, adds, dxs, partial);
+                const int ring = wide ? kBackDepth<X, Y> * kBackThreads * kHeld * (2 * static_cast<int>(sizeof(X)) + static_cast<int>(sizeof(Y))) : kSumsBytes;
+                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring);
+                if (e == cudaSuccess) kernel<<<ctas, kBackThreads, ring, h->stream>>>(a, dys, xs, stats, adds, dxs, partial);
             });
         }
     });
