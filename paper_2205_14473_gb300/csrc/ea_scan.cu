@@ -12,7 +12,6 @@ namespace ea {
 
 constexpr uint32_t kStatusLength = 8u;  // a length outside [0, length]
 constexpr int kWalkThreads = 128;
-constexpr int kTileThreads = 128;
 constexpr int kMaxCluster = 16;
 
 // A tensor: element 0 of row t of sequence i at p + i * batch + t * row.
@@ -307,26 +306,28 @@ __global__ void __launch_bounds__(kWalkThreads) scan_walk_back_kernel(const Scan
 
 // ---------------------------------------------------------------------------------------------- tiles
 // A thread's V columns are 16 bytes where rows allow it (eight lanes then cover a 128-byte piece of a row), else one element
-// (a warp covers 32 columns).  S: its rows.
-template <class T, int V, int S>
+// (a warp covers 32 columns).  S: its rows.  NT: threads of the CTA.
+template <class T, int V, int S, int NT>
 struct Tile {
+    static constexpr int kThreads = NT;
     static constexpr int kLanes = V == 1 ? 32 : 8;            // lanes across a row
     static constexpr int kColumns = kLanes * V;
     static constexpr int kRows = S;
-    static constexpr int kSegs = kTileThreads / kLanes;       // threads along the rows
+    static constexpr int kSegs = NT / kLanes;       // threads along the rows
     static constexpr int kChunk = kSegs * kRows;              // rows of a CTA in a step
     static constexpr bool kRing = V > 1;                      // rows come through shared memory, else through registers
-    static constexpr int kGroups = kTileThreads / kColumns;   // threads that compose a column's pieces, adjacent lanes
+    static constexpr int kGroups = NT / kColumns;   // threads that compose a column's pieces, adjacent lanes
     static constexpr int kPieces = kSegs / kGroups;           // of each of them
 };
 
 // What a tile's CTA shares, behind its ring of copies.  A piece's columns are turned around within 32 lanes' worth by its group,
 // so that the lanes that read a column's pieces fall into different banks.
-template <class L>
+template <class L, bool CLUSTER>
 struct TileShared {
+    static constexpr int kRanks = CLUSTER ? kMaxCluster : 1;
     uint64_t arrived[2];                                       // barriers of `rank`
     float a[L::kSegs][L::kColumns], b[L::kSegs][L::kColumns];  // each thread's composition, then in b the state it starts with
-    float2 rank[2][kMaxCluster][L::kColumns];                  // the CTAs' compositions, of this step and the last
+    float2 rank[2][kRanks][L::kColumns];                       // the CTAs' compositions, of this step and the last
     static __device__ __forceinline__ int at(int seg, int column) { return column ^ (seg / L::kPieces * (32 / L::kGroups)); }
 };
 
@@ -386,7 +387,7 @@ __device__ __forceinline__ void to_shared(float *p, const Lanes<V> &a)
 // column threadIdx.x / kGroups, and the one after it on return.  A CTA's composition goes to all CTAs of its cluster, into one
 // of two buffers: a CTA sends the next but one after it has waited for the next, which the others send after this one is read.
 template <bool CLUSTER, class L, int V>
-__device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V> &B, float &carry, TileShared<L> &sh, Exchange &x, uint32_t *status)
+__device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V> &B, float &carry, TileShared<L, CLUSTER> &sh, Exchange &x, uint32_t *status)
 {
     constexpr int G = L::kGroups;
     const int seg = threadIdx.x / L::kLanes, c0 = threadIdx.x % L::kLanes * V;
@@ -443,13 +444,13 @@ __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V>
 }
 
 // blockIdx.x: sequence and tile of columns, in clusters along the rows (blockIdx.x / ranks is the tile).
-template <class T, int V, int S, int DEPTH, bool CLUSTER>
-__global__ void __launch_bounds__(kTileThreads) scan_tile_kernel(const ScanArgs a, const Seq<const T> zs, const Seq<const T> vs, const Seq<T> hs, float *final)
+template <class T, int V, int S, int NT, int DEPTH, bool CLUSTER>
+__global__ void __launch_bounds__(NT) scan_tile_kernel(const ScanArgs a, const Seq<const T> zs, const Seq<const T> vs, const Seq<T> hs, float *final)
 {
-    using L = Tile<T, V, S>;
+    using L = Tile<T, V, S, NT>;
     using W = Vec<T, V>;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(16) TileShared<L> sh;
+    __shared__ __align__(16) TileShared<L, CLUSTER> sh;
     Exchange x;
     if constexpr (CLUSTER) x.begin(sh);
     const uint32_t tile = blockIdx.x / x.ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
@@ -457,48 +458,49 @@ __global__ void __launch_bounds__(kTileThreads) scan_tile_kernel(const ScanArgs 
     const int64_t c = c0 + threadIdx.x % L::kLanes * V;
     const bool inside = c < a.dim;
     const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk;
-    const T *z = zs.p + i * zs.batch + c, *v = vs.p + i * vs.batch + c;
-    T *h = hs.p + i * hs.batch + c;
     const int64_t column = c0 + threadIdx.x / L::kGroups;  // of the state that this thread carries
     float carry = column < a.dim && a.initial ? a.initial[i * a.dim + column] : 0.0f;
-    const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;  // this thread's first row
+    // This thread's first row of the step that is fetched, and of the step at hand, as rows that are left from there on.
+    const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;
+    int next = static_cast<int>(n - first), left = next;
+    const int step = static_cast<int>(stride);
+    const T *z = zs.p + (i * zs.batch + first * zs.row + c), *v = vs.p + (i * vs.batch + first * vs.row + c);
+    T *h = hs.p + (i * hs.batch + first * hs.row + c);
     // Rows that are not there have z of infinity and v of 0: the state passes through them.
     const W closed = filled<T, V>(__int_as_float(0x7f800000)), zero = filled<T, V>(0.0f);
     W *ring = reinterpret_cast<W *>(smem) + threadIdx.x;  // a stage: S of z, then S of v, one per thread each
     W zv[S], vv[S];
-    auto fetch = [&](int64_t t, int stage) {
-        const T *from_z = z + t * zs.row, *from_v = v + t * vs.row;
-        if constexpr (L::kRing) {
-            W *to = ring + stage * (2 * S * kTileThreads);
+    auto fetch = [&](int stage) {
+        const T *pz = z, *pv = v;
+        W *to = ring + stage * (2 * S * NT);
 #pragma unroll
-            for (int r = 0; r < S; ++r) {
-                if (inside && t + r < n) {
-                    cp_async16(to + r * kTileThreads, from_z + r * zs.row);
-                    cp_async16(to + (S + r) * kTileThreads, from_v + r * vs.row);
+        for (int r = 0; r < S; ++r, pz += zs.row, pv += vs.row) {
+            const bool on = inside && next > r;
+            if constexpr (L::kRing) {
+                if (on) {
+                    cp_async16(to + r * NT, pz);
+                    cp_async16(to + (S + r) * NT, pv);
                 } else {
-                    to[r * kTileThreads] = closed;
-                    to[(S + r) * kTileThreads] = zero;
+                    to[r * NT] = closed;
+                    to[(S + r) * NT] = zero;
                 }
-            }
-            cp_async_commit();
-        } else {
-#pragma unroll
-            for (int r = 0; r < S; ++r) {
-                const bool on = inside && t + r < n;
-                zv[r] = on ? *reinterpret_cast<const W *>(from_z + r * zs.row) : closed;
-                vv[r] = on ? *reinterpret_cast<const W *>(from_v + r * vs.row) : zero;
+            } else {
+                zv[r] = on ? *reinterpret_cast<const W *>(pz) : closed;
+                vv[r] = on ? *reinterpret_cast<const W *>(pv) : zero;
             }
         }
+        next -= step;
+        z += stride * zs.row, v += stride * vs.row;
+        if constexpr (L::kRing) cp_async_commit();
     };
-    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(first + d * stride, d);
+    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(d);
     int stage = 0;
     for (int64_t base = 0; base < n; base += stride) {
-        const int64_t t = first + base;
         if constexpr (L::kRing) {
             cp_async_wait<DEPTH - 1>();
-            const W *from = ring + stage * (2 * S * kTileThreads);
+            const W *from = ring + stage * (2 * S * NT);
 #pragma unroll
-            for (int r = 0; r < S; ++r) zv[r] = from[r * kTileThreads], vv[r] = from[(S + r) * kTileThreads];
+            for (int r = 0; r < S; ++r) zv[r] = from[r * NT], vv[r] = from[(S + r) * NT];
         }
         Lanes<V> f[S], u[S], A, B;
 #pragma unroll
@@ -509,83 +511,91 @@ __global__ void __launch_bounds__(kTileThreads) scan_tile_kernel(const ScanArgs 
             B = r ? fma(f[r], B, u[r]) : u[r];
             A = r ? f[r] * A : f[r];
         }
-        fetch(t + (L::kRing ? DEPTH : 1) * stride, stage);
+        fetch(stage);
         Lanes<V> state = tile_start<CLUSTER>(A, B, carry, sh, x, a.status);
-        T *to = h + t * hs.row;
-        if (inside)
+        T *to = h;
 #pragma unroll
-            for (int r = 0; r < S; ++r) {
-                state = fma(f[r], state, u[r]);
-                if (t + r < n) *reinterpret_cast<W *>(to + r * hs.row) = rounded<T, V>(state);
-            }
+        for (int r = 0; r < S; ++r, to += hs.row) {
+            state = fma(f[r], state, u[r]);
+            if (inside && left > r) *reinterpret_cast<W *>(to) = rounded<T, V>(state);
+        }
+        left -= step;
+        h += stride * hs.row;
         stage = stage + 1 == DEPTH ? 0 : stage + 1;
     }
     if (inside)
-        for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs) *reinterpret_cast<W *>(h + t * hs.row) = zero;
+        for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs)
+            *reinterpret_cast<W *>(hs.p + (i * hs.batch + t * hs.row + c)) = zero;
     if (final && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) final[i * a.dim + column] = carry;
 }
 
-// The same from the last row to the first: q counts rows from the sequence's end.
-template <class T, int V, int S, int DEPTH, bool CLUSTER>
-__global__ void __launch_bounds__(kTileThreads) scan_tile_back_kernel(const ScanArgs a, const ScanGrads<T> g)
+// The same from the sequence's last row to its first.
+template <class T, int V, int S, int NT, int DEPTH, bool CLUSTER>
+__global__ void __launch_bounds__(NT) scan_tile_back_kernel(const ScanArgs a, const ScanGrads<T> g)
 {
-    using L = Tile<T, V, S>;
+    using L = Tile<T, V, S, NT>;
     using W = Vec<T, V>;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(16) TileShared<L> sh;
+    __shared__ __align__(16) TileShared<L, CLUSTER> sh;
     Exchange x;
     if constexpr (CLUSTER) x.begin(sh);
     const uint32_t tile = blockIdx.x / x.ranks, tiles = static_cast<uint32_t>((a.dim + L::kColumns - 1) / L::kColumns);
     const int64_t i = tile / tiles, c0 = static_cast<int64_t>(tile % tiles) * L::kColumns;
     const int64_t c = c0 + threadIdx.x % L::kLanes * V;
     const bool inside = c < a.dim;
-    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk, end = n - 1;
-    const T *z = g.z.p + i * g.z.batch + c, *v = g.v.p + i * g.v.batch + c, *h = g.h.p + i * g.h.batch + c, *dh = g.dh.p + i * g.dh.batch + c;
-    T *dz = g.dz.p + i * g.dz.batch + c, *dv = g.dv.p + i * g.dv.batch + c;
+    const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk;
     const int64_t column = c0 + threadIdx.x / L::kGroups;
     float carry = column < a.dim && g.d_final ? g.d_final[i * a.dim + column] : 0.0f;
-    const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;
+    // Rows count from the end here: this thread's first ones of the step that is fetched and of the step at hand.
+    const int64_t top = n - 1 - (x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S);
+    int next = static_cast<int>(top), t0 = next;
+    const int step = static_cast<int>(stride);
+    const T *z = g.z.p + (i * g.z.batch + top * g.z.row + c), *v = g.v.p + (i * g.v.batch + top * g.v.row + c);
+    const T *dh = g.dh.p + (i * g.dh.batch + top * g.dh.row + c), *h = g.h.p + (i * g.h.batch + (top - 1) * g.h.row + c);
+    T *dz = g.dz.p + (i * g.dz.batch + top * g.dz.row + c), *dv = g.dv.p + (i * g.dv.batch + top * g.dv.row + c);
     const W closed = filled<T, V>(__int_as_float(0x7f800000)), zero = filled<T, V>(0.0f);
     W *ring = reinterpret_cast<W *>(smem) + threadIdx.x;  // a stage: S of z, of dh, of v and of h
-    auto slot = [&](int stage, int what, int r) -> W & { return ring[((stage * 4 + what) * S + r) * kTileThreads]; };
+    auto slot = [&](int stage, int what, int r) -> W & { return ring[((stage * 4 + what) * S + r) * NT]; };
     constexpr int R = L::kRing ? 1 : S;
     W zr[R], dr[R], vr[R], hr[R], zn[R], dn[R], vn[R], hn[R];  // without the ring: this step's and the next one's
-    auto fetch = [&](int64_t q, int stage) {
+    auto fetch = [&](int stage) {
+        const T *pz = z, *pd = dh, *pv = v, *ph = h;
 #pragma unroll
         for (int r = 0; r < S; ++r) {
-            const int64_t t = end - q - r;
-            const bool on = inside && t >= 0;
+            const bool on = inside && next >= r;
             if constexpr (L::kRing) {
                 if (on) {
-                    cp_async16(&slot(stage, 0, r), z + t * g.z.row);
-                    cp_async16(&slot(stage, 1, r), dh + t * g.dh.row);
-                    cp_async16(&slot(stage, 2, r), v + t * g.v.row);
-                    if (t) cp_async16(&slot(stage, 3, r), h + (t - 1) * g.h.row);
+                    cp_async16(&slot(stage, 0, r), pz);
+                    cp_async16(&slot(stage, 1, r), pd);
+                    cp_async16(&slot(stage, 2, r), pv);
+                    if (next > r) cp_async16(&slot(stage, 3, r), ph);
                 } else {
                     slot(stage, 0, r) = closed;
                     slot(stage, 1, r) = zero;
                 }
             } else {
-                zn[r] = on ? *reinterpret_cast<const W *>(z + t * g.z.row) : closed;
-                dn[r] = on ? *reinterpret_cast<const W *>(dh + t * g.dh.row) : zero;
-                vn[r] = on ? *reinterpret_cast<const W *>(v + t * g.v.row) : zero;
-                hn[r] = on && t ? *reinterpret_cast<const W *>(h + (t - 1) * g.h.row) : zero;
+                zn[r] = on ? *reinterpret_cast<const W *>(pz) : closed;
+                dn[r] = on ? *reinterpret_cast<const W *>(pd) : zero;
+                vn[r] = on ? *reinterpret_cast<const W *>(pv) : zero;
+                hn[r] = on && next > r ? *reinterpret_cast<const W *>(ph) : zero;
             }
+            pz -= g.z.row, pd -= g.dh.row, pv -= g.v.row, ph -= g.h.row;
         }
+        next -= step;
+        z -= stride * g.z.row, dh -= stride * g.dh.row, v -= stride * g.v.row, h -= stride * g.h.row;
         if constexpr (L::kRing) cp_async_commit();
     };
-    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(first + d * stride, d);
+    for (int d = 0; d < (L::kRing ? DEPTH : 1); ++d) fetch(d);
     Lanes<V> minus;
     minus.set(-1.0f);
     int stage = 0;
     for (int64_t base = 0; base < n; base += stride) {
-        const int64_t q = first + base;
         if constexpr (L::kRing) {
             cp_async_wait<DEPTH - 1>();
         } else {
 #pragma unroll
             for (int r = 0; r < S; ++r) zr[r] = zn[r], dr[r] = dn[r], vr[r] = vn[r], hr[r] = hn[r];
-            fetch(q + stride, 0);
+            fetch(0);
         }
         Lanes<V> f[S], shut[S], A, B;
 #pragma unroll
@@ -597,16 +607,15 @@ __global__ void __launch_bounds__(kTileThreads) scan_tile_back_kernel(const Scan
             A = r ? f[r] * A : f[r];
         }
         Lanes<V> later = tile_start<CLUSTER>(A, B, carry, sh, x, a.status);
-        if (inside)
+        T *pz = dz, *pv = dv;
 #pragma unroll
-            for (int r = 0; r < S; ++r) {
-                const int64_t t = end - q - r;
-                if (t < 0) continue;
+        for (int r = 0; r < S; ++r, pz -= g.dz.row, pv -= g.dv.row)
+            if (inside && t0 >= r) {
                 W d, vv, hv;
                 if constexpr (L::kRing) d = slot(stage, 1, r), vv = slot(stage, 2, r), hv = slot(stage, 3, r);
                 else d = dr[r], vv = vr[r], hv = hr[r];
                 Lanes<V> before = lanes(hv);
-                if (t == 0) {
+                if (t0 == r) {  // the sequence's first row
                     float y[V];
 #pragma unroll
                     for (int j = 0; j < V; ++j) y[j] = a.initial ? a.initial[i * a.dim + c + j] : 0.0f;
@@ -614,16 +623,18 @@ __global__ void __launch_bounds__(kTileThreads) scan_tile_back_kernel(const Scan
                 }
                 const Lanes<V> gt = lanes(d) + later, dvt = shut[r] * gt;
                 later = f[r] * gt;
-                *reinterpret_cast<W *>(dv + t * g.dv.row) = rounded<T, V>(dvt);
-                *reinterpret_cast<W *>(dz + t * g.dz.row) = rounded<T, V>((f[r] * dvt) * fma(lanes(vv), minus, before));
+                *reinterpret_cast<W *>(pv) = rounded<T, V>(dvt);
+                *reinterpret_cast<W *>(pz) = rounded<T, V>((f[r] * dvt) * fma(lanes(vv), minus, before));
             }
-        if constexpr (L::kRing) fetch(q + DEPTH * stride, stage);
+        t0 -= step;
+        dz -= stride * g.dz.row, dv -= stride * g.dv.row;
+        if constexpr (L::kRing) fetch(stage);
         stage = stage + 1 == DEPTH ? 0 : stage + 1;
     }
     if (inside)
         for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs) {
-            *reinterpret_cast<W *>(dz + t * g.dz.row) = zero;
-            *reinterpret_cast<W *>(dv + t * g.dv.row) = zero;
+            *reinterpret_cast<W *>(g.dz.p + (i * g.dz.batch + t * g.dz.row + c)) = zero;
+            *reinterpret_cast<W *>(g.dv.p + (i * g.dv.batch + t * g.dv.row + c)) = zero;
         }
     if (g.d_initial && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) g.d_initial[i * a.dim + column] = carry;
 }
@@ -637,6 +648,7 @@ struct ea_scan {
     DeviceOf dev;
     cudaStream_t stream = nullptr;
     uint32_t *status = nullptr;
+    Allowed allowed;
 };
 
 namespace {
@@ -668,10 +680,16 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
     return EA_OK;
 }
 
+#ifndef WPK
+#define WPK 256
+#endif
 constexpr int64_t kWalkRows = 16;  // sequences up to this length are walked along
-constexpr int kDepth = 3, kClusterDepth = 2, kBackDepth = 2;  // stages of the rings
-// A thread's rows: of 16-byte accesses without and within a cluster, of single elements, and the same of the gradient.
-constexpr int kRows = 4, kClusterRows = 8, kRowsOfOne = 16, kBackRows = 4, kBackRowsOfOne = 8;
+// Stages of a ring, and a thread's rows: 16-byte accesses without and within a cluster, and single elements.  Forward, 16 x 1024 x
+// 1600 bf16: 26.6 us; 3 stages 27.8, 2 rows 32.0.  2 x 65,536 x 1024 in clusters: 148 us; 4 rows 171.  Gradient of the former: 51.3 us; 3
+// stages 53.6, 4 rows 55.0, 1 row 59; in clusters (2 x 16,384 x 1024) 69.7 us; 2 rows 100, 8 rows 88.
+constexpr int kDepth = 2, kTileThreads = 128;
+constexpr int kRows = 4, kClusterRows = 8, kRowsOfOne = 8;
+constexpr int kBackRows = 2, kBackClusterRows = 4, kBackRowsOfOne = 8;
 
 // CTAs of a cluster along a sequence: 1 where the tiles alone occupy `fill` quarters of the SMs (an exchange costs as much as
 // a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes, and no more than the
@@ -687,14 +705,18 @@ int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
 }
 
 template <class L, class... KArgs, class... Args>
-cudaError_t launch_tiles(const ea_scan *s, const ScanArgs &a, int ranks, int stages, void (*kernel)(KArgs...), Args &&...args)
+cudaError_t launch_tiles(ea_scan *s, const ScanArgs &a, int ranks, int stages, void (*kernel)(KArgs...), Args &&...args)
 {
-    const size_t ring = L::kRing ? static_cast<size_t>(stages) * L::kRows * kTileThreads * 16 : 0;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(ring));
-    if (e == cudaSuccess && ranks > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    const size_t ring = L::kRing ? static_cast<size_t>(stages) * L::kRows * L::kThreads * 16 : 0;
+    const cudaError_t e = s->allowed(kernel, ring, ranks > 1);
     if (e != cudaSuccess) return e;
     const int64_t tiles = a.batch * over<int64_t>(a.dim, L::kColumns);
-    return launch_lm(kernel, dim3(static_cast<unsigned>(tiles * ranks)), kTileThreads, ring, s->stream, false, ranks, a, std::forward<Args>(args)...);
+    return launch_lm(kernel, dim3(static_cast<unsigned>(tiles * ranks)), L::kThreads, ring, s->stream, false, ranks, a, std::forward<Args>(args)...);
+}
+
+bool walks(const ea_scan *s, const ScanArgs &a, int32_t type)
+{
+    return a.length <= kWalkRows || a.batch * a.dim * static_cast<int64_t>(type_bytes(type)) >= static_cast<int64_t>(s->dev.sms) * 16 * WPK;
 }
 
 bool states_on_16(const void *p, const void *q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) % 16 == 0; }
@@ -753,9 +775,10 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
         if (r == EA_OK) r = check_rows_apart(a.batch, a.length, c->h_batch, c->h_row, a.dim, "h");
     }
     if (r != EA_OK || !a.batch || (!a.length && !final)) return r;
+    const bool walk = walks(s, a, c->type);
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
     const bool all = wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) && wide(h, c->h_batch, c->h_row) &&
-                     (a.length > kWalkRows || states_on_16(initial, final));
+                     (!walk || states_on_16(initial, final));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
@@ -764,16 +787,16 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
             constexpr int S = V == 1 ? kRowsOfOne : kRows, SC = V == 1 ? kRowsOfOne : kClusterRows;
-            using L = Tile<T, V, S>;
-            using LC = Tile<T, V, SC>;
-            if (a.length <= kWalkRows) {
+            using L = Tile<T, V, S, kTileThreads>;
+            using LC = Tile<T, V, SC, kTileThreads>;
+            if (walk) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, zs, vs, hs, final);
                 e = cudaGetLastError();
             } else {
                 const int ranks = scan_ranks<LC>(s, a, 5);
-                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kClusterDepth * 2, scan_tile_kernel<T, V, SC, kClusterDepth, true>, zs, vs, hs, final);
-                else e = launch_tiles<L>(s, a, 1, kDepth * 2, scan_tile_kernel<T, V, S, kDepth, false>, zs, vs, hs, final);
+                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 2, scan_tile_kernel<T, V, SC, kTileThreads, kDepth, true>, zs, vs, hs, final);
+                else e = launch_tiles<L>(s, a, 1, kDepth * 2, scan_tile_kernel<T, V, S, kTileThreads, kDepth, false>, zs, vs, hs, final);
             }
         });
     });
@@ -798,10 +821,11 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
     }
     if (r == EA_OK && d_initial && d_initial == initial) r = lm_fail(EA_E_INVAL, "d_initial may not be initial");
     if (r != EA_OK || !a.batch || (!a.length && !d_initial)) return r;
+    const bool walk = walks(s, a, c->type);
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
     const bool all = wide(dh, c->dh_batch, c->dh_row) && wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) &&
                      wide(h, c->h_batch, c->h_row) && wide(dz, c->dz_batch, c->dz_row) && wide(dv, c->dv_batch, c->dv_row) &&
-                     (a.length > kWalkRows || (states_on_16(initial, d_final) && states_on_16(d_initial, nullptr)));
+                     (!walk || (states_on_16(initial, d_final) && states_on_16(d_initial, nullptr)));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
@@ -811,16 +835,17 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
                              out(dz, c->dz_batch, c->dz_row), out(dv, c->dv_batch, c->dv_row), d_final,                     d_initial};
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
-            constexpr int S = V == 1 ? kBackRowsOfOne : kBackRows;
-            using L = Tile<T, V, S>;
-            if (a.length <= kWalkRows) {
+            constexpr int S = V == 1 ? kBackRowsOfOne : kBackRows, SC = V == 1 ? kBackRowsOfOne : kBackClusterRows;
+            using L = Tile<T, V, S, kTileThreads>;
+            using LC = Tile<T, V, SC, kTileThreads>;
+            if (walk) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_back_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, g);
                 e = cudaGetLastError();
             } else {
-                const int ranks = scan_ranks<L>(s, a, 9);
-                if (ranks > 1) e = launch_tiles<L>(s, a, ranks, kBackDepth * 4, scan_tile_back_kernel<T, V, S, kBackDepth, true>, g);
-                else e = launch_tiles<L>(s, a, 1, kBackDepth * 4, scan_tile_back_kernel<T, V, S, kBackDepth, false>, g);
+                const int ranks = scan_ranks<LC>(s, a, 9);
+                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 4, scan_tile_back_kernel<T, V, SC, kTileThreads, kDepth, true>, g);
+                else e = launch_tiles<L>(s, a, 1, kDepth * 4, scan_tile_back_kernel<T, V, S, kTileThreads, kDepth, false>, g);
             }
         });
     });
