@@ -92,50 +92,40 @@ __device__ __forceinline__ void store_eight(f16 *p, const float (&x)[8])
     *reinterpret_cast<Eight<f16> *>(p) = r;
 }
 
-constexpr int kDropUnroll = 2;
+// CTAs of an SM.  Of 16-bit types alone, whose threads have 16 or 32 bytes on their way, as many as fit (16,384 x 1600 with a
+// residual 25.4 us; 5 of them 27.0); with binary32 fewer (260,096 x 768 to bf16 174 us; 8 of them 200).
+template <class X, class Y>
+constexpr int kDropCtas = sizeof(X) + sizeof(Y) == 4 ? 8 : 5;
 
 // Rows that are whole blocks of eight, each on its boundary, `packs` of them a row (0: all in one); limit below 2^16.  The
 // random words are formed while the loads are on their way.
 template <class X, class Y, bool ADD>
-__global__ void __launch_bounds__(kDropThreads) dropout_packs_kernel(const DropArgs a, const Rows packs, const RowsOf<const X> xs, const RowsOf<const Y> adds,
-                                                                     const RowsOf<Y> ys)
+__global__ void __launch_bounds__(kDropThreads, kDropCtas<X, Y>) dropout_packs_kernel(const DropArgs a, const Rows packs, const RowsOf<const X> xs,
+                                                                                       const RowsOf<const Y> adds, const RowsOf<Y> ys)
 {
     const uint2 counter = drop_counter(a);
-    const int64_t blocks = a.n / kDropVec, stride = static_cast<int64_t>(gridDim.x) * (kDropThreads * kDropUnroll);
+    const int64_t blocks = a.n / kDropVec, stride = static_cast<int64_t>(gridDim.x) * kDropThreads;
     const uint32_t limit = a.limit << 16;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * (kDropThreads * kDropUnroll) + threadIdx.x; first < blocks; first += stride) {
-        Eight<X> x[kDropUnroll];
-        Eight<Y> add[kDropUnroll];
-        Y *to[kDropUnroll];
-#pragma unroll
-        for (int k = 0; k < kDropUnroll; ++k) {
-            const int64_t q = first + k * kDropThreads;
-            if (q >= blocks) break;
-            uint32_t r = 0;
-            int64_t column = q * kDropVec;
-            if (packs.inner) {
-                r = packs.outer_of(static_cast<uint32_t>(q));
-                column = static_cast<int64_t>(static_cast<uint32_t>(q) - r * packs.inner) * kDropVec;
-            }
-            x[k] = load_eight(xs.row(a.rows, r) + column);
-            if constexpr (ADD) add[k] = load_eight(adds.row(a.rows, r) + column);
-            to[k] = ys.row(a.rows, r) + column;
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * kDropThreads + threadIdx.x; q < blocks; q += stride) {
+        uint32_t r = 0;
+        int64_t column = q * kDropVec;
+        if (packs.inner) {
+            r = packs.outer_of(static_cast<uint32_t>(q));
+            column = static_cast<int64_t>(static_cast<uint32_t>(q) - r * packs.inner) * kDropVec;
         }
+        const Eight<X> x = load_eight(xs.row(a.rows, r) + column);
+        Eight<Y> add;
+        if constexpr (ADD) add = load_eight(adds.row(a.rows, r) + column);
+        const uint4 w = drop_words(a, q, counter);
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        float y[8];
 #pragma unroll
-        for (int k = 0; k < kDropUnroll; ++k) {
-            const int64_t q = first + k * kDropThreads;
-            if (q >= blocks) break;
-            const uint4 w = drop_words(a, q, counter);
-            const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-            float y[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool kept = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) >= limit;
-                y[i] = kept ? __fmul_rn(to_f32(x[k].x[i]), a.scale) : 0.0f;
-                if constexpr (ADD) y[i] = __fadd_rn(y[i], to_f32(add[k].x[i]));
-            }
-            store_eight(to[k], y);
+        for (int i = 0; i < 8; ++i) {
+            const bool kept = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) >= limit;
+            y[i] = kept ? __fmul_rn(to_f32(x.x[i]), a.scale) : 0.0f;
+            if constexpr (ADD) y[i] = __fadd_rn(y[i], to_f32(add.x[i]));
         }
+        store_eight(ys.row(a.rows, r) + column, y);
     }
 }
 
@@ -248,7 +238,7 @@ int ea_dropout_apply(ea_dropout *h, const ea_dropout_call *c, const void *x, con
         if (wide && (flat || (blocks < kMaxRows && dim > kDropVec)) && a.limit < 65536) {
             if (flat) a.rows = Rows{};
             const Rows packs = flat ? Rows{} : rows_of(dim / kDropVec);
-            const int64_t ctas = std::min<int64_t>(over<int64_t>(blocks, kDropThreads * kDropUnroll), h->dev.sms * kDropCtasPerSm);
+            const int64_t ctas = std::min<int64_t>(over<int64_t>(blocks, kDropThreads), h->dev.sms * kDropCtas<X, Y>);
             auto kernel = add ? dropout_packs_kernel<X, Y, true> : dropout_packs_kernel<X, Y, false>;
             kernel<<<static_cast<unsigned>(ctas), kDropThreads, 0, h->stream>>>(a, packs, xs, adds, ys);
             return;
