@@ -114,35 +114,36 @@ class LayerNorm(_Block):
 
     def __init__(self, dim: int, max_rows: int, eps: float = 1e-5, stream=None, device=None):
         self.dim, self.max_rows, self.eps = int(dim), int(max_rows), float(eps)
-        self._c, self._row = ea_layernorm_call(), torch.Size((self.dim,))
+        self._row = torch.Size((self.dim,))
+        # The descriptions of a call: of any rows, and of rows one behind another, where only their number changes.
+        self._c, d = ea_layernorm_call(), self.dim
+        self._flat = ea_layernorm_call(outer=1, x_inner=d, y_inner=d, dx_inner=d, add_inner=d)
         self._open(ea_layernorm_config(self.dim, self.max_rows, self.eps), stream, device)
 
-    def _x(self, x):
-        if not isinstance(x, _Tensor) or x.device != self.device:
-            self._on_device(x, "x")
-        shape, c = x.shape, self._c
+    def _x(self, x, flat):
+        """Describes x's rows; returns the description and what to pass for x.  flat: whether all tensors of the call are
+        contiguous."""
+        shape = x.shape
         if not shape or shape[-1] != self.dim:
             _refuse(f"x is {tuple(shape)}: its rows are not {self.dim} long")
-        c.x_type = _TYPE.get(x.dtype) or _type(x.dtype, "x")
-        stride = x.stride()
-        if len(shape) == 3 and stride[2] == 1:
-            c.outer, c.inner = shape[0], shape[1]
-            c.x_outer, c.x_inner = stride[0], stride[1]
+        if flat:
+            c = self._flat
+            c.inner = x.numel() // self.dim
         else:
+            c = self._c
             c.outer, c.inner = _counts(shape)
             x, c.x_outer, c.x_inner = self._read(x, shape, "x")
-        return x
+        c.x_type = _TYPE.get(x.dtype) or _type(x.dtype, "x")
+        return c, x
 
-    def _weight(self, t, dtype, what):
-        """The address of a weight (None: 0)."""
-        if t is None:
-            return None
+    def _weight(self, t, c, dtype, what):
+        """The address of a weight."""
         if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
         own = t.dtype
         if dtype is not None and own != dtype:
             _refuse(f"{what} is {own}, the other one {dtype}")
-        self._c.weight_type = _TYPE.get(own) or _type(own, what)
+        c.weight_type = _TYPE.get(own) or _type(own, what)
         if t.shape != self._row or not t.is_contiguous():
             _refuse(f"{what} is not a contiguous tensor of {self.dim}")
         return t.data_ptr()
@@ -150,23 +151,35 @@ class LayerNorm(_Block):
     def forward(self, x, weight=None, bias=None, out=None, dtype=None, stats=None):
         """(y, stats): y of x's shape in `dtype` (default: x's) or in `out` (which may be x); stats, of shape
         x.shape[:-1] + (2,), each row's mean and 1 / sqrt(variance + eps), which grad takes, or into `stats`."""
-        given = None if out is None and stats is None else [t for t in (out, stats) if t is not None]
-        shape, x = getattr(x, "shape", None), self._x(x)
-        c = self._c
-        w = self._weight(weight, None, "weight")
-        b = self._weight(bias, weight.dtype if w is not None else None, "bias")
-        if out is None:
+        if not isinstance(x, _Tensor) or x.device != self.device:
+            self._on_device(x, "x")
+        shape, new = x.shape, out is None
+        if not new:
+            outer, inner = self._written(out, shape, dtype or getattr(out, "dtype", None), "out")
+        flat = x.is_contiguous() and (new or out.is_contiguous())
+        c, x = self._x(x, flat)
+        w = b = None
+        if weight is not None:
+            w = self._weight(weight, c, None, "weight")
+        if bias is not None:
+            b = self._weight(bias, c, None if w is None else weight.dtype, "bias")
+        if new:
             kind = dtype or x.dtype
             c.y_type = _TYPE.get(kind) or _type(kind, "out")
             out = torch.empty_like(x, dtype=kind, memory_format=_ROWS)
-            c.y_outer, c.y_inner = c.inner * self.dim, self.dim
+            outer, inner = c.inner * self.dim, self.dim
         else:
-            c.y_outer, c.y_inner = self._written(out, shape, dtype or getattr(out, "dtype", None), "out")
             c.y_type = _type(out.dtype, "out")
+        if not flat:
+            c.y_outer, c.y_inner = outer, inner
+        given = None
         if stats is None:
             stats = x.new_empty((*shape[:-1], 2), dtype=_F32)
+            if not new:
+                given = (out,)
         else:
             self._values(stats, (*shape[:-1], 2), _F32, "stats")
+            given = (stats,) if new else (out, stats)
         self._run(self._L.ea_layernorm_forward, (c, x.data_ptr(), w, b, out.data_ptr(), stats.data_ptr()), (x, weight, bias, out, stats))
         if given:
             _C._increment_version(given)
@@ -180,7 +193,8 @@ class LayerNorm(_Block):
             return torch.empty(self._row, dtype=_F32, device=self.device)
         if not isinstance(t, _Tensor) or t.device != self.device:
             self._on_device(t, what)
-        self._values(t, self._row, t.dtype, what)
+        if t.shape != self._row or not t.is_contiguous():
+            _refuse(f"{what} is not a contiguous tensor of {self.dim}")
         return t
 
     def grad(self, dy, x, stats, weight=None, add=None, out=None, dw=None, db=None, accumulate: bool = False):
@@ -188,34 +202,45 @@ class LayerNorm(_Block):
         that are added to dx (the gradient that passes the block by).  dx: into `out` (which may be dy, x or add) or new.
         dw, db: None (not computed), True (new, in 32 bits) or tensors of one type that are written to or, with accumulate, added
         to."""
-        given = [t for t in (out, dw, db) if isinstance(t, _Tensor)]
         if accumulate and (dw is True or db is True):
             _refuse("accumulate needs dw's and db's tensors")
-        shape, x = getattr(x, "shape", None), self._x(x)
-        c = self._c
-        dy, c.y_outer, c.y_inner = self._read(dy, shape, "dy")
-        c.y_type = _type(dy.dtype, "dy")
-        at = self._values(stats, (*shape[:-1], 2), _F32, "stats")
-        w = self._weight(weight, None, "weight")
+        if not isinstance(x, _Tensor) or x.device != self.device:
+            self._on_device(x, "x")
+        shape, new, given = x.shape, out is None, []
+        y, y_outer, y_inner = self._read(dy, shape, "dy")
         if add is not None:
-            add, c.add_outer, c.add_inner = self._read(add, shape, "add")
+            add, add_outer, add_inner = self._read(add, shape, "add")
             if add.dtype != x.dtype:
                 _refuse(f"add is {add.dtype}, x {x.dtype}")
+        if not new:
+            outer, inner = self._written(out, shape, x.dtype, "out")
+            given.append(out)
+        flat = x.is_contiguous() and y.is_contiguous() and (add is None or add.is_contiguous()) and (new or out.is_contiguous())
+        c, x = self._x(x, flat)
+        c.y_type = _TYPE.get(y.dtype) or _type(y.dtype, "dy")
+        at = self._values(stats, (*shape[:-1], 2), _F32, "stats")
+        w = None if weight is None else self._weight(weight, c, None, "weight")
+        if isinstance(dw, _Tensor):
+            given.append(dw)
+        if isinstance(db, _Tensor):
+            given.append(db)
         dw, db = self._sums(dw, "dw"), self._sums(db, "db")
         if dw is not None and db is not None and dw.dtype != db.dtype:
             _refuse(f"dw is {dw.dtype}, db {db.dtype}")
-        for t in (dw, db):
-            if t is not None:
-                c.grad_type = _type(t.dtype, "a weight's gradient")
-        if out is None:
+        one = db if dw is None else dw
+        if one is not None:
+            c.grad_type = _TYPE.get(one.dtype) or _type(one.dtype, "a weight's gradient")
+        if new:
             out = torch.empty_like(x, memory_format=_ROWS)
-            c.dx_outer, c.dx_inner = c.inner * self.dim, self.dim
-        else:
-            c.dx_outer, c.dx_inner = self._written(out, shape, x.dtype, "out")
+            outer, inner = c.inner * self.dim, self.dim
+        if not flat:
+            c.y_outer, c.y_inner, c.dx_outer, c.dx_inner = y_outer, y_inner, outer, inner
+            if add is not None:
+                c.add_outer, c.add_inner = add_outer, add_inner
         self._run(self._L.ea_layernorm_backward,
-                  (c, dy.data_ptr(), x.data_ptr(), at, w, None if add is None else add.data_ptr(), out.data_ptr(),
+                  (c, y.data_ptr(), x.data_ptr(), at, w, None if add is None else add.data_ptr(), out.data_ptr(),
                    None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), int(accumulate)),
-                  (dy, x, stats, weight, add, out, dw, db))
+                  (y, x, stats, weight, add, out, dw, db))
         if given:
             _C._increment_version(given)
         return out, dw, db
@@ -364,7 +389,7 @@ class Dropout(_Block):
         self.seed = int(seed)
         if not 0 <= self.seed < 1 << 64:
             _refuse("seed is outside [0, 2^64)")
-        self._c = ea_dropout_call()
+        self._c, self._flat = ea_dropout_call(), ea_dropout_call(outer=1, inner=1)
         self._open(ea_dropout_config(float(p), self.seed), stream, device)
         self.p = round(65536 * float(p)) / 65536
 
@@ -372,28 +397,34 @@ class Dropout(_Block):
         """residual + x / (1 - p) where an element is kept, residual (or 0) where it is not, of x's shape, in `dtype` (default:
         the residual's type, or x's) or into `out` (which may be x or residual).  x and the result are of one type, or one of them
         float32; residual is of the result's."""
-        c, given = self._c, out is not None
+        given = out is not None
         if not isinstance(x, _Tensor) or x.device != self.device:
             self._on_device(x, "x")
         shape = x.shape
         if not shape:
             _refuse("x has no dimensions")
-        c.x_type = _type(x.dtype, "x")
-        c.outer, c.inner = _counts(shape)
-        c.dim = shape[-1]
-        x, c.x_outer, c.x_inner = self._read(x, shape, "x")
         if dtype is None:
             dtype = (out if given else residual if residual is not None else x).dtype
+        if given:
+            outer, inner = self._written(out, shape, dtype, "out")
         if residual is not None:
-            residual, c.add_outer, c.add_inner = self._read(residual, shape, "residual")
+            residual, add_outer, add_inner = self._read(residual, shape, "residual")
             if residual.dtype != dtype:
                 _refuse(f"residual is {residual.dtype}, the result {dtype}")
-        c.y_type = _type(dtype, "the result")
+        if x.is_contiguous() and (residual is None or residual.is_contiguous()) and (not given or out.is_contiguous()):
+            c = self._flat
+            c.dim = x.numel()
+        else:
+            c = self._c
+            c.outer, c.inner = _counts(shape)
+            c.dim = shape[-1]
+            x, c.x_outer, c.x_inner = self._read(x, shape, "x")
+            if residual is not None:
+                c.add_outer, c.add_inner = add_outer, add_inner
+            c.y_outer, c.y_inner = (outer, inner) if given else (c.inner * c.dim, c.dim)
+        c.x_type, c.y_type = _TYPE.get(x.dtype) or _type(x.dtype, "x"), _TYPE.get(dtype) or _type(dtype, "the result")
         if not given:
             out = torch.empty_like(x, dtype=dtype, memory_format=_ROWS)
-            c.y_outer, c.y_inner = c.inner * c.dim, c.dim
-        else:
-            c.y_outer, c.y_inner = self._written(out, shape, dtype, "out")
         if isinstance(counter, _Tensor):
             if counter.device != self.device or counter.dtype != torch.int64 or counter.numel() != 1:
                 _refuse(f"counter is an integer or an int64 tensor of one value on {self.device}")

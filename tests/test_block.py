@@ -145,7 +145,7 @@ def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
         want = [(name, 1)] if raw == 7 else [(7, 5), (name, 1), (5, 7)] + [("record", 7)] * tensors
         assert log == want and device[0] == here, name
 
-    norm = handle(block.LayerNorm, dim=4, _row=torch.Size((4,)), _c=A.ea_layernorm_call())
+    norm = handle(block.LayerNorm, dim=4, _row=torch.Size((4,)), _c=A.ea_layernorm_call(), _flat=A.ea_layernorm_call())
     x, w, stats = torch.ones(3, 4), torch.ones(4), torch.ones(3, 2)
     seen("ea_layernorm_forward", 5, lambda: norm.forward(x, w, w))
     seen("ea_layernorm_backward", 8, lambda: norm.grad(x, x, stats, w, add=x, dw=True, db=True))
@@ -153,7 +153,7 @@ def test_calls_run_on_the_handles_device(monkeypatch, here, raw):
     seen("ea_scan_forward", 6, lambda: scan.forward(z, z, initial=state, lengths=torch.tensor([1, 2]), final=True))
     seen("ea_scan_forward", 4, lambda: scan.step(z[:, 0], z[:, 0], state))
     seen("ea_scan_backward", 10, lambda: scan.grad(z, z, z, z, initial=state, lengths=torch.tensor([1, 2]), d_final=state, d_initial=True))
-    drop = handle(block.Dropout, _c=A.ea_dropout_call())
+    drop = handle(block.Dropout, _c=A.ea_dropout_call(), _flat=A.ea_dropout_call())
     seen("ea_dropout_apply", 4, lambda: drop(x, torch.tensor([5]), residual=x))
     log.clear()
     scan.sync()
