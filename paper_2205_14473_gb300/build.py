@@ -17,8 +17,8 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libea.so")
 LM_SOURCES = ["ea_embed.cu", "ea_norm.cu", "ea_adamw.cu"]  # the units of include/ea_lm.h
 LM_HEADERS = ["ea_lm.cuh"]                                 # read by those and the next alone
-BLOCK_SOURCES = ["ea_layernorm.cu", "ea_scan.cu", "ea_dropout.cu"]  # the units of include/ea_block.h
-BLOCK_HEADERS = ["ea_block.cuh"]                                    # read by those alone
+BLOCK_SOURCES = ["ea_layernorm_grad.cu", "ea_layernorm.cu", "ea_scan.cu", "ea_dropout.cu"]  # the units of include/ea_block.h
+BLOCK_HEADERS = ["ea_block.cuh", "ea_layernorm.cuh"]                                       # read by those alone
 SOURCES = ["ea_api.cu", "ea_worker.cu", "ea_noalloc.cu", "ea_selftest.cu", *LM_SOURCES, *BLOCK_SOURCES] + [
     f"ea_server_{part}{m}_q{q}.cu" for q in (2, 1, 3, 0) for part in ("", "general_") for m in "sw"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
