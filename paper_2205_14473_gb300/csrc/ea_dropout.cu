@@ -30,6 +30,15 @@ __device__ __forceinline__ uint2 drop_counter(const DropArgs &a)
     return make_uint2(static_cast<uint32_t>(c), static_cast<uint32_t>(c >> 32));
 }
 
+// One element: x as kept or dropped by its half word, and what is added.
+template <class X, class Y>
+__device__ __forceinline__ Y drop_one(const DropArgs &a, uint32_t half, X x, const Y *add)
+{
+    float y = half >= a.limit ? __fmul_rn(to_f32(x), a.scale) : 0.0f;
+    if (add) y = __fadd_rn(y, to_f32(*add));
+    return from_f32<Y>(y);
+}
+
 // Eight consecutive elements of the call at a time, each found for itself.
 template <class X, class Y>
 __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropArgs a, const RowsOf<const X> xs, const RowsOf<const Y> adds, const RowsOf<Y> ys)
@@ -44,9 +53,8 @@ __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropArg
         for (int i = 0; i < kDropVec; ++i) {
             if (q * kDropVec + i >= a.n) break;
             const uint32_t half = i & 1 ? word[i >> 1] >> 16 : word[i >> 1] & 0xffffu;
-            float x = half >= a.limit ? __fmul_rn(to_f32(xs.row(a.rows, static_cast<uint32_t>(r))[column]), a.scale) : 0.0f;
-            if (adds.p) x = __fadd_rn(x, to_f32(adds.row(a.rows, static_cast<uint32_t>(r))[column]));
-            ys.row(a.rows, static_cast<uint32_t>(r))[column] = from_f32<Y>(x);
+            const uint32_t row = static_cast<uint32_t>(r);
+            ys.row(a.rows, row)[column] = drop_one(a, half, xs.row(a.rows, row)[column], adds.p ? adds.row(a.rows, row) + column : nullptr);
             if (++column == a.dim) column = 0, ++r;
         }
     }
@@ -127,6 +135,18 @@ __global__ void __launch_bounds__(kDropThreads, kDropCtas<X, Y>) dropout_packs_k
         }
         store_eight(ys.row(a.rows, r) + column, y);
     }
+}
+
+// The up to seven elements behind the blocks of one row, a thread each (in the kernel above they would cost every thread registers:
+// 16,384 x 1600 bf16 35.6 us instead of 25.3).
+template <class X, class Y>
+__global__ void dropout_tail_kernel(const DropArgs a, const X *x, const Y *add, Y *y)
+{
+    const int64_t q = a.n / kDropVec, e = q * kDropVec + threadIdx.x;
+    if (e >= a.n) return;
+    const uint4 w = drop_words(a, q, drop_counter(a));
+    const uint32_t word = threadIdx.x < 2 ? w.x : threadIdx.x < 4 ? w.y : threadIdx.x < 6 ? w.z : w.w;
+    y[e] = drop_one(a, threadIdx.x & 1 ? word >> 16 : word & 0xffffu, x[e], add ? add + e : nullptr);
 }
 
 }  // namespace ea
@@ -231,16 +251,17 @@ int ea_dropout_apply(ea_dropout *h, const ea_dropout_call *c, const void *x, con
         const RowsOf<Y> ys{static_cast<Y *>(y), c->y_outer, one ? c->y_outer : c->y_inner};
         // all rows one behind another are one row
         const bool flat = follows(c, c->x_outer, c->x_inner) && follows(c, c->y_outer, c->y_inner) && (!add || follows(c, c->add_outer, c->add_inner));
-        const int64_t dim = flat ? a.n : a.dim, outer = flat ? 1 : c->outer, inner = flat ? 1 : c->inner, blocks = over<int64_t>(a.n, kDropVec);
+        const int64_t dim = flat ? a.n / kDropVec * kDropVec : a.dim, outer = flat ? 1 : c->outer, inner = flat ? 1 : c->inner, blocks = over<int64_t>(a.n, kDropVec);
         auto whole = [&](const void *p, int32_t type, int64_t o, int64_t i) { return rows_on(8 * type_bytes(type), p, type, dim, outer, inner, o, i); };
         const bool wide = whole(x, c->x_type, c->x_outer, c->x_inner) && whole(y, c->y_type, c->y_outer, c->y_inner) &&
                           (!add || whole(add, c->y_type, c->add_outer, c->add_inner));
         if (wide && (flat || (blocks < kMaxRows && dim > kDropVec)) && a.limit < 65536) {
             if (flat) a.rows = Rows{};
             const Rows packs = flat ? Rows{} : rows_of(dim / kDropVec);
-            const int64_t ctas = std::min<int64_t>(over<int64_t>(blocks, kDropThreads), h->dev.sms * kDropCtas<X, Y>);
+            const int64_t ctas = std::min<int64_t>(over<int64_t>(a.n / kDropVec, kDropThreads), h->dev.sms * kDropCtas<X, Y>);
             auto kernel = add ? dropout_packs_kernel<X, Y, true> : dropout_packs_kernel<X, Y, false>;
-            kernel<<<static_cast<unsigned>(ctas), kDropThreads, 0, h->stream>>>(a, packs, xs, adds, ys);
+            if (ctas) kernel<<<static_cast<unsigned>(ctas), kDropThreads, 0, h->stream>>>(a, packs, xs, adds, ys);
+            if (a.n % kDropVec) dropout_tail_kernel<X, Y><<<1, kDropVec, 0, h->stream>>>(a, xs.p, adds.p, ys.p);
             return;
         }
         const int64_t ctas = over<int64_t>(blocks, kDropThreads);

@@ -255,7 +255,7 @@ int ea_layernorm_backward(ea_layernorm *h, const ea_layernorm_call *c, const voi
             if (!a.n) return;
             const RowsOf<const Y> dys = rows_at<const Y>(c, dy, c->y_outer, c->y_inner);
             const RowsOf<const X> xs = rows_at<const X>(c, x, c->x_outer, c->x_inner);
-            const RowsOf<const X> adds = rows_at<const X>(c, add, c->add_outer, c->add_inner);
+            const RowsOf<const X> adds = rows_at<const X>(c, dx ? add : nullptr, c->add_outer, c->add_inner);
             const RowsOf<X> dxs = rows_at<X>(c, dx, c->dx_outer, c->dx_inner);
             if (a.dim > kMostHeld) {
                 if (dw || db) {  // before dx, which may be in the place of dy or x

@@ -197,7 +197,7 @@ def _check_grad(got, dy, x, stats, w, add=None, before=None):
 
 # numbers of rows around every split of the sums over them
 @pytest.mark.parametrize("rows", [1, 2, 3, 7, 8, 9, 31, 33, 100, 151, 152, 153, 303, 305, 607, 609, 1215, 1217, 2433, 5003, 20_011])
-@pytest.mark.parametrize("dim", [8, 64, 515, 1600])
+@pytest.mark.parametrize("dim", [1, 3, 8, 64, 515, 1600])
 def test_norm_rows(rows, dim):
     x, dy, w = _randn(rows, dim, seed=rows, dtype=BF16, mean=0.1), _randn(rows, dim, seed=rows + 1, dtype=BF16), _randn(dim, seed=18)
     norm = ea.LayerNorm(dim, rows)
@@ -256,6 +256,24 @@ def test_norm_in_place(dim):
         c, a, e = dy.clone(), x.clone(), add.clone()
         got = norm.grad(c, a, stats, w, add=e, out=(c, a, e)[k], dw=True, db=True)
         assert all(_same(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("dim,off", [(64, 0), (64, 1), (77, 0), (77, 3), (9000, 1)])
+def test_norm_sums_alone(dim, off):
+    """The C call without dx; what is named as added, at an address of its own, is not looked at."""
+    from paper_2205_14473_gb300 import block_abi as A
+
+    x, dy, add = _off(_randn(21, dim, seed=34, dtype=BF16), off), _off(_randn(21, dim, seed=35, dtype=BF16), off), _off(_randn(21, dim, seed=36, dtype=BF16), 1)
+    norm = ea.LayerNorm(dim, 21)
+    _, stats = norm.forward(x)
+    dw, db = torch.empty(2, dim, device="cuda")
+    c = A.ea_layernorm_call(1, 21, 0, dim, 0, dim, 0, 0, 0, dim, 1, 1, 0, 0)
+    L = ea.lib()
+    assert L.ea_layernorm_backward(norm.h, c, dy.data_ptr(), x.data_ptr(), stats.data_ptr(), None, add.data_ptr(), None, dw.data_ptr(), db.data_ptr(), 0) == 0
+    want = norm.grad(dy, x, stats, dw=True, db=True)
+    assert _same(dw, want[1]) and _same(db, want[2])
+    assert L.ea_layernorm_backward(norm.h, c, dy.data_ptr(), x.data_ptr(), stats.data_ptr(), None, None, None, None, None, 0) == 0
+    torch.cuda.synchronize()
 
 
 def test_norm_of_no_rows():
@@ -918,7 +936,7 @@ def test_refusals():
             (scan.forward, (x, x), dict(out=turned)), (scan.forward, (x, x), dict(out=h[:1].expand(2, 3, dim))), (scan.step, (x, x, state), {}),
             (scan.step, (x[:, 0], x[:, 0], None), {}), (scan.step, (x[:, 0], x[:, 0], state[:1]), {}), (scan.step, (x[:, 0], x[:, 0], state), dict(out=x)),
             (scan.grad, (x, x, x, h[:1]), {}), (scan.grad, (x.half(), x, x, h), {}), (scan.grad, (x, x, x, h), dict(dz=h)), (scan.grad, (x, x, x, h), dict(dv=turned)),
-            (scan.grad, (x, x, x, h), dict(d_final=state[:1])), (scan.grad, (x, x, x, h), dict(d_initial=state.double())),
+            (scan.grad, (x, x, x, h), dict(initial=state, d_initial=state)), (scan.grad, (x, x, x, h), dict(d_final=state[:1])), (scan.grad, (x, x, x, h), dict(d_initial=state.double())),
             (drop, (x.cpu(), 1), {}), (drop, (x.double(), 1), {}), (drop, (x, -1), {}), (drop, (x, 2 ** 64), {}), (drop, (x, torch.tensor([1])), {}),
             (drop, (x, torch.tensor([1.0], device="cuda")), {}), (drop, (x, torch.tensor([1, 2], device="cuda")), {}), (drop, (x, 1), dict(residual=x.half(), dtype=F32)),
             (drop, (x, 1), dict(residual=x[:1])), (drop, (x, 1), dict(out=y[:1])), (drop, (x, 1), dict(out=turned)), (drop, (x, 1), dict(out=y, dtype=BF16)),
