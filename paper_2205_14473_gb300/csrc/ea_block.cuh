@@ -104,7 +104,8 @@ inline int check_rows_apart(int64_t outer, int64_t inner, int64_t outer_stride, 
     return small && large ? EA_OK : lm_fail(EA_E_INVAL, "the rows of %s overlap", what);
 }
 
-// The kernels of a handle that may have more shared memory than they get unasked, or clusters of 16: asked for once each.
+// The kernels of a handle that may have more shared memory than the 48 KB, their own variables included, that they get unasked, or
+// clusters of 16: asked for once each.
 struct Allowed {
     const void *kernels[16] = {};
     template <class K>
@@ -112,7 +113,7 @@ struct Allowed {
     {
         const void *k = reinterpret_cast<const void *>(kernel);
         const size_t at = reinterpret_cast<uintptr_t>(k) / 16 % 16;
-        if (kernels[at] == k || (bytes <= 48 * 1024 && !large_cluster)) return cudaSuccess;
+        if (kernels[at] == k || (bytes <= 16 * 1024 && !large_cluster)) return cudaSuccess;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
         if (e == cudaSuccess && large_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e == cudaSuccess) kernels[at] = k;

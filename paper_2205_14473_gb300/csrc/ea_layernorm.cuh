@@ -37,31 +37,16 @@ __device__ __forceinline__ float row_block_sum(float v, float *red)
 // ---------------------------------------------------------------------------------------------- rows in registers
 constexpr int kHeld = 16;                // elements of a thread
 constexpr int kBackThreads = 512;
-constexpr int kForwardDepth = 4;         // rows on their way
+constexpr int kForwardDepth = 3;         // rows on their way
 // Of the gradient: what 192 KB hold of x, dy and the added rows.
 template <class X, class Y>
 constexpr int kBackDepth = 192 * 1024 / (kBackThreads * kHeld * (2 * static_cast<int>(sizeof(X)) + static_cast<int>(sizeof(Y))));
 
-// An asynchronous copy global -> shared of BYTES (8 or 16) bytes, of which the first `have` are read and the others 0.
-template <int BYTES>
-__device__ __forceinline__ void cp_async_first(void *dst, const void *src, int have)
+// An 8-byte asynchronous copy global -> shared.
+__device__ __forceinline__ void cp_async8(void *dst, const void *src)
 {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(have) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_addr(dst)), "l"(src), "r"(have) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
 }
-
-// Where a row lies among the packs that its group reads: from element `off` of pack 0 to before element `end`.  Rows that are
-// whole packs start at 0.  Rows that do not start on a pack's boundary (SHIFT) are read from the boundary before them, and a
-// group's rows all lie `off` behind one: it takes every 8 m-th row.
-template <int VEC, bool SHIFT>
-struct Span {
-    int off, end, packs;
-
-    __device__ __forceinline__ Span(int dim, int shift) : off(SHIFT ? shift : 0), end(off + dim), packs(SHIFT ? (end + VEC - 1) / VEC : dim / VEC) {}
-    // whether element j of pack i is one of the row's, for a pack below `packs`
-    __device__ __forceinline__ bool has(int i, int j) const { return !SHIFT || static_cast<unsigned>(i * VEC + j - off) < static_cast<unsigned>(end - off); }
-    __device__ __forceinline__ bool whole(int i) const { return !SHIFT || (i * VEC >= off && (i + 1) * VEC <= end); }
-};
 
 // A thread's 16 elements of a row: packs of VEC, pack k of lane l of a group of G being pack l + k G of the row.
 template <class T, int VEC>
@@ -72,26 +57,16 @@ struct Held {
     static constexpr int kPacks = kHeld / VEC;
     Pack p[kPacks];
 
-    // A row's packs on their way to `slots`, every kStep-th of which is the thread's, zeros behind the row.  What lies in pack 0
-    // before the row is the end of the row before it; the first row of a tensor has none.
-    template <int G, int kStep, class S>
-    static __device__ __forceinline__ void fetch(Pack *slots, const T *row, int lane, const S &span, const T *tensor)
+    // A row's packs on their way to `slots`, every kStep-th of which is the thread's.
+    template <int G, int kStep>
+    static __device__ __forceinline__ void fetch(Pack *slots, const T *row, int lane, int packs)
     {
-        const T *from = row - span.off;
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const int i = lane + k * G;
-            if (i >= span.packs) continue;
-            if (span.whole(i)) {
-                if constexpr (sizeof(Pack) == 16) cp_async16(slots + k * kStep, from + i * VEC);
-                else cp_async_first<sizeof(Pack)>(slots + k * kStep, from + i * VEC, sizeof(Pack));
-            } else if (from + i * VEC >= tensor) {
-                cp_async_first<sizeof(Pack)>(slots + k * kStep, from + i * VEC, min(span.end - i * VEC, VEC) * static_cast<int>(sizeof(T)));
-            } else {
-#pragma unroll 1
-                for (int j = 0; j < VEC; ++j) slots[k * kStep].x[j] = span.has(i, j) ? from[i * VEC + j] : from_f32<T>(0.0f);
+        for (int k = 0; k < kPacks; ++k)
+            if (lane + k * G < packs) {
+                if constexpr (sizeof(Pack) == 16) cp_async16(slots + k * kStep, row + (lane + k * G) * VEC);
+                else cp_async8(slots + k * kStep, row + (lane + k * G) * VEC);
             }
-        }
     }
     template <int kStep>
     static __device__ __forceinline__ void clear(Pack *slots)
@@ -99,15 +74,11 @@ struct Held {
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) slots[k * kStep] = Pack{};
     }
-    template <int kStep, class S>
-    __device__ __forceinline__ void take(const Pack *slots, int lane, const S &span)
+    template <int kStep>
+    __device__ __forceinline__ void take(const Pack *slots)
     {
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) p[k] = slots[k * kStep];
-        if (lane == 0 && span.off)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (j < span.off) p[0].x[j] = from_f32<T>(0.0f);
     }
     template <int G>
     __device__ __forceinline__ void load(const T *row, int lane, int packs)
@@ -137,10 +108,9 @@ struct Held {
             }
         }
     }
-    template <int G, class S>
-    static __device__ __forceinline__ void store(T *row, int lane, const S &span, const F2 (&y)[kHeld / 2])
+    template <int G>
+    static __device__ __forceinline__ void store(T *row, int lane, int packs, const F2 (&y)[kHeld / 2])
     {
-        T *to = row - span.off;
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
             Pack q;
@@ -151,28 +121,20 @@ struct Held {
                 unpack2(y[i / 2], a, b);
                 q.x[j] = from_f32<T>(i & 1 ? b : a);
             }
-            const int i = lane + k * G;
-            if (i >= span.packs) continue;
-            if (span.whole(i)) {
-                reinterpret_cast<Pack *>(to)[i] = q;
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (span.has(i, j)) to[i * VEC + j] = q.x[j];
-            }
+            if (lane + k * G < packs) reinterpret_cast<Pack *>(row)[lane + k * G] = q;
         }
     }
 };
 
 // The same elements of a weight of any type and alignment; `fill` for a weight that is NULL and outside the row.
-template <int G, int VEC, bool SHIFT>
-__device__ __forceinline__ void load_weight(const void *w, int32_t type, int lane, const Span<VEC, SHIFT> &span, float fill, F2 (&y)[kHeld / 2])
+template <int VEC, int G>
+__device__ __forceinline__ void load_weight(const void *w, int32_t type, int lane, int packs, float fill, F2 (&y)[kHeld / 2])
 {
     float f[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
         const int pack = lane + i / VEC * G;
-        f[i] = w && pack < span.packs && span.has(pack, i % VEC) ? load_any(w, type, pack * VEC + i % VEC - span.off) : fill;
+        f[i] = w && pack < packs ? load_any(w, type, pack * VEC + i % VEC) : fill;
     }
 #pragma unroll
     for (int i = 0; i < kHeld / 2; ++i) y[i] = pack2(f[2 * i], f[2 * i + 1]);
@@ -212,13 +174,6 @@ __device__ __forceinline__ void group_sync(int group)
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(G) : "memory");
 }
 
-// How far behind a pack's boundary a row starts.
-template <int VEC, class T>
-__device__ __forceinline__ int phase_of(const RowsOf<T> &t, const Rows &rows, uint32_t r)
-{
-    return static_cast<int>(reinterpret_cast<uintptr_t>(t.row(rows, r)) / sizeof(T) % VEC);
-}
-
 }  // namespace ea
 
 struct ea_layernorm {
@@ -235,7 +190,6 @@ namespace ea {
 constexpr int kPartCtas = 8;
 constexpr int64_t kMostHeld = kBackThreads * kHeld;                   // longer rows go the way of any width
 constexpr int kSumsBytes = kBackThreads * kHeld * 2 * sizeof(float);
-constexpr int kForwardThreads = 768;                                  // of an SM
 inline int64_t max_parts(const ea_layernorm_config &c)
 {
     if (c.dim <= kBackThreads * kHeld) return std::min<int64_t>(kMaxSms, std::max<int64_t>(c.max_rows, 1));  // one a CTA
@@ -304,35 +258,28 @@ void with_group(int64_t dim, F f)
     else f(Int<512>());
 }
 
-// How a call's rows can be read: in whole packs of VEC elements, in packs from the boundary before them, or one by one.
-enum Access { kWhole, kShifted, kSingle };
-
-struct AccessOf {
+// Whether a call's rows are whole packs of VEC elements, each on its boundary, and whether they follow one another at one
+// distance, whatever sequence they are in.
+struct RowsLie {
     const ea_layernorm_call *c;
     int64_t dim, vec;
-    bool whole = true, flat = true, alike = true;
-    int64_t phase = -1, step = 0;
+    bool whole = true, flat = true;
 
     void add(const void *p, int32_t type, int64_t outer, int64_t inner)
     {
         whole = whole && rows_on(vec * type_bytes(type), p, type, dim, c->outer, c->inner, outer, inner);
         flat = flat && (c->outer <= 1 || c->inner <= 1 || outer == c->inner * inner);
-        const int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(p) / type_bytes(type) % vec), by = (c->inner > 1 ? inner : outer) % vec;
-        alike = alike && (phase < 0 || (at == phase && by == step));
-        phase = at, step = by;
     }
-    // binary32 elements are read one by one as fast (7,021 x 769, gradient: 19.6 us; shifted 23.3)
-    Access get() const { return whole ? kWhole : vec > 4 && flat && alike && dim + vec - 1 <= kMostHeld ? kShifted : kSingle; }
 };
 
-// f(Int<G>, Int<VEC>, whether shifted) for an access of packs of VEC.
+// f(Int<G>, Int<elements of a pack>) for rows in packs of VEC, or one element after the other.
 template <int VEC, class F>
-void with_rows(int64_t dim, Access access, F f)
+void with_rows(int64_t dim, bool whole, F f)
 {
-    if (access == kWhole) with_group(dim, [&](auto group) { f(group, Int<VEC>(), std::false_type()); });
-    else if (access == kShifted) {
-        if constexpr (VEC > 4) with_group(dim + VEC - 1, [&](auto group) { f(group, Int<VEC>(), std::true_type()); });
-    } else with_group(dim, [&](auto group) { f(group, Int<1>(), std::false_type()); });
+    with_group(dim, [&](auto group) {
+        if (whole) f(group, Int<VEC>());
+        else f(group, Int<1>());
+    });
 }
 
 // A tensor's rows; where the call has one row in a sequence or one sequence, the rows of the other direction.

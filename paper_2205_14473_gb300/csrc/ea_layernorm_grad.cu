@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kColumnLanes *kJoinRows) ln_join_kernel(const 
 }
 
 // One CTA to an SM; groups of G threads walk through the rows, and leave the CTA's sums of dw and db in its part.
-template <class X, class Y, int VEC, bool SHIFT, int G>
+template <class X, class Y, int VEC, int G>
 __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnArgs a, const RowsOf<const Y> dys, const RowsOf<const X> xs, const float *stats,
                                                                       const RowsOf<const X> adds, const RowsOf<X> dxs, float *partial)
 {
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
     const int lane = threadIdx.x % G, group = threadIdx.x / G, warp = threadIdx.x / 32;
     const uint32_t stride = gridDim.x * kGroups;
     uint32_t r = blockIdx.x * kGroups + group;
-    const Span<VEC, SHIFT> span(static_cast<int>(a.dim), SHIFT ? phase_of<VEC>(xs, a.rows, r) : 0);
+    const int packs = static_cast<int>(a.dim / VEC);
     F2 w[kHeld / 2], dw[kHeld / 2], db[kHeld / 2];
     HX nx, na;
     HY ny;
@@ -115,16 +115,16 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
         s = row < a.n ? *reinterpret_cast<const float2 *>(stats + 2 * static_cast<int64_t>(row)) : make_float2(0.0f, 0.0f);
         if constexpr (kRing) {
             if (row < a.n) {
-                HX::template fetch<G, T>(ring_x + stage * (HX::kPacks * T), xs.row(a.rows, row), lane, span, xs.p);
-                HY::template fetch<G, T>(ring_y + stage * (HY::kPacks * T), dys.row(a.rows, row), lane, span, dys.p);
-                if (adds.p) HX::template fetch<G, T>(ring_add + stage * (HX::kPacks * T), adds.row(a.rows, row), lane, span, adds.p);
+                HX::template fetch<G, T>(ring_x + stage * (HX::kPacks * T), xs.row(a.rows, row), lane, packs);
+                HY::template fetch<G, T>(ring_y + stage * (HY::kPacks * T), dys.row(a.rows, row), lane, packs);
+                if (adds.p) HX::template fetch<G, T>(ring_add + stage * (HX::kPacks * T), adds.row(a.rows, row), lane, packs);
             } else {
                 HX::template clear<T>(ring_x + stage * (HX::kPacks * T));
                 HY::template clear<T>(ring_y + stage * (HY::kPacks * T));
             }
             cp_async_commit();
         } else {
-            const int there = row < a.n ? span.packs : 0;
+            const int there = row < a.n ? packs : 0;
             nx.template load<G>(xs.row(a.rows, row), lane, there);
             ny.template load<G>(dys.row(a.rows, row), lane, there);
         }
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
             HX::template clear<T>(ring_add + d * (HX::kPacks * T));
             fetch(r + d * stride, d, st[d]);
         }
-    load_weight<G>(a.w, a.weight_type, lane, span, 1.0f, w);
+    load_weight<VEC, G>(a.w, a.weight_type, lane, packs, 1.0f, w);
 #pragma unroll
     for (int i = 0; i < kHeld / 2; ++i) dw[i] = db[i] = both(0.0f);
     int buffer = 0, stage = 0;
@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
         F2 t[kHeld / 2], q[kHeld / 2];
         if constexpr (kRing) {
             cp_async_wait<kDepth - 1>();
-            nx.template take<T>(ring_x + stage * (HX::kPacks * T), lane, span);
-            ny.template take<T>(ring_y + stage * (HY::kPacks * T), lane, span);
+            nx.template take<T>(ring_x + stage * (HX::kPacks * T));
+            ny.template take<T>(ring_y + stage * (HY::kPacks * T));
         } else {
             fetch(r, 0, st[0]);
         }
@@ -162,8 +162,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
             q[i] = times2(q[i], w[i]);
         }
         if (adds.p) {
-            if constexpr (kRing) na.template take<T>(ring_add + stage * (HX::kPacks * T), lane, span);
-            else na.template load<G>(adds.row(a.rows, r), lane, on ? span.packs : 0);
+            if constexpr (kRing) na.template take<T>(ring_add + stage * (HX::kPacks * T));
+            else na.template load<G>(adds.row(a.rows, r), lane, on ? packs : 0);
         }
         if constexpr (kRing) {
 #pragma unroll
@@ -195,20 +195,20 @@ __global__ void __launch_bounds__(kBackThreads, 1) ln_backward_kernel(const LnAr
 #pragma unroll
             for (int i = 0; i < kHeld / 2; ++i) t[i] = add2(t[i], q[i]);
         }
-        if (on) Held<X, VEC>::template store<G>(dxs.row(a.rows, r), lane, span, t);
+        if (on) Held<X, VEC>::template store<G>(dxs.row(a.rows, r), lane, packs, t);
     }
     if (!partial) return;
     cp_async_wait<0>();
     __syncthreads();  // the sums take the ring's place
-    // column c of a row is element (off + c) % VEC of pack (off + c) / VEC
+    // column c of a row is element c % VEC of pack c / VEC
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
         const int pack = lane + i / VEC * G;
         float e, f, g, h;
         unpack2(dw[i / 2], e, f);
         unpack2(db[i / 2], g, h);
-        if (pack < span.packs && span.has(pack, i % VEC)) {
-            float *to = sums + group * (2 * kHeld * G) + pack * VEC + i % VEC - span.off;
+        if (pack < packs) {
+            float *to = sums + group * (2 * kHeld * G) + pack * VEC + i % VEC;
             to[0] = i & 1 ? f : e;
             to[kHeld * G] = i & 1 ? h : g;
         }
@@ -269,18 +269,18 @@ int ea_layernorm_backward(ea_layernorm *h, const ea_layernorm_call *c, const voi
             }
             if (!dx && !dw && !db) return;
             constexpr int kVec = 16 / sizeof(X);
-            AccessOf access{c, a.dim, kVec};
-            access.add(x, c->x_type, c->x_outer, c->x_inner);
-            access.add(dy, c->y_type, c->y_outer, c->y_inner);
-            if (dx) access.add(dx, c->x_type, c->dx_outer, c->dx_inner);
-            if (dx && add) access.add(add, c->x_type, c->add_outer, c->add_inner);
-            if (access.flat) a.rows = Rows{};
-            with_rows<kVec>(a.dim, access.get(), [&](auto group, auto vec, auto shift) {
+            RowsLie lie{c, a.dim, kVec};
+            lie.add(x, c->x_type, c->x_outer, c->x_inner);
+            lie.add(dy, c->y_type, c->y_outer, c->y_inner);
+            if (dx) lie.add(dx, c->x_type, c->dx_outer, c->dx_inner);
+            if (dx && add) lie.add(add, c->x_type, c->add_outer, c->add_inner);
+            if (lie.flat) a.rows = Rows{};
+            with_rows<kVec>(a.dim, lie.whole, [&](auto group, auto vec) {
                 constexpr int G = decltype(group)::value, V = decltype(vec)::value;
-                const uint32_t ctas = std::min<uint32_t>(over<uint32_t>(a.n, kBackThreads / G), std::max(h->dev.sms / 8 * 8, 1));
+                const uint32_t ctas = std::min<uint32_t>(over<uint32_t>(a.n, kBackThreads / G), h->dev.sms);
                 float *partial = dw || db ? h->partial : nullptr;
                 if (partial) parts = static_cast<int>(ctas);
-                auto kernel = ln_backward_kernel<X, Y, V, decltype(shift)::value, G>;
+                auto kernel = ln_backward_kernel<X, Y, V, G>;
                 const size_t ring = V > 1 ? kBackDepth<X, Y> * kBackThreads * kHeld * (2 * sizeof(X) + sizeof(Y)) : kSumsBytes;
                 e = h->allowed(kernel, ring);
                 if (e == cudaSuccess) kernel<<<ctas, kBackThreads, ring, h->stream>>>(a, dys, xs, stats, adds, dxs, partial);
