@@ -1,5 +1,12 @@
 // ea_scan.cu -- ea_scan_forward and ea_scan_backward.
 //
+// Bound by HBM where the columns fill the device, else by a step's latency along each sequence.  One GB300, us a call, GB/s of the
+// bytes that a call cannot do without, against a copy's 6,767:
+//   16 x 1024 x 1600 bf16            26.5 us, 5,950 GB/s; its gradient 51.3 us, 6,130 GB/s
+//   256 x 256 x 1024                 61.7 us, 6,520 GB/s
+//   2 x 65,536 x 1024                148 us, 5,430 GB/s (clusters of 8; 128 steps of 1.2 us)
+//   9 sequences of up to 3001 x 515 binary32, off any boundary, gradient  54 us, 4,110 GB/s
+//   1 x 65,536 x 128                 61 us (latency: clusters of 16, 32 CTAs in all)
 // h_t = f_t h_{t-1} + u_t composes: two pieces (A, B) and (A', B') of a sequence, each standing for h -> A h + B, are together
 // (A' A, A' B + B').  A cluster of CTAs takes the same columns of one sequence and walks along it, every CTA a chunk of rows at a
 // step: threads compose their rows, warps and CTAs compose what those left, the cluster's CTAs exchange theirs, and every
@@ -313,10 +320,10 @@ struct Tile {
     static constexpr int kLanes = V == 1 ? 32 : 8;            // lanes across a row
     static constexpr int kColumns = kLanes * V;
     static constexpr int kRows = S;
-    static constexpr int kSegs = NT / kLanes;       // threads along the rows
+    static constexpr int kSegs = NT / kLanes;                 // threads along the rows
     static constexpr int kChunk = kSegs * kRows;              // rows of a CTA in a step
     static constexpr bool kRing = V > 1;                      // rows come through shared memory, else through registers
-    static constexpr int kGroups = NT / kColumns;   // threads that compose a column's pieces, adjacent lanes
+    static constexpr int kGroups = NT / kColumns;             // threads that compose a column's pieces, adjacent lanes
     static constexpr int kPieces = kSegs / kGroups;           // of each of them
 };
 
@@ -680,10 +687,9 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
     return EA_OK;
 }
 
-#ifndef WPK
-#define WPK 256
-#endif
-constexpr int64_t kWalkRows = 16;  // sequences up to this length are walked along
+// Sequences up to this length are walked along, and any where there are so many 16-byte packs of columns to an SM: 512 x 33 x 1024 bf16
+// (431 packs) 21.5 us, in tiles 37.7; 512 x 100 x 1024 56.6 and 61.7; with 215 packs (256 x 256 x 1024) 106 and 61.7.
+constexpr int64_t kWalkRows = 16, kWalkPacks = 256;
 // Stages of a ring, and a thread's rows: 16-byte accesses without and within a cluster, and single elements.  Forward, 16 x 1024 x
 // 1600 bf16: 26.6 us; 3 stages 27.8, 2 rows 32.0.  2 x 65,536 x 1024 in clusters: 148 us; 4 rows 171.  Gradient of the former: 51.3 us; 3
 // stages 53.6, 4 rows 55.0, 1 row 59; in clusters (2 x 16,384 x 1024) 69.7 us; 2 rows 100, 8 rows 88.
@@ -692,9 +698,10 @@ constexpr int kRows = 4, kClusterRows = 8, kRowsOfOne = 8;
 constexpr int kBackRows = 2, kBackClusterRows = 4, kBackRowsOfOne = 8;
 
 // CTAs of a cluster along a sequence: 1 where the tiles alone occupy `fill` quarters of the SMs (an exchange costs as much as
-// a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes, and no more than the
-// sequence has chunks.  Clusters of 16 are for what occupies a part of the device even so (2 x 65,536 x 1024: 146 us in
-// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61).
+// a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes (8 x 2048 x 768: 29.6 us
+// without, 23.7 of two, 25.3 of four; a gradient of 9 x 3001 x 515, whose steps are longer: 76 us of two, 61 of four), and no more
+// than the sequence has chunks.  Clusters of 16 are for what occupies a part of the device even so (2 x 65,536 x 1024: 146 us in
+// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61).  Times of when the rule was made.
 template <class L>
 int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
 {
@@ -716,7 +723,7 @@ cudaError_t launch_tiles(ea_scan *s, const ScanArgs &a, int ranks, int stages, v
 
 bool walks(const ea_scan *s, const ScanArgs &a, int32_t type)
 {
-    return a.length <= kWalkRows || a.batch * a.dim * static_cast<int64_t>(type_bytes(type)) >= static_cast<int64_t>(s->dev.sms) * 16 * WPK;
+    return a.length <= kWalkRows || a.batch * a.dim * static_cast<int64_t>(type_bytes(type)) >= static_cast<int64_t>(s->dev.sms) * 16 * kWalkPacks;
 }
 
 bool states_on_16(const void *p, const void *q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) % 16 == 0; }

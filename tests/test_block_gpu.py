@@ -2,8 +2,9 @@
 
 Tolerances come from the operators' own roundings: u = 2^-24 for each operation in binary32, half a unit in the last place for
 the rounding to a 16-bit type, gamma_n = n u / (1 - n u) for a sum of n terms in any order (Higham, Accuracy and Stability of
-Numerical Algorithms, Section 4.2), and what CUDA's documentation gives for __expf, 2 + 1.173 |x| units in the last place,
-and __fdividef, 2 units.  Products of bounds (u^2 and the like) are covered by a factor of 1.01."""
+Numerical Algorithms, Section 4.2), and of a gate 6 + 1.2 |z| units of 2^-23: the documented 2 and 1 of the approximate power
+of two and reciprocal, 1.2 |z| of the exponent's product with log2 e, and the roundings of a sum and two products.  Products of
+bounds (u^2 and the like) are covered by a factor of 1.01."""
 import numpy as np
 import pytest
 import torch
