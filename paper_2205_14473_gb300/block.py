@@ -55,6 +55,14 @@ class _Block(_Handle):
             stride = t.stride()
         return t, stride[0] if n == 3 else 0, stride[-2] if n > 1 else 0
 
+    def _follows(self, t, shape, what) -> bool:
+        """Whether a tensor of rows of this shape is contiguous."""
+        if not isinstance(t, _Tensor) or t.device != self.device:
+            self._on_device(t, what)
+        if t.shape != shape:
+            _refuse(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+        return t.is_contiguous()
+
     def _written(self, t, shape, dtype, what):
         """(Its outer stride, its inner stride) for one that is written."""
         if not isinstance(t, _Tensor) or t.device != self.device:
@@ -207,24 +215,31 @@ class LayerNorm(_Block):
         if not isinstance(x, _Tensor) or x.device != self.device:
             self._on_device(x, "x")
         shape, new, given = x.shape, out is None, []
-        y, y_outer, y_inner = self._read(dy, shape, "dy")
-        if add is not None:
-            add, add_outer, add_inner = self._read(add, shape, "add")
-            if add.dtype != x.dtype:
-                _refuse(f"add is {add.dtype}, x {x.dtype}")
         if not new:
             outer, inner = self._written(out, shape, x.dtype, "out")
             given.append(out)
-        flat = x.is_contiguous() and y.is_contiguous() and (add is None or add.is_contiguous()) and (new or out.is_contiguous())
+        flat = self._follows(dy, shape, "dy") and x.is_contiguous() and (new or out.is_contiguous())
+        if add is not None:
+            flat = self._follows(add, shape, "add") and flat
+            if add.dtype != x.dtype:
+                _refuse(f"add is {add.dtype}, x {x.dtype}")
+        y = dy
+        if not flat:
+            y, y_outer, y_inner = self._read(dy, shape, "dy")
+            if add is not None:
+                add, add_outer, add_inner = self._read(add, shape, "add")
         c, x = self._x(x, flat)
         c.y_type = _TYPE.get(y.dtype) or _type(y.dtype, "dy")
         at = self._values(stats, (*shape[:-1], 2), _F32, "stats")
         w = None if weight is None else self._weight(weight, c, None, "weight")
-        if isinstance(dw, _Tensor):
-            given.append(dw)
-        if isinstance(db, _Tensor):
-            given.append(db)
-        dw, db = self._sums(dw, "dw"), self._sums(db, "db")
+        if dw is not None:
+            if isinstance(dw, _Tensor):
+                given.append(dw)
+            dw = self._sums(dw, "dw")
+        if db is not None:
+            if isinstance(db, _Tensor):
+                given.append(db)
+            db = self._sums(db, "db")
         if dw is not None and db is not None and dw.dtype != db.dtype:
             _refuse(f"dw is {dw.dtype}, db {db.dtype}")
         one = db if dw is None else dw
@@ -407,11 +422,12 @@ class Dropout(_Block):
             dtype = (out if given else residual if residual is not None else x).dtype
         if given:
             outer, inner = self._written(out, shape, dtype, "out")
+        flat = x.is_contiguous() and (not given or out.is_contiguous())
         if residual is not None:
-            residual, add_outer, add_inner = self._read(residual, shape, "residual")
+            flat = self._follows(residual, shape, "residual") and flat
             if residual.dtype != dtype:
                 _refuse(f"residual is {residual.dtype}, the result {dtype}")
-        if x.is_contiguous() and (residual is None or residual.is_contiguous()) and (not given or out.is_contiguous()):
+        if flat:
             c = self._flat
             c.dim = x.numel()
         else:
@@ -420,7 +436,7 @@ class Dropout(_Block):
             c.dim = shape[-1]
             x, c.x_outer, c.x_inner = self._read(x, shape, "x")
             if residual is not None:
-                c.add_outer, c.add_inner = add_outer, add_inner
+                residual, c.add_outer, c.add_inner = self._read(residual, shape, "residual")
             c.y_outer, c.y_inner = (outer, inner) if given else (c.inner * c.dim, c.dim)
         c.x_type, c.y_type = _TYPE.get(x.dtype) or _type(x.dtype, "x"), _TYPE.get(dtype) or _type(dtype, "the result")
         if not given:
