@@ -62,29 +62,36 @@ __global__ void __launch_bounds__(kColumnLanes *kColumnRows) ln_columns_any_kern
     }
 }
 
-// The parts' sums added, each of a warp's in order and then the warps': a CTA takes 32 columns of dw (blockIdx.y = 0) or db.
-constexpr int kJoinRows = 32;
+// The parts' sums added: a CTA takes 32 columns of dw (blockIdx.y = 0) or db, a warp every 32nd part, kJoinAhead of them on their
+// way at a time, and then a column's 32 sums.
+constexpr int kJoinRows = 32, kJoinAhead = 5;
 
 __global__ void __launch_bounds__(kColumnLanes *kJoinRows) ln_join_kernel(const LnArgs a, const float *partial, int parts, void *dw, void *db, int accumulate)
 {
-    __shared__ float red[kJoinRows][kColumnLanes];
+    __shared__ float red[kJoinRows][kColumnLanes + 1];
     const int lane = threadIdx.x % kColumnLanes, row = threadIdx.x / kColumnLanes;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * kColumnLanes, column = first + lane;
     void *out = blockIdx.y ? db : dw;
     pdl_wait();
     if (!out) return;
-    const int64_t column = static_cast<int64_t>(blockIdx.x) * kColumnLanes + lane;
     float s = 0.0f;
-    if (column < a.dim)
-#pragma unroll 8
-        for (int k = row; k < parts; k += kJoinRows) s = __fadd_rn(s, partial[(static_cast<int64_t>(k) * 2 + blockIdx.y) * a.dim + column]);
+    const float *from = partial + blockIdx.y * a.dim + column;
+    for (int k = row; k < parts; k += kJoinRows * kJoinAhead) {
+        float v[kJoinAhead];
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j) {
+            const int64_t part = k + j * kJoinRows;
+            v[j] = part < parts && column < a.dim ? from[part * 2 * a.dim] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j) s = __fadd_rn(s, v[j]);
+    }
     red[row][lane] = s;
     __syncthreads();
-    if (row || column >= a.dim) return;
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kJoinRows; ++i) s = __fadd_rn(s, red[i][lane]);
-    if (accumulate) s = __fadd_rn(s, load_any(out, a.grad_type, column));
-    store_any(out, a.grad_type, column, s);
+    s = warp_sum(red[lane][row]);
+    if (lane || first + row >= a.dim) return;
+    if (accumulate) s = __fadd_rn(s, load_any(out, a.grad_type, first + row));
+    store_any(out, a.grad_type, first + row, s);
 }
 
 // One CTA to an SM; groups of G threads walk through the rows, and leave the CTA's sums of dw and db in its part.
