@@ -6,7 +6,7 @@
 //   256 x 256 x 1024                 61.7 us, 6,520 GB/s
 //   2 x 65,536 x 1024                148 us, 5,430 GB/s (clusters of 8; 128 steps of 1.2 us)
 //   9 sequences of up to 3001 x 515 binary32, off any boundary, gradient  54 us, 4,110 GB/s
-//   1 x 65,536 x 128                 61 us (latency: clusters of 16, 32 CTAs in all)
+//   1 x 65,536 x 128                 28 us (latency: 8 steps of clusters of 16, 128 CTAs in all)
 // h_t = f_t h_{t-1} + u_t composes: two pieces (A, B) and (A', B') of a sequence, each standing for h -> A h + B, are together
 // (A' A, A' B + B').  A cluster of CTAs takes the same columns of one sequence and walks along it, every CTA a chunk of rows at a
 // step: threads compose their rows, warps and CTAs compose what those left, the cluster's CTAs exchange theirs, and every
@@ -313,11 +313,11 @@ __global__ void __launch_bounds__(kWalkThreads) scan_walk_back_kernel(const Scan
 
 // ---------------------------------------------------------------------------------------------- tiles
 // A thread's V columns are 16 bytes where rows allow it (eight lanes then cover a 128-byte piece of a row), else one element
-// (a warp covers 32 columns).  S: its rows.  NT: threads of the CTA.
-template <class T, int V, int S, int NT>
+// (a warp covers 32 columns).  S: its rows.  NT: threads of the CTA.  NARROW: two lanes of 16 bytes instead of eight.
+template <class T, int V, int S, int NT, bool NARROW>
 struct Tile {
     static constexpr int kThreads = NT;
-    static constexpr int kLanes = V == 1 ? 32 : 8;            // lanes across a row
+    static constexpr int kLanes = V == 1 ? 32 : NARROW ? 2 : 8;  // lanes across a row
     static constexpr int kColumns = kLanes * V;
     static constexpr int kRows = S;
     static constexpr int kSegs = NT / kLanes;                 // threads along the rows
@@ -325,17 +325,19 @@ struct Tile {
     static constexpr bool kRing = V > 1;                      // rows come through shared memory, else through registers
     static constexpr int kGroups = NT / kColumns;             // threads that compose a column's pieces, adjacent lanes
     static constexpr int kPieces = kSegs / kGroups;           // of each of them
+    static constexpr int kTurn = V > 32 / kGroups ? V : 32 / kGroups;
 };
 
-// What a tile's CTA shares, behind its ring of copies.  A piece's columns are turned around within 32 lanes' worth by its group,
-// so that the lanes that read a column's pieces fall into different banks.
+// What a tile's CTA shares, behind its ring of copies.  A piece's columns are turned around by its group, kTurn of them (what a warp
+// reads of a piece, and no less than a thread writes) for each, so that the lanes that read a column's pieces fall into different
+// banks.
 template <class L, bool CLUSTER>
 struct TileShared {
     static constexpr int kRanks = CLUSTER ? kMaxCluster : 1;
     uint64_t arrived[2];                                       // barriers of `rank`
     float a[L::kSegs][L::kColumns], b[L::kSegs][L::kColumns];  // each thread's composition, then in b the state it starts with
     float2 rank[2][kRanks][L::kColumns];                       // the CTAs' compositions, of this step and the last
-    static __device__ __forceinline__ int at(int seg, int column) { return column ^ (seg / L::kPieces * (32 / L::kGroups)); }
+    static __device__ __forceinline__ int at(int seg, int column) { return column ^ (seg / L::kPieces * L::kTurn % L::kColumns); }
 };
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -451,10 +453,10 @@ __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V>
 }
 
 // blockIdx.x: sequence and tile of columns, in clusters along the rows (blockIdx.x / ranks is the tile).
-template <class T, int V, int S, int NT, int DEPTH, bool CLUSTER>
+template <class T, int V, int S, int NT, bool NARROW, int DEPTH, bool CLUSTER>
 __global__ void __launch_bounds__(NT) scan_tile_kernel(const ScanArgs a, const Seq<const T> zs, const Seq<const T> vs, const Seq<T> hs, float *final)
 {
-    using L = Tile<T, V, S, NT>;
+    using L = Tile<T, V, S, NT, NARROW>;
     using W = Vec<T, V>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(16) TileShared<L, CLUSTER> sh;
@@ -537,10 +539,10 @@ __global__ void __launch_bounds__(NT) scan_tile_kernel(const ScanArgs a, const S
 }
 
 // The same from the sequence's last row to its first.
-template <class T, int V, int S, int NT, int DEPTH, bool CLUSTER>
+template <class T, int V, int S, int NT, bool NARROW, int DEPTH, bool CLUSTER>
 __global__ void __launch_bounds__(NT) scan_tile_back_kernel(const ScanArgs a, const ScanGrads<T> g)
 {
-    using L = Tile<T, V, S, NT>;
+    using L = Tile<T, V, S, NT, NARROW>;
     using W = Vec<T, V>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(16) TileShared<L, CLUSTER> sh;
@@ -690,6 +692,7 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
 // Sequences up to this length are walked along, and any where there are so many 16-byte packs of columns to an SM: 512 x 33 x 1024 bf16
 // (431 packs) 21.5 us, in tiles 37.7; 512 x 100 x 1024 56.6 and 61.7; with 215 packs (256 x 256 x 1024) 106 and 61.7.
 constexpr int64_t kWalkRows = 16, kWalkPacks = 256;
+constexpr int64_t kFewRows = 512;  // a chunk of a narrow tile, forward
 // Stages of a ring, and a thread's rows: 16-byte accesses without and within a cluster, and single elements.  Forward, 16 x 1024 x
 // 1600 bf16: 26.6 us; 3 stages 27.8, 2 rows 32.0.  2 x 65,536 x 1024 in clusters: 148 us; 4 rows 171.  Gradient of the former: 51.3 us; 3
 // stages 53.6, 4 rows 55.0, 1 row 59; in clusters (2 x 16,384 x 1024) 69.7 us; 2 rows 100, 8 rows 88.
@@ -701,7 +704,7 @@ constexpr int kBackRows = 2, kBackClusterRows = 4, kBackRowsOfOne = 8;
 // a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes (8 x 2048 x 768: 29.6 us
 // without, 23.7 of two, 25.3 of four; a gradient of 9 x 3001 x 515, whose steps are longer: 76 us of two, 61 of four), and no more
 // than the sequence has chunks.  Clusters of 16 are for what occupies a part of the device even so (2 x 65,536 x 1024: 146 us in
-// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61).  Times of when the rule was made.
+// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61, before tiles were narrow there).  Times of when the rule was made.
 template <class L>
 int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
 {
@@ -709,6 +712,15 @@ int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
     int ranks = 1;
     while (ranks < kMaxCluster && ranks < chunks && tiles * ranks * 4 < sms * fill && (ranks < 8 || tiles * 16 <= sms)) ranks *= 2;
     return ranks;
+}
+
+// Whether long sequences have so few columns that clusters of 16 leave SMs idle: tiles of a quarter of the columns then, whose
+// CTAs take four times as many rows at a step (1 x 65,536 x 128 bf16 28 us instead of 62, its gradient 53 instead of 105;
+// 1 x 4,096 x 64 4.4 instead of 5.7; 2 x 65,536 x 1024, with 32 wide tiles, 211 instead of 148).
+template <class L>
+bool few_tiles(const ea_scan *s, const ScanArgs &a)
+{
+    return a.length > kFewRows && a.batch * over<int64_t>(a.dim, L::kColumns) * kMaxCluster <= s->dev.sms;
 }
 
 template <class L, class... KArgs, class... Args>
@@ -794,16 +806,19 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
             constexpr int S = V == 1 ? kRowsOfOne : kRows, SC = V == 1 ? kRowsOfOne : kClusterRows;
-            using L = Tile<T, V, S, kTileThreads>;
-            using LC = Tile<T, V, SC, kTileThreads>;
+            using L = Tile<T, V, S, kTileThreads, false>;
+            using LC = Tile<T, V, SC, kTileThreads, false>;
+            using LN = Tile<T, V, SC, kTileThreads, (V > 1)>;
             if (walk) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, zs, vs, hs, final);
                 e = cudaGetLastError();
             } else {
                 const int ranks = scan_ranks<LC>(s, a, 5);
-                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 2, scan_tile_kernel<T, V, SC, kTileThreads, kDepth, true>, zs, vs, hs, final);
-                else e = launch_tiles<L>(s, a, 1, kDepth * 2, scan_tile_kernel<T, V, S, kTileThreads, kDepth, false>, zs, vs, hs, final);
+                if (V > 1 && few_tiles<LC>(s, a))
+                    e = launch_tiles<LN>(s, a, scan_ranks<LN>(s, a, 5), kDepth * 2, scan_tile_kernel<T, V, SC, kTileThreads, (V > 1), kDepth, true>, zs, vs, hs, final);
+                else if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 2, scan_tile_kernel<T, V, SC, kTileThreads, false, kDepth, true>, zs, vs, hs, final);
+                else e = launch_tiles<L>(s, a, 1, kDepth * 2, scan_tile_kernel<T, V, S, kTileThreads, false, kDepth, false>, zs, vs, hs, final);
             }
         });
     });
@@ -843,16 +858,19 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
         with_columns<T>(all, [&](auto columns) {
             constexpr int V = decltype(columns)::value;
             constexpr int S = V == 1 ? kBackRowsOfOne : kBackRows, SC = V == 1 ? kBackRowsOfOne : kBackClusterRows;
-            using L = Tile<T, V, S, kTileThreads>;
-            using LC = Tile<T, V, SC, kTileThreads>;
+            using L = Tile<T, V, S, kTileThreads, false>;
+            using LC = Tile<T, V, SC, kTileThreads, false>;
+            using LN = Tile<T, V, SC, kTileThreads, (V > 1)>;
             if (walk) {
                 const int64_t ctas = over<int64_t>(a.batch * (a.dim / V), kWalkThreads);
                 scan_walk_back_kernel<T, V><<<static_cast<unsigned>(ctas), kWalkThreads, 0, s->stream>>>(a, g);
                 e = cudaGetLastError();
             } else {
                 const int ranks = scan_ranks<LC>(s, a, 9);
-                if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 4, scan_tile_back_kernel<T, V, SC, kTileThreads, kDepth, true>, g);
-                else e = launch_tiles<L>(s, a, 1, kDepth * 4, scan_tile_back_kernel<T, V, S, kTileThreads, kDepth, false>, g);
+                if (V > 1 && few_tiles<LC>(s, a))
+                    e = launch_tiles<LN>(s, a, scan_ranks<LN>(s, a, 9), kDepth * 4, scan_tile_back_kernel<T, V, SC, kTileThreads, (V > 1), kDepth, true>, g);
+                else if (ranks > 1) e = launch_tiles<LC>(s, a, ranks, kDepth * 4, scan_tile_back_kernel<T, V, SC, kTileThreads, false, kDepth, true>, g);
+                else e = launch_tiles<L>(s, a, 1, kDepth * 4, scan_tile_back_kernel<T, V, S, kTileThreads, false, kDepth, false>, g);
             }
         });
     });
