@@ -51,8 +51,8 @@ int ea_layernorm_init(const ea_layernorm_config *cfg, void *workspace, size_t wo
 
 /* y = (x - mean) * rstd * w + b for every row, mean its mean, rstd = 1 / sqrt(variance + eps) with the variance about that
  * mean; in binary32, rounded once to y's type.  w, b: dim values, or NULL for ones and zeros.  stats: NULL, or two binary32
- * values per row (mean, rstd; row (i, j) at 2 (i * inner + j)) for the backward call.  y may be x, with the same strides and
- * type. */
+ * values per row (mean, rstd; row (i, j) at 2 (i * inner + j)) for the backward call, aligned to 8 bytes.  y may be x, with
+ * the same strides and type. */
 int ea_layernorm_forward(ea_layernorm *h, const ea_layernorm_call *c, const void *x, const void *w, const void *b, void *y, float *stats);
 
 /* With t = (x - mean) * rstd and q = dy * w, per row
@@ -109,7 +109,8 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
                      const void *lengths, const float *d_final, void *dz, void *dv, float *d_initial);
 
 /* Synchronize the stream; EA_E_CUDA for a CUDA error, EA_E_DEVICE_CHECK if a length since the last such call lay outside
- * [0, length]. */
+ * [0, length], EA_E_TIMEOUT if a wait between the CTAs of a cluster ran out (after two seconds; what the call wrote is then
+ * not to be used). */
 int ea_scan_sync_status(ea_scan *s);
 int ea_scan_destroy(ea_scan *s);
 
