@@ -277,6 +277,21 @@ def test_norm_sums_alone(dim, off):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("wt", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 100, 8200])
+def test_norm_weights_at_any_address(wt, dim):
+    """Pieces of flat vectors, off every boundary."""
+    x, dy, w, b = _randn(9, dim, seed=37), _randn(9, dim, seed=38), _randn(dim, seed=39, dtype=wt), _randn(dim, seed=40, dtype=wt)
+    norm, flat = ea.LayerNorm(dim, 9), torch.full((2 * dim + 9,), 7.0, device="cuda", dtype=wt)
+    y, stats = norm.forward(x, w, b)
+    for k in (1, 3, 4):
+        assert _same(norm.forward(x, _off(w, k), _off(b, k + 1))[0], y)
+        flat.fill_(7.0)
+        got = norm.grad(dy, x, stats, _off(w, k), dw=flat[k:k + dim], db=flat[k + dim + 1:k + 2 * dim + 1])
+        _check_grad(got, dy, x, stats, w)
+        assert (flat[:k] == 7).all() and float(flat[k + dim]) == 7 and (flat[k + 2 * dim + 1:] == 7).all()
+
+
 def test_norm_of_no_rows():
     norm, x, stats = ea.LayerNorm(8, 4), torch.zeros(0, 8, device="cuda"), torch.zeros(0, 2, device="cuda")
     dw, db = torch.full((2, 8), 3.0, device="cuda")
@@ -589,6 +604,24 @@ def test_pieces_of_a_sequence():
     late = scan.grad(dh[:, cut:], z[:, cut:], v[:, cut:], b, initial=mid, d_final=last, d_initial=True)
     early = scan.grad(dh[:, :cut], z[:, :cut], v[:, :cut], a, initial=first, d_final=late[2], d_initial=True)
     _check_scan_grad((torch.cat([early[0], late[0]], 1), torch.cat([early[1], late[1]], 1), early[2]), dh, z, v, h, first, None, last)
+
+
+@pytest.mark.parametrize("length", [0, 1, 5, 40, 700])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_states_at_any_address(length, dtype):
+    """States that lie at no more than their element's boundary, and no sequences at all."""
+    z, v, dh, first, last = _scan_inputs(3, length, 64, dtype, seed=13)
+    scan = ea.GatedScan(64)
+    h, final, got = _check_both(scan, z, v, dh, first, last)
+    for k in (1, 2, 3):
+        state, late = _off(first, k), _off(last, k)
+        out = scan.forward(z, v, initial=state, final=state)
+        _check_scan(out[0], out[1], z, v, first)
+        back = scan.grad(dh, z, v, h, initial=_off(first, k), d_final=late, d_initial=late)
+        _check_scan_grad(back, dh, z, v, h, first, None, last)
+    none, end = scan.forward(z[:0], v[:0], final=True)
+    assert none.shape == (0, length, 64) and end.shape == (0, 64)
+    assert scan.grad(dh[:0], z[:0], v[:0], h[:0], d_initial=True)[2].shape == (0, 64)
 
 
 def test_scan_gradient_against_differences():
