@@ -4,8 +4,9 @@
  * gradient.
  *
  * Calls, streams, workspaces, graphs, devices and errors are as in ea_lm.h: every call is asynchronous on the stream
- * given to the init call, except ea_scan_sync_status; the library allocates no device memory; a handle belongs to one
- * device and to one host thread at a time; a call that is refused has done nothing, and ea_last_error(NULL) says why.
+ * given to the init call, except the *_sync_status and *_selftest_* calls; the library allocates no device memory; a
+ * handle belongs to one device and to one host thread at a time; a call that is refused has done nothing, and
+ * ea_last_error(NULL) says why.
  *
  * Tensors are rows of `dim` consecutive elements, outer x inner of them: row (i, j) lies at i * outer stride +
  * j * inner stride elements from the address.  Strides of what is read may be any that stay inside the caller's memory
@@ -113,6 +114,11 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
  * not to be used). */
 int ea_scan_sync_status(ea_scan *s);
 int ea_scan_destroy(ea_scan *s);
+
+/* The exchange between the CTAs of a cluster by itself, with this limit (in cycles of the SM) of its waits: EA_OK with
+ * *timed_out = 0 where all of them take part (silent = -1), and with 1 where CTA `silent` (0 .. 3) stops halfway: the others'
+ * waits run out, and the kernel ends. */
+int ea_scan_selftest_exchange(int64_t limit_cycles, int32_t silent, void *stream, int32_t *timed_out);
 
 /* ------------------------------------------------------------------------------- dropout */
 

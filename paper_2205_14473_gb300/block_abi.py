@@ -49,8 +49,10 @@ def declare(L) -> None:
     L.ea_scan_forward.argtypes = [_P, ctypes.POINTER(ea_scan_call), _P, _P, _P, _P, _P, _P]
     L.ea_scan_backward.argtypes = [_P, ctypes.POINTER(ea_scan_call), _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]
     L.ea_scan_sync_status.argtypes = [_P]
+    L.ea_scan_selftest_exchange.argtypes = [_i64, _i32, _P, ctypes.POINTER(_i32)]
     L.ea_dropout_apply.argtypes = [_P, ctypes.POINTER(ea_dropout_call), _P, _P, _u64, _P, _P]
 
 
 EXPORTED = [f"{n}_{f}" for n in ("ea_layernorm", "ea_scan", "ea_dropout") for f in ("workspace_bytes", "init", "destroy")] + [
-    "ea_layernorm_forward", "ea_layernorm_backward", "ea_scan_forward", "ea_scan_backward", "ea_scan_sync_status", "ea_dropout_apply"]
+    "ea_layernorm_forward", "ea_layernorm_backward", "ea_scan_forward", "ea_scan_backward", "ea_scan_sync_status", "ea_scan_selftest_exchange",
+    "ea_dropout_apply"]

@@ -371,7 +371,7 @@ __device__ __forceinline__ void store_remote(float2 *p, uint64_t *bar, uint32_t 
 // A CTA's place in its cluster, and the step that its exchange is at.
 struct Exchange {
     uint32_t rank = 0, ranks = 1, step = 0;
-    bool late = false;  // whether a wait has run out
+    bool late = false;  // whether a wait of this thread has run out
 
     template <class S>
     __device__ __forceinline__ void begin(S &sh)
@@ -384,6 +384,29 @@ struct Exchange {
         }
         cluster_sync();  // before any CTA stores into another
     }
+
+    // A column's composition, sent to all CTAs of the cluster by a group of G threads, into one of two buffers, and a wait for
+    // theirs; returns the buffer that they are in.  A CTA sends the next but one after it has waited for the next, which the
+    // others send after this one is read.  A thread whose wait has run out sends no more: the other CTAs' waits run out at
+    // this step or the next then, and no barrier counts what belongs to a step that its CTA is not at.
+    template <class S>
+    __device__ __forceinline__ uint32_t pass(S &sh, float2 all, int column, int columns, int group, int G, uint32_t *status, long long limit = kWaitLimitCycles)
+    {
+        const uint32_t buffer = step & 1;
+        if (!late) {
+            if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.arrived[buffer], ranks * columns * 8);
+            for (uint32_t r = group; r < ranks; r += G) store_remote(&sh.rank[buffer][rank][column], &sh.arrived[buffer], r, all);
+            if (!mbar_wait(&sh.arrived[buffer], step >> 1 & 1, limit)) {
+                late = true;
+                report_status(status, kStatusTimeout);
+            }
+        }
+        ++step;
+        return buffer;
+    }
+
+    // Every CTA stays until the last one has stopped sending: completed waits say so, one that has run out does not.
+    __device__ __forceinline__ void end() { cluster_sync(); }
 };
 
 template <int V>
@@ -393,8 +416,7 @@ __device__ __forceinline__ void to_shared(float *p, const Lanes<V> &a)
 }
 
 // From each thread's composition (A, B) of its rows to the state that it starts with.  carry: the state before the step of
-// column threadIdx.x / kGroups, and the one after it on return.  A CTA's composition goes to all CTAs of its cluster, into one
-// of two buffers: a CTA sends the next but one after it has waited for the next, which the others send after this one is read.
+// column threadIdx.x / kGroups, and the one after it on return.
 template <bool CLUSTER, class L, int V>
 __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V> &B, float &carry, TileShared<L, CLUSTER> &sh, Exchange &x, uint32_t *status)
 {
@@ -426,19 +448,12 @@ __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V>
     y = __shfl_up_sync(0xffffffffu, y, 1, G);
     float state = carry;
     if constexpr (CLUSTER) {
-        const uint32_t buffer = x.step & 1;
-        if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.arrived[buffer], x.ranks * L::kColumns * 8);
-        for (uint32_t r = group; r < x.ranks; r += G) store_remote(&sh.rank[buffer][x.rank][column], &sh.arrived[buffer], r, all);
-        if (!x.late && !mbar_wait(&sh.arrived[buffer], x.step >> 1 & 1)) {
-            x.late = true;
-            report_status(status, kStatusTimeout);
-        }
+        const uint32_t buffer = x.pass(sh, all, column, L::kColumns, group, G, status);
         for (uint32_t r = 0; r < x.ranks; ++r) {
             if (r == x.rank) state = carry;
             const float2 c = sh.rank[buffer][r][column];
             carry = __fmaf_rn(c.x, carry, c.y);
         }
-        ++x.step;
     } else {
         carry = __fmaf_rn(all.x, carry, all.y);
     }
@@ -536,6 +551,7 @@ __global__ void __launch_bounds__(NT) scan_tile_kernel(const ScanArgs a, const S
         for (int64_t t = n + x.rank * L::kSegs + threadIdx.x / L::kLanes; t < a.length; t += x.ranks * L::kSegs)
             *reinterpret_cast<W *>(hs.p + (i * hs.batch + t * hs.row + c)) = zero;
     if (final && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) final[i * a.dim + column] = carry;
+    if constexpr (CLUSTER) x.end();
 }
 
 // The same from the sequence's last row to its first.
@@ -646,6 +662,38 @@ __global__ void __launch_bounds__(NT) scan_tile_back_kernel(const ScanArgs a, co
             *reinterpret_cast<W *>(g.dv.p + (i * g.dv.batch + t * g.dv.row + c)) = zero;
         }
     if (g.d_initial && column < a.dim && x.rank == 0 && threadIdx.x % L::kGroups == 0) g.d_initial[i * a.dim + column] = carry;
+    if constexpr (CLUSTER) x.end();
+}
+
+// ---------------------------------------------------------------------------------------------- self-test
+constexpr int kTestRanks = 4, kTestSteps = 8, kTestColumns = 32;
+
+struct TestShared {
+    uint64_t arrived[2];
+    float2 rank[2][kTestRanks][kTestColumns];
+};
+
+__device__ uint32_t g_exchange_status;
+
+// One cluster whose CTAs exchange kTestSteps times.  CTA `silent` (-1: none) stops halfway, as one whose own wait has run out.
+__global__ void __launch_bounds__(kWalkThreads) scan_exchange_kernel(long long limit, int silent)
+{
+    constexpr int G = kWalkThreads / kTestColumns;
+    __shared__ __align__(16) TestShared sh;
+    Exchange x;
+    x.begin(sh);
+    const int column = threadIdx.x / G;
+    for (int t = 0; t < kTestSteps; ++t) {
+        if (t == kTestSteps / 2 && static_cast<int>(x.rank) == silent) x.late = true;
+        const float2 mine = make_float2(static_cast<float>(x.rank), static_cast<float>(t * kTestColumns + column));
+        const uint32_t buffer = x.pass(sh, mine, column, kTestColumns, threadIdx.x % G, G, &g_exchange_status, limit);
+        for (int r = 0; r < kTestRanks && !x.late; ++r) {
+            const float2 c = sh.rank[buffer][r][column];
+            if (c.x != static_cast<float>(r) || c.y != mine.y) report_status(&g_exchange_status, kStatusCheck);
+        }
+        __syncthreads();  // read before the next but one is sent
+    }
+    x.end();
 }
 
 }  // namespace ea
@@ -887,6 +935,26 @@ int ea_scan_sync_status(ea_scan *s)
     if (r != EA_OK) return r;
     if (st & kStatusTimeout) return lm_fail(EA_E_TIMEOUT, "a wait within a cluster ran out");
     if (st & kStatusLength) return lm_fail(EA_E_DEVICE_CHECK, "a sequence's length lay outside its rows");
+    return EA_OK;
+}
+
+int ea_scan_selftest_exchange(int64_t limit_cycles, int32_t silent, void *stream, int32_t *timed_out)
+{
+    if (!timed_out) return lm_fail(EA_E_INVAL, "timed_out is NULL");
+    if (limit_cycles < 1 || limit_cycles > kWaitLimitCycles)
+        return lm_fail(EA_E_INVAL, "limit_cycles must be in [1, %lld]", static_cast<long long>(kWaitLimitCycles));
+    if (silent < -1 || silent >= kTestRanks) return lm_fail(EA_E_INVAL, "silent is a CTA, or -1 for none");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const uint32_t zero = 0;
+    uint32_t st = 0;
+    cudaError_t e = cudaMemcpyToSymbolAsync(g_exchange_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess)
+        e = launch_lm(scan_exchange_kernel, dim3(kTestRanks), kWalkThreads, 0, s, false, kTestRanks, static_cast<long long>(limit_cycles), static_cast<int>(silent));
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbolAsync(&st, g_exchange_status, sizeof st, 0, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e != cudaSuccess) return lm_cuda(e, "exchange self-test");
+    if (st & kStatusCheck) return lm_fail(EA_E_DEVICE_CHECK, "an exchange delivered other values than were sent");
+    *timed_out = st & kStatusTimeout ? 1 : 0;
     return EA_OK;
 }
 
