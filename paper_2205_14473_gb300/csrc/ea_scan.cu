@@ -396,7 +396,7 @@ struct Exchange {
         if (!late) {
             if (threadIdx.x == 0) mbar_arrive_expect_tx(&sh.arrived[buffer], ranks * columns * 8);
             for (uint32_t r = group; r < ranks; r += G) store_remote(&sh.rank[buffer][rank][column], &sh.arrived[buffer], r, all);
-            if (!mbar_wait(&sh.arrived[buffer], step >> 1 & 1, limit)) {
+            if (!mbar_wait<true>(&sh.arrived[buffer], step >> 1 & 1, limit)) {
                 late = true;
                 report_status(status, kStatusTimeout);
             }

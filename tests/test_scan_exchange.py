@@ -42,3 +42,19 @@ def test_waits_that_run_out_end_the_kernel():
     rows = [scan.step(z[:, t], v[:, t], state) for t in range(40)]
     assert (h[:, :40] - torch.stack(rows, 1)).abs().max() <= 800 * 2.0 ** -24 * v.abs().max()
     scan.sync()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch,length,dim", [(1, 300, 512), (1, 700, 2048), (2, 5000, 64), (1, 9000, 256), (3, 1200, 33)])
+def test_every_run_of_clusters_gives_the_same_bits(batch, length, dim):
+    """In clusters of two and more, wide and narrow tiles and single elements: what another CTA of the cluster sends is seen
+    whole, every time."""
+    assert [_exchange(200_000_000, -1) for _ in range(200)] == [(ea.EA_OK, 0)] * 200
+    z, v, dh = torch.randn(3, batch, length, dim, device="cuda", generator=torch.Generator(device="cuda").manual_seed(length)).unbind()
+    scan = ea.GatedScan(dim)
+    h, final = scan.forward(z, v, final=True)
+    want = [h, final, *scan.grad(dh, z, v, h, d_initial=True)]
+    for _ in range(50):
+        out, last = scan.forward(z, v, final=True)
+        assert all(torch.equal(a, b) for a, b in zip(want, [out, last, *scan.grad(dh, z, v, h, d_initial=True)]))
+    scan.sync()
