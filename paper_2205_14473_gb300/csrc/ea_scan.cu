@@ -737,9 +737,23 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
     return EA_OK;
 }
 
-// Sequences up to this length are walked along, and any where there are so many 16-byte packs of columns to an SM: 512 x 33 x 1024 bf16
-// (431 packs) 21.5 us, in tiles 37.7; 512 x 100 x 1024 56.6 and 61.7; with 215 packs (256 x 256 x 1024) 106 and 61.7.
+// Sequences up to kWalkRows are walked along; longer ones where so many 16-byte packs of columns are there to an SM that each
+// thread's loads fill the device, and no longer than this: a tile's chunk of rows, and its exchange, costs the same whether
+// its rows are there or not, and what it reads is further ahead.  bf16, us walked and in tiles:
+//   forward (4 rows of loads ahead)   320 x 33 x 1024 (270 packs) 18.2 and 24.6, x 48 0.95 of the tiles' time, x 64 1.12, x 256 113.7 and 75.4;
+//     512 x 33 x 1024 (431 packs) 21.4 and 37.4, x 100 56.4 and 61.5, x 128 70.9 and 65.3;  256 x 64 x 1024 (215 packs) 1.27
+//   gradient (none)   320 x 33 x 1024 35.2 and 31.6, x 256 248 and 149;  400 x 33 x 1024 (337 packs) 0.97, x 40 44.9 and 40.3;
+//     512 x 33 x 1024 41.8 and 47.8, x 40 50.1 and 49.9, x 64 77.5 and 58.8, x 256 296 and 236;  1024 x 48 x 1024 (862 packs) 0.91,
+//     x 64 1.05, x 65 121.7 and 131.4, x 80 0.98, x 128 1.02;  700 x 48 x 1024 (589 packs) 1.01;  in single elements 300 x 17 x 1025 (253 packs) 27.9 and 38.9, x 40 58.8 and
+//     58.5, 320 x 48 x 1025 70.4 and 63.2
+// That is where columns fill at least three quarters of their tiles; else any length is walked from kWalkPacks on: 45,600 x 300 x 8 (an
+// eighth, 300 packs) 183 and 679, gradient 418 and 1,111;  27,000 x 300 x 40 (0.62) 330 and 425, 723 and 724;  23,000 x 300 x 48 (0.75) 358 and 359, 757 and 604.
 constexpr int64_t kWalkRows = 16, kWalkPacks = 256;
+struct WalkRule {
+    int64_t packs, rows;  // from so many packs an SM, up to so many rows
+};
+constexpr WalkRule kWalk[] = {{kWalkPacks, 48}, {400, 100}};
+constexpr WalkRule kWalkBack[] = {{400, 40}, {600, 48}, {800, 80}}, kWalkBackOfOne[] = {{kWalkPacks, 40}, {600, 48}};
 constexpr int64_t kFewRows = 512;  // a chunk of a narrow tile, forward
 // Stages of a ring, and a thread's rows: 16-byte accesses without and within a cluster, and single elements.  Forward, 16 x 1024 x
 // 1600 bf16: 26.6 us; 3 stages 27.8, 2 rows 32.0.  2 x 65,536 x 1024 in clusters: 148 us; 4 rows 171.  Gradient of the former: 51.3 us; 3
@@ -781,9 +795,16 @@ cudaError_t launch_tiles(ea_scan *s, const ScanArgs &a, int ranks, int stages, v
     return launch_lm(kernel, dim3(static_cast<unsigned>(tiles * ranks)), L::kThreads, ring, s->stream, false, ranks, a, std::forward<Args>(args)...);
 }
 
-bool walks(const ea_scan *s, const ScanArgs &a, int32_t type)
+// whole: whether the call's tensors are read in 16-byte accesses.
+template <size_t N>
+bool walks(const ea_scan *s, const ScanArgs &a, int32_t type, bool whole, const WalkRule (&rules)[N])
 {
-    return a.length <= kWalkRows || a.batch * a.dim * static_cast<int64_t>(type_bytes(type)) >= static_cast<int64_t>(s->dev.sms) * 16 * kWalkPacks;
+    if (a.length <= kWalkRows) return true;
+    const int64_t size = type_bytes(type), columns = whole ? 8 * 16 / size : 32;
+    const bool full = 4 * a.dim >= 3 * over(a.dim, columns) * columns;
+    const int64_t packs = a.batch * a.dim * size / (static_cast<int64_t>(s->dev.sms) * 16);
+    if (!full) return packs >= kWalkPacks;
+    return std::any_of(rules, rules + N, [&](const WalkRule &r) { return packs >= r.packs && a.length <= r.rows; });
 }
 
 bool states_on_16(const void *p, const void *q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) % 16 == 0; }
@@ -842,10 +863,9 @@ int ea_scan_forward(ea_scan *s, const ea_scan_call *c, const void *z, const void
         if (r == EA_OK) r = check_rows_apart(a.batch, a.length, c->h_batch, c->h_row, a.dim, "h");
     }
     if (r != EA_OK || !a.batch || (!a.length && !final)) return r;
-    const bool walk = walks(s, a, c->type);
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
-    const bool all = wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) && wide(h, c->h_batch, c->h_row) &&
-                     (!walk || states_on_16(initial, final));
+    const bool whole = wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) && wide(h, c->h_batch, c->h_row);
+    const bool walk = walks(s, a, c->type, whole, kWalk), all = whole && (!walk || states_on_16(initial, final));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
@@ -891,11 +911,11 @@ int ea_scan_backward(ea_scan *s, const ea_scan_call *c, const void *dh, const vo
     }
     if (r == EA_OK && d_initial && d_initial == initial) r = lm_fail(EA_E_INVAL, "d_initial may not be initial");
     if (r != EA_OK || !a.batch || (!a.length && !d_initial)) return r;
-    const bool walk = walks(s, a, c->type);
     auto wide = [&](const void *p, int64_t batch, int64_t row) { return rows_on(16, p, c->type, a.dim, a.batch, a.length, batch, row); };
-    const bool all = wide(dh, c->dh_batch, c->dh_row) && wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) &&
-                     wide(h, c->h_batch, c->h_row) && wide(dz, c->dz_batch, c->dz_row) && wide(dv, c->dv_batch, c->dv_row) &&
-                     (!walk || (states_on_16(initial, d_final) && states_on_16(d_initial, nullptr)));
+    const bool whole = wide(dh, c->dh_batch, c->dh_row) && wide(z, c->z_batch, c->z_row) && wide(v, c->v_batch, c->v_row) &&
+                       wide(h, c->h_batch, c->h_row) && wide(dz, c->dz_batch, c->dz_row) && wide(dv, c->dv_batch, c->dv_row);
+    const bool walk = whole ? walks(s, a, c->type, true, kWalkBack) : walks(s, a, c->type, false, kWalkBackOfOne);
+    const bool all = whole && (!walk || (states_on_16(initial, d_final) && states_on_16(d_initial, nullptr)));
     cudaError_t e = cudaSuccess;
     with_float(c->type, [&](auto *t) {
         using T = std::remove_reference_t<decltype(*t)>;
