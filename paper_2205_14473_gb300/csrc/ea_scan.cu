@@ -405,8 +405,13 @@ struct Exchange {
         return buffer;
     }
 
-    // Every CTA stays until the last one has stopped sending: completed waits say so, one that has run out does not.
-    __device__ __forceinline__ void end() { cluster_sync(); }
+    // A CTA whose waits have all been completed is sent no more, and may end.  One with a wait that has run out stays until every
+    // thread of the cluster has come here.
+    __device__ __forceinline__ void end()
+    {
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        if (late) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
 };
 
 template <int V>
@@ -693,6 +698,7 @@ __global__ void __launch_bounds__(kWalkThreads) scan_exchange_kernel(long long l
         }
         __syncthreads();  // read before the next but one is sent
     }
+    if (silent < 0 && x.rank == 0) x.late = true;  // stays until the others, who do not wait, have come to their end
     x.end();
 }
 
