@@ -421,7 +421,8 @@ __device__ __forceinline__ void to_shared(float *p, const Lanes<V> &a)
 }
 
 // From each thread's composition (A, B) of its rows to the state that it starts with.  carry: the state before the step of
-// column threadIdx.x / kGroups, and the one after it on return.
+// column threadIdx.x / kGroups, and the one after it on return.  In a cluster the state before the first step is in the first
+// CTA's hands alone, as part of what that makes of it: the same CTA writes the last state, which may lie in the same place.
 template <bool CLUSTER, class L, int V>
 __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V> &B, float &carry, TileShared<L, CLUSTER> &sh, Exchange &x, uint32_t *status)
 {
@@ -448,14 +449,16 @@ __device__ __forceinline__ Lanes<V> tile_start(const Lanes<V> &A, const Lanes<V>
             m = __fmul_rn(m, a);
         }
     }
-    const float2 all = make_float2(__shfl_sync(0xffffffffu, m, G - 1, G), __shfl_sync(0xffffffffu, y, G - 1, G));
+    float2 all = make_float2(__shfl_sync(0xffffffffu, m, G - 1, G), __shfl_sync(0xffffffffu, y, G - 1, G));
     m = __shfl_up_sync(0xffffffffu, m, 1, G);
     y = __shfl_up_sync(0xffffffffu, y, 1, G);
     float state = carry;
     if constexpr (CLUSTER) {
+        const bool first = x.step == 0 && x.rank == 0;
+        if (first) all = make_float2(0.0f, __fmaf_rn(all.x, carry, all.y)), carry = 0.0f;
         const uint32_t buffer = x.pass(sh, all, column, L::kColumns, group, G, status);
         for (uint32_t r = 0; r < x.ranks; ++r) {
-            if (r == x.rank) state = carry;
+            if (r == x.rank && !first) state = carry;
             const float2 c = sh.rank[buffer][r][column];
             carry = __fmaf_rn(c.x, carry, c.y);
         }
@@ -488,7 +491,7 @@ __global__ void __launch_bounds__(NT) scan_tile_kernel(const ScanArgs a, const S
     const bool inside = c < a.dim;
     const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk;
     const int64_t column = c0 + threadIdx.x / L::kGroups;  // of the state that this thread carries
-    float carry = column < a.dim && a.initial ? a.initial[i * a.dim + column] : 0.0f;
+    float carry = column < a.dim && a.initial && x.rank == 0 ? a.initial[i * a.dim + column] : 0.0f;
     // This thread's first row of the step that is fetched, and of the step at hand, as rows that are left from there on.
     const int64_t first = x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S;
     int next = static_cast<int>(n - first), left = next;
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(NT) scan_tile_back_kernel(const ScanArgs a, co
     const bool inside = c < a.dim;
     const int64_t n = scan_length(a, i), stride = static_cast<int64_t>(x.ranks) * L::kChunk;
     const int64_t column = c0 + threadIdx.x / L::kGroups;
-    float carry = column < a.dim && g.d_final ? g.d_final[i * a.dim + column] : 0.0f;
+    float carry = column < a.dim && g.d_final && x.rank == 0 ? g.d_final[i * a.dim + column] : 0.0f;
     // Rows count from the end here: this thread's first ones of the step that is fetched and of the step at hand.
     const int64_t top = n - 1 - (x.rank * static_cast<int64_t>(L::kChunk) + threadIdx.x / L::kLanes * S);
     int next = static_cast<int>(top), t0 = next;

@@ -34,3 +34,17 @@ def test_wide_batches(batch, dim, length):
     # a sequence's results do not depend on the others, but for how it is cut into pieces
     few = scan.forward(z[:3], v[:3], initial=first[:3], final=True)
     _check_scan(few[0], few[1], z[:3], v[:3], first[:3])
+
+
+@pytest.mark.parametrize("batch,length,dim", [(2, 40, 1600), (3, 130, 512), (2, 300, 512), (1, 700, 2048), (1, 1100, 64), (2, 9000, 24), (1, 1100, 33)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_states_in_place(batch, length, dim, dtype):
+    """The last states into the first ones' memory (and their gradients'), which every CTA of a cluster has read by then."""
+    z, v, dh, first, last = _scan_inputs(batch, length, dim, dtype, seed=21)
+    scan = ea.GatedScan(dim)
+    h, final, got = _check_both(scan, z, v, dh, first, last)
+    for _ in range(30):
+        s, d = first.clone(), last.clone()
+        out, end = scan.forward(z, v, initial=s, final=s)
+        assert end is s and _same(s, final) and _same(out, h)
+        assert all(_same(p, q) for p, q in zip(scan.grad(dh, z, v, h, initial=first, d_final=d, d_initial=d), got))
