@@ -772,17 +772,18 @@ constexpr int kRows = 4, kClusterRows = 8, kRowsOfOne = 8;
 constexpr int kBackRows = 2, kBackClusterRows = 4, kBackRowsOfOne = 8;
 
 // CTAs of a cluster along a sequence: 1 where the tiles alone occupy `fill` quarters of the SMs (an exchange costs as much as
-// a step: 16 x 1024 x 1600 bf16 28.5 us without, 39 with clusters of two); else as many as that takes (8 x 2048 x 768: 29.6 us
-// without, 23.7 of two, 25.3 of four; a gradient of 9 x 3001 x 515, whose steps are longer: 76 us of two, 61 of four), and no more
-// than the sequence has chunks.  Clusters of 16 are for what occupies a part of the device even so (2 x 65,536 x 1024: 146 us in
-// clusters of 8, 214 of 16, as not all of them fit at once; 65,536 x 128: 108 and 61, before tiles were narrow there).  Times of when the rule was made.
+// a step: 16 x 1024 x 1600 bf16 26.7 us without, 35.8 with clusters of two); else as many as that takes, in powers of two (8 x 2048 x
+// 768: 24.4 us without, 21.5 of two, 23.2 of four;  a gradient of 9 x up to 3001 x 515, whose steps are longer, 62.7 of two and 52.7 of four,
+// of full sequences 68.7 and 78.8), and no more than the sequence has chunks (a gradient of 1 x 1100 x 256, five chunks:
+// 4.1 us of five, 5.3 of eight, three of which have no rows, 5.6 of four).  Clusters of 16 are for what occupies a part of the device even
+// so (2 x 65,536 x 1024: 147.6 us in clusters of 8, 219 of 16, as not all of them fit at once).
 template <class L>
 int scan_ranks(const ea_scan *s, const ScanArgs &a, int fill)
 {
     const int64_t tiles = a.batch * over<int64_t>(a.dim, L::kColumns), chunks = over<int64_t>(a.length, L::kChunk), sms = s->dev.sms;
     int ranks = 1;
     while (ranks < kMaxCluster && ranks < chunks && tiles * ranks * 4 < sms * fill && (ranks < 8 || tiles * 16 <= sms)) ranks *= 2;
-    return ranks;
+    return static_cast<int>(std::min<int64_t>(ranks, std::max<int64_t>(chunks, 1)));
 }
 
 // Whether long sequences have so few columns that clusters of 16 leave SMs idle: tiles of a quarter of the columns then, whose

@@ -48,3 +48,15 @@ def test_states_in_place(batch, length, dim, dtype):
         out, end = scan.forward(z, v, initial=s, final=s)
         assert end is s and _same(s, final) and _same(out, h)
         assert all(_same(p, q) for p, q in zip(scan.grad(dh, z, v, h, initial=first, d_final=d, d_initial=d), got))
+
+
+# Of 16-byte accesses a cluster takes 128 rows to a CTA and 64 back, in narrow tiles 512 (and 256), of single elements 32.
+@pytest.mark.parametrize("batch,dim,rows,dtype,chunks", [(6, 256, 128, BF16, 3), (6, 256, 128, BF16, 5), (6, 256, 64, BF16, 3), (6, 256, 64, BF16, 7),
+                                                         (1, 64, 512, F16, 3), (1, 64, 512, F16, 5), (1, 64, 256, F16, 11), (1, 33, 32, F32, 3),
+                                                         (1, 33, 32, F32, 6), (1, 33, 32, F32, 9), (1, 33, 32, F32, 13), (1, 33, 32, F32, 15)])
+def test_clusters_of_every_number_of_chunks(batch, dim, rows, dtype, chunks):
+    """No more CTAs in a cluster than the sequence has chunks, so also numbers that are no powers of two."""
+    z, v, dh, first, last = _scan_inputs(batch, chunks * rows - 1, dim, dtype, seed=22)
+    scan = ea.GatedScan(dim)
+    _check_both(scan, z, v, dh, first, last)
+    scan.sync()
