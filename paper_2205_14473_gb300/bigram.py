@@ -59,6 +59,8 @@ class Bigram:
     """The parameters (one flat vector) and a worker's gradient."""
 
     def __init__(self, vocab: int, dim: int, tokens: int, device, seed: int = 0, blocks: int = 0, dropout: float = 0.0):
+        if dropout and not blocks:
+            raise ValueError("dropout is in the blocks, and there are none")
         self.vocab, self.dim, self.scale = vocab, dim, dim ** 0.5
         self.sizes = [vocab * dim, dim * dim, dim] + [dim, dim, 2 * dim * dim, 2 * dim, dim * dim] * blocks
         gen = torch.Generator(device=device).manual_seed(seed)
@@ -169,4 +171,6 @@ if __name__ == "__main__":
     ap.add_argument("--blocks", type=int, default=0)
     ap.add_argument("--dropout", type=float, default=0.0)
     a = ap.parse_args()
+    if a.dropout and not a.blocks:
+        ap.error("--dropout is in the blocks: it needs --blocks")
     train(a.optimizer, workers=a.workers, steps=a.steps, lr=a.lr, log=print, blocks=a.blocks, dropout=a.dropout)
