@@ -157,6 +157,8 @@ def train(optimizer: str = "adamw", vocab: int = 512, dim: int = 64, sequences: 
         if log and (t % 20 == 0 or t == steps - 1):
             log(f"step {t:4d}  loss {float(losses[-1]):.4f}")
     model.table.sync()
+    if blocks:
+        model.scan.sync()
     if optimizer == "round":
         rnd.sync()
     return [float(x) for x in losses]
