@@ -213,7 +213,9 @@ __device__ __forceinline__ void store_states(float *p, const Lanes<V> &a)
     }
 }
 
-// With e = 2^(-z log2 e), at most 2^126:  f = 1 / (1 + e) and 1 - f = e f, each with a small relative error at either end.
+// With e = 2^(-z log2 e), at most 2^126:  f = 1 / (1 + e) and 1 - f = e f.  In units of 2^-23, relative: e is off by 2 of the power of
+// two and 0.61 |z| of its rounded exponent, f and 1 - f by no more than that (each has a factor below 1 for it) and 0.5 of the sum, 1
+// of the reciprocal and 0.5 of the product: 4 + 0.7 |z|, where the smaller of the two is small, and less for the other.
 // 2^-126 less makes f 0 where e is at its limit and does not change an f of 2^-101 or more.
 template <int V>
 __device__ __forceinline__ void gate(const Lanes<V> &z, Lanes<V> &f, Lanes<V> &shut)
