@@ -93,8 +93,10 @@ int ea_scan_init(const ea_scan_config *cfg, void *workspace, size_t workspace_by
 /* In every sequence and column, with f_t = 1 / (1 + exp(-z_t)),
  *   h_t = f_t h_{t-1} + (1 - f_t) v_t,    h_{-1} = initial,
  * the states carried in binary32 and each rounded once to h's type.  f and 1 - f each are within (4 + 0.7 |z|) 2^-23 of
- * themselves (exp's argument is a rounded product, whose absolute error grows with |z|) and 2^-126.  A state that is not finite
- * leaves the later ones of its column not finite.  initial: batch x dim binary32 values, or NULL for zeros.  final: NULL, or batch x dim binary32 values that receive every sequence's last state; it may be initial.
+ * themselves (exp's argument is a rounded product, whose absolute error grows with |z|) and 2^-126.  Each is rounded by itself,
+ * and each of the terms that make up a state is off by up to 2^-21 of itself for every row that it is carried through (2^-25 was
+ * measured where gates nearly hold): over that many rows of such gates f and 1 - f do not keep a state between its inputs as a
+ * mean would.  A state that is not finite leaves the later ones of its column not finite.  initial: batch x dim binary32 values, or NULL for zeros.  final: NULL, or batch x dim binary32 values that receive every sequence's last state; it may be initial.
  * lengths: NULL, or one length per sequence on the device: rows from there on are not read, their h is 0, and the state after
  * the last row before them is the final one (the initial one for a length of 0).  A length outside [0, length] counts as
  * the nearest of the two, and ea_scan_sync_status reports it.  h may be z or v, with the same strides. */
