@@ -60,3 +60,101 @@ def test_clusters_of_every_number_of_chunks(batch, dim, rows, dtype, chunks):
     scan = ea.GatedScan(dim)
     _check_both(scan, z, v, dh, first, last)
     scan.sync()
+
+
+# batch, length, dim of each plan, in 16 bits and in 32.
+PLANS = {
+    "short": (5, 5, 40), "short at its limit": (6, 16, 264), "wide": (320, 45, 1024), "wide and thin": (9200, 70, 40), "tiles": (100, 70, 512),
+    "tiles of several chunks": (30, 300, 512), "clusters": (6, 700, 256), "narrow tiles": (4, 1500, 64),
+}
+
+
+def _ends_of(batch, length, kind):
+    g = torch.Generator().manual_seed(batch + length)
+    ends = torch.randint(0, length + 1, (batch,), generator=g)
+    ends[:4] = torch.tensor([0, 1, length, length - 1])
+    return ends.to(kind).cuda()
+
+
+def _halves_of(a, b):
+    both = torch.cat([a, b], 2)
+    return both[..., :a.shape[2]], both[..., a.shape[2]:]
+
+
+def _by_time(t):
+    return t.transpose(0, 1).contiguous().transpose(0, 1)
+
+
+def _inside(t, k):
+    """A copy of t in longer and more rows, k elements in, and the whole of it."""
+    whole = torch.full((t.shape[0], t.shape[1] + 2, t.shape[2] + 16), 7.0, device="cuda", dtype=t.dtype)
+    piece = whole[:, 1:-1, k:k + t.shape[2]]
+    piece.copy_(t)
+    return piece, whole
+
+
+@pytest.mark.parametrize("layout", ["rows", "halves", "by time", "pieces", "pieces off a boundary", "in place"])
+@pytest.mark.parametrize("dtype,kind", [(BF16, torch.int64), (F16, torch.int32), (F32, torch.int32)])
+@pytest.mark.parametrize("plan", PLANS)
+def test_ragged_batches_of_every_plan(plan, dtype, kind, layout):
+    """Lengths of zero, one, all rows and between, NaN behind them, in the layouts that a call takes."""
+    batch, length, dim = PLANS[plan]
+    z, v, dh, first, last = _scan_inputs(batch, length, dim, dtype, seed=23)
+    lengths = _ends_of(batch, length, kind)
+    behind = torch.arange(length, device="cuda")[None] >= lengths[:, None]
+    clean = [t.masked_fill(behind[..., None], 0.0) for t in (z, v, dh)]
+    for t in (z, v, dh):
+        t[behind] = float("nan")
+    scan, wholes, out, dz, dv = ea.GatedScan(dim), [], None, None, None
+    if layout == "halves":
+        (z, v), (dz, dv) = _halves_of(z, v), _halves_of(z, v)
+    elif layout == "by time":
+        z, v, dh, out, dz, dv = (_by_time(t) for t in (z, v, dh, z, z, v))
+    elif layout.startswith("pieces"):
+        k = 8 if layout == "pieces" else 3
+        (z, _), (v, _), (dh, _) = (_inside(t, k) for t in (z, v, dh))
+        (out, a), (dz, b), (dv, c) = (_inside(t, k) for t in (z, z, v))
+        wholes = [(a, out), (b, dz), (c, dv)]
+        first, last = _off(first, k), _off(last, k)
+    if layout == "in place":
+        out = z.clone()
+        h, final = scan.forward(out, v, initial=first, lengths=lengths, out=out, final=True)
+    else:
+        h, final = scan.forward(z, v, initial=first, lengths=lengths, out=out, final=True)
+    assert out is None or h is out
+    _check_scan(h, final, clean[0], clean[1], first, lengths)
+    assert _same(final[0], first[0])
+    h = h.masked_fill(behind[..., None], float("nan"))
+    if layout == "in place":
+        dz, dv, d = z, dh, last.clone()
+        got = scan.grad(dv, dz, v, h, initial=first, lengths=lengths, d_final=d, dz=dz, dv=dv, d_initial=d)
+    else:
+        got = scan.grad(dh, z, v, h, initial=first, lengths=lengths, d_final=last, dz=dz, dv=dv, d_initial=True)
+    _check_scan_grad(got, clean[2], clean[0], clean[1], h.masked_fill(behind[..., None], 0.0), first, lengths, last)
+    assert _same(got[2][0], last[0])
+    for whole, piece in wholes:  # nothing beside what was asked for
+        piece.fill_(7.0)
+        assert (whole == 7.0).all()
+    scan.sync()
+
+
+@pytest.mark.parametrize("dtype,kind", [(BF16, torch.int64), (F16, torch.int32)])
+@pytest.mark.parametrize("plan", PLANS)
+def test_lengths_outside_the_rows_of_every_plan(plan, dtype, kind):
+    """They count as the nearest that are inside, and sync() raises for them, once."""
+    batch, length, dim = PLANS[plan]
+    z, v, dh, first, last = _scan_inputs(batch, length, dim, dtype, seed=24)
+    lengths = _ends_of(batch, length, kind)
+    inside = lengths.clone()
+    lengths[0], lengths[2], lengths[3], inside[3] = -1, length + 1, torch.iinfo(kind).max, length
+    scan = ea.GatedScan(dim)
+    want = scan.forward(z, v, initial=first, lengths=inside, final=True)
+    back = scan.grad(dh, z, v, want[0], initial=first, lengths=inside, d_final=last, d_initial=True)
+    scan.sync()
+    for f, ref in ((lambda: scan.forward(z, v, initial=first, lengths=lengths, final=True), want),
+                   (lambda: scan.grad(dh, z, v, want[0], initial=first, lengths=lengths, d_final=last, d_initial=True), back)):
+        assert all(_same(a, b) for a, b in zip(f(), ref))
+        with pytest.raises(ea.EAError) as ex:
+            scan.sync()
+        assert ex.value.status == ea.EA_E_DEVICE_CHECK
+        scan.sync()
