@@ -140,12 +140,6 @@ __device__ __forceinline__ void load_weight(const void *w, int32_t type, int lan
     for (int i = 0; i < kHeld / 2; ++i) y[i] = pack2(f[2 * i], f[2 * i + 1]);
 }
 
-__device__ __forceinline__ F2 times2(F2 a, F2 b)
-{
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
 __device__ __forceinline__ float total(F2 a)
 {
     float x, y;

@@ -98,12 +98,6 @@ struct Lanes<1> {
 __device__ __forceinline__ float fma2(float a, float b, float c) { return __fmaf_rn(a, b, c); }
 __device__ __forceinline__ float add2(float a, float b) { return __fadd_rn(a, b); }
 __device__ __forceinline__ float times2(float a, float b) { return __fmul_rn(a, b); }
-__device__ __forceinline__ F2 times2(F2 a, F2 b)
-{
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
 template <int V>
 __device__ __forceinline__ Lanes<V> fma(const Lanes<V> &a, const Lanes<V> &b, const Lanes<V> &c)
 {
