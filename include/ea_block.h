@@ -51,9 +51,9 @@ int ea_layernorm_workspace_bytes(const ea_layernorm_config *cfg, size_t *bytes);
 int ea_layernorm_init(const ea_layernorm_config *cfg, void *workspace, size_t workspace_bytes, void *stream, ea_layernorm **out);
 
 /* y = (x - mean) * rstd * w + b for every row, mean its mean, rstd = 1 / sqrt(variance + eps) with the variance about that
- * mean; in binary32, rounded once to y's type.  w, b: dim values, or NULL for ones and zeros.  stats: NULL, or two binary32
- * values per row (mean, rstd; row (i, j) at 2 (i * inner + j)) for the backward call, aligned to 8 bytes.  y may be x, with
- * the same strides and type. */
+ * mean; in binary32, rounded once to y's type (of a row whose sum or squares pass binary32's range, y is not to be used).
+ * w, b: dim values, or NULL for ones and zeros.  stats: NULL, or two binary32 values per row (mean, rstd; row (i, j) at
+ * 2 (i * inner + j)) for the backward call, aligned to 8 bytes.  y may be x, with the same strides and type. */
 int ea_layernorm_forward(ea_layernorm *h, const ea_layernorm_call *c, const void *x, const void *w, const void *b, void *y, float *stats);
 
 /* With t = (x - mean) * rstd and q = dy * w, per row
@@ -96,7 +96,9 @@ int ea_scan_init(const ea_scan_config *cfg, void *workspace, size_t workspace_by
  * themselves (exp's argument is a rounded product, whose absolute error grows with |z|) and 2^-126.  Each is rounded by itself,
  * and each of the terms that make up a state is off by up to 2^-21 of itself for every row that it is carried through (2^-25 was
  * measured where gates nearly hold): over that many rows of such gates f and 1 - f do not keep a state between its inputs as a
- * mean would.  A state that is not finite leaves the later ones of its column not finite.  initial: batch x dim binary32 values, or NULL for zeros.  final: NULL, or batch x dim binary32 values that receive every sequence's last state; it may be initial.
+ * mean would.  A state that is not finite leaves the later ones of its column not finite.
+ * initial: batch x dim binary32 values, or NULL for zeros.  final: NULL, or batch x dim binary32 values that receive every
+ * sequence's last state; it may be initial.
  * lengths: NULL, or one length per sequence on the device: rows from there on are not read, their h is 0, and the state after
  * the last row before them is the final one (the initial one for a length of 0).  A length outside [0, length] counts as
  * the nearest of the two, and ea_scan_sync_status reports it.  h may be z or v, with the same strides. */

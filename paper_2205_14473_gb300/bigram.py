@@ -10,6 +10,10 @@ vector [E, M, b], as EARound takes it.  A worker's step is
     table.grad(tokens, de, out=dE, accumulate=True)         the lookup's part, added to it
     clip = norm([g])                        the gradient's norm and clipping factor
 
+and the parameters move either by AdamW on the clipped mean gradient (32- or 8-bit states), or by a round of
+Efficient-Adam, in which every worker compresses its clipped gradient's Adam step.  A gradient that is not finite is not
+used: AdamW skips the step, a worker of the round takes part with a gradient of zeros.
+
 With blocks, the model sees more than the current token: between lookup and head stand residual blocks of a gated linear
 recurrence, e <- e + dropout(scan(z, v) O) with [z, v] = layernorm(e) A + a, whose parameters (the norm's weight and bias, A, a,
 O) follow in the flat vector:
@@ -18,10 +22,6 @@ O) follow in the flat vector:
     h, _ = scan.forward(z, v)               e = drop(h O, counter, residual=e)
 
 and back the same way, every operator by its own gradient.
-
-and the parameters move either by AdamW on the clipped mean gradient (32- or 8-bit states), or by a round of
-Efficient-Adam, in which every worker compresses its clipped gradient's Adam step.  A gradient that is not finite is not
-used: AdamW skips the step, a worker of the round takes part with a gradient of zeros.
 
     python -m paper_2205_14473_gb300.bigram --optimizer adamw8
     python -m paper_2205_14473_gb300.bigram --optimizer round --workers 4

@@ -263,7 +263,8 @@ class LayerNorm(_Block):
 
 class GatedScan(_Block):
     """The gated linear recurrence h_t = f_t h_{t-1} + (1 - f_t) v_t, f = sigmoid(z), in every column of sequences of rows of
-    dim values, and its gradient.  z, v, h and their gradients are of one type; states are float32, of shape (batch, dim)."""
+    dim values, and its gradient.  z, v, h and their gradients are of one type; states are float32, of shape (batch, dim).  f and 1 - f are
+    rounded by themselves: over very many rows of gates that nearly hold, states drift (include/ea_block.h says how far)."""
 
     _kind = "ea_scan"
 

@@ -2,7 +2,7 @@
 //
 // Bound by HBM, with the generator's 60 instructions for eight elements beside it (half of the ALU's slots).  One GB300, us a call,
 // GB/s of the bytes that a call cannot do without, against a copy's 6,767:
-//   16,384 x 1600 bf16, with a residual   25.3 us, 6,210 GB/s; off a 16-byte boundary 34.5, rows of 1601 in 1611 55
+//   16,384 x 1600 bf16, with a residual   25.3 us, 6,210 GB/s; off a 16-byte boundary 36, without and rows of 1601 in 1611 58
 //   65,536 x 1600 bf16, without           68.0 us, 6,170 GB/s
 //   260,096 x 768, binary32 to bf16       173.4 us, 6,910 GB/s
 #include "ea_block.cuh"
@@ -47,7 +47,7 @@ __device__ __forceinline__ Y drop_one(const DropArgs &a, uint32_t half, X x, con
 
 // Any rows: a warp takes 256 consecutive elements of the call, a lane forms the words of eight of them, and through shared memory every
 // lane gets the half words of every 32nd, so that accesses of single elements lie side by side (16,384 x 1600 bf16 with a residual,
-// off every boundary, 34.5 us; 87 with eight consecutive elements a lane).  FLAT: all rows are one.
+// off every boundary, 36 us; 87 with eight consecutive elements a lane).  FLAT: all rows are one.
 template <class X, class Y, bool FLAT>
 __global__ void __launch_bounds__(kDropThreads) dropout_any_kernel(const DropArgs a, const RowsOf<const X> xs, const RowsOf<const Y> adds, const RowsOf<Y> ys)
 {

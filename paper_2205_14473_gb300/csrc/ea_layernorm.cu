@@ -2,10 +2,12 @@
 //
 // Mean and variance: each warp's mean and the squares about it, joined (Chan, Golub and LeVeque, "Updating formulae and a
 // pairwise algorithm for computing sample variances"), so that the variance does not cancel and a row costs one barrier.
-// Bound by instructions (issue slots 60% used, 194 for a warp's part of a row) where rows are whole 16-byte packs, else by accesses
-// of single elements.  One GB300, us a call, GB/s of the bytes that a call cannot do without, against a copy's 6,767:
+// Bound by a row's chain of dependent steps (two reductions by shuffles and a barrier one behind another, one row at a time in a CTA:
+// issue slots 60% used by 28 warps an SM, 194 instructions for a warp's part of a row) where rows are whole 16-byte packs, else
+// by accesses of single elements.  One GB300, us a call, GB/s of the bytes that a call cannot do without, against a copy's 6,767:
 //   16,384 x 1600 bf16 21.5 us, 4,900 GB/s; 1601 wide 28.5;  262,144 x 128 23.7 us, 5,760 GB/s;  8,192 x 4,096 26 us, 5,170 GB/s
-//   16,384 x 1600, binary32 to bf16 27 us, 5,800 GB/s
+//   16,384 x 1600, binary32 to bf16 27 us, 5,800 GB/s;  4,096 x 8,192 bf16 33.7 us, 3,990 GB/s, one CTA to an SM
+//   rows that registers do not hold, read three times by single elements: 4,096 x 12,288 bf16 161 us, 1,250 GB/s
 #include "ea_layernorm.cuh"
 
 namespace ea {

@@ -2,8 +2,9 @@
 //
 // The gradients of weight and bias are sums over rows: every thread keeps those of its columns, a CTA's groups are added at its
 // end, and a second launch adds the CTAs' in order.
-// Bound by instructions and HBM together (issue slots 58% used).  One GB300, us a call, GB/s as in ea_layernorm.cu:
-//   16,384 x 1600 bf16 with the residual's gradient 39.4 us, 5,320 GB/s; 1601 wide 63;  8,192 x 4,096 48 us, 5,600 GB/s
+// Bound by a row's chain of dependent steps and HBM together (issue slots 58% used).  One GB300, us a call, GB/s as in ea_layernorm.cu:
+//   16,384 x 1600 bf16 with the residual's gradient 39.4 us, 5,320 GB/s; 1601 wide 63;  8,192 x 4,096 48 us, 5,600 GB/s;  4,096 x 8,192 49.6
+//   rows that registers do not hold: 4,096 x 12,288 bf16 465 us, 870 GB/s
 //   7,021 x 769 binary32 17.6 us, 3,690 GB/s, of which 7 are what 64 rows take: launches, weights and the join
 #include "ea_layernorm.cuh"
 

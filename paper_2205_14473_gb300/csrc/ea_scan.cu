@@ -3,7 +3,7 @@
 // Bound by HBM where the columns fill the device, else by a step's latency along each sequence.  One GB300, us a call, GB/s of the
 // bytes that a call cannot do without, against a copy's 6,767:
 //   16 x 1024 x 1600 bf16            26.5 us, 5,950 GB/s; its gradient 51.3 us, 6,130 GB/s
-//   256 x 256 x 1024                 61.7 us, 6,520 GB/s
+//   256 x 256 x 1024                 61.5 us, 6,550 GB/s;  320 x 256 x 1024 75.3 us, its gradient 148 us, 6,800 GB/s
 //   2 x 65,536 x 1024                148 us, 5,430 GB/s (clusters of 8; 128 steps of 1.2 us)
 //   9 sequences of up to 3001 x 515 binary32, off any boundary, gradient  54 us, 4,110 GB/s
 //   1 x 65,536 x 128                 28 us (latency: 8 steps of clusters of 16, 128 CTAs in all)
@@ -742,7 +742,8 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
     return EA_OK;
 }
 
-// Sequences up to kWalkRows are walked along; longer ones where so many 16-byte packs of columns are there to an SM that each
+// Sequences up to kWalkRows are walked along (400 x 16 x 1024 bf16 9.3 us, in tiles 28.6;  64 x 16 x 1600 5.3 and 8.4, gradient 8.2 and 7.5, x 8
+// 4.9 and 7.1; few of them would be faster in tiles: 4 x 16 x 1600 5.3 and 2.5, x 4 equal, gradient 7.8 and 2.6); longer ones where so many 16-byte packs of columns are there to an SM that each
 // thread's loads fill the device, and no longer than this: a tile's chunk of rows, and its exchange, costs the same whether
 // its rows are there or not, and what it reads is further ahead.  bf16, us walked and in tiles:
 //   forward (4 rows of loads ahead)   320 x 33 x 1024 (270 packs) 18.2 and 24.6, x 48 0.95 of the tiles' time, x 64 1.12, x 256 113.7 and 75.4;
