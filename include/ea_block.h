@@ -94,9 +94,10 @@ int ea_scan_init(const ea_scan_config *cfg, void *workspace, size_t workspace_by
  *   h_t = f_t h_{t-1} + (1 - f_t) v_t,    h_{-1} = initial,
  * the states carried in binary32 and each rounded once to h's type.  f and 1 - f each are within (4 + 0.7 |z|) 2^-23 of
  * themselves (exp's argument is a rounded product, whose absolute error grows with |z|) and 2^-126.  Each is rounded by itself,
- * and each of the terms that make up a state is off by up to 2^-21 of itself for every row that it is carried through (2^-25 was
- * measured where gates nearly hold): over that many rows of such gates f and 1 - f do not keep a state between its inputs as a
- * mean would.  A state that is not finite leaves the later ones of its column not finite.
+ * and each of the terms that make up a state is off, relative to itself, by what f is and a rounding for every row that it is
+ * carried through, 2^-21 at most where z >= 0 (2^-25 was measured where gates nearly hold): over very many rows of such gates f and
+ * 1 - f do not keep a state between its inputs as a mean would.  A state that is not finite leaves the later ones of its column
+ * not finite.
  * initial: batch x dim binary32 values, or NULL for zeros.  final: NULL, or batch x dim binary32 values that receive every
  * sequence's last state; it may be initial.
  * lengths: NULL, or one length per sequence on the device: rows from there on are not read, their h is 0, and the state after

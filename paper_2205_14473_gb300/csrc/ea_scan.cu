@@ -742,18 +742,20 @@ int check_call(const ea_scan *s, const ea_scan_call *c, const float *initial, co
     return EA_OK;
 }
 
-// Sequences up to kWalkRows are walked along (400 x 16 x 1024 bf16 9.3 us, in tiles 28.6;  64 x 16 x 1600 5.3 and 8.4, gradient 8.2 and 7.5, x 8
-// 4.9 and 7.1; few of them would be faster in tiles: 4 x 16 x 1600 5.3 and 2.5, x 4 equal, gradient 7.8 and 2.6); longer ones where so many 16-byte packs of columns are there to an SM that each
-// thread's loads fill the device, and no longer than this: a tile's chunk of rows, and its exchange, costs the same whether
-// its rows are there or not, and what it reads is further ahead.  bf16, us walked and in tiles:
-//   forward (4 rows of loads ahead)   320 x 33 x 1024 (270 packs) 18.2 and 24.6, x 48 0.95 of the tiles' time, x 64 1.12, x 256 113.7 and 75.4;
-//     512 x 33 x 1024 (431 packs) 21.4 and 37.4, x 100 56.4 and 61.5, x 128 70.9 and 65.3;  256 x 64 x 1024 (215 packs) 1.27
-//   gradient (none)   320 x 33 x 1024 35.2 and 31.6, x 256 248 and 149;  400 x 33 x 1024 (337 packs) 0.97, x 40 44.9 and 40.3;
-//     512 x 33 x 1024 41.8 and 47.8, x 40 50.1 and 49.9, x 64 77.5 and 58.8, x 256 296 and 236;  1024 x 48 x 1024 (862 packs) 0.91,
-//     x 64 1.05, x 65 121.7 and 131.4, x 80 0.98, x 128 1.02;  700 x 48 x 1024 (589 packs) 1.01;  in single elements 300 x 17 x 1025 (253 packs) 27.9 and 38.9, x 40 58.8 and
-//     58.5, 320 x 48 x 1025 70.4 and 63.2
-// That is where columns fill at least three quarters of their tiles; else any length is walked from kWalkPacks on: 45,600 x 300 x 8 (an
-// eighth, 300 packs) 183 and 679, gradient 418 and 1,111;  27,000 x 300 x 40 (0.62) 330 and 425, 723 and 724;  23,000 x 300 x 48 (0.75) 358 and 359, 757 and 604.
+// Sequences up to kWalkRows are walked along; longer ones where so many 16-byte packs of columns are there to an SM that each
+// thread's loads fill the device, and no longer than this: a tile's chunk of rows, and its exchange, costs the same whether its
+// rows are there or not, and what it reads is further ahead.  bf16, us walked and in tiles:
+//   up to 16 rows   400 x 16 x 1024 9.3 and 28.6;  64 x 16 x 1600 5.3 and 8.4, gradient 8.2 and 7.5, x 8 4.9 and 7.1.  Few of them would be
+//     faster in tiles: 4 x 16 x 1600 5.3 and 2.5, gradient 7.8 and 2.6, x 4 2.5 and 2.5, 3.1 and 2.5
+//   forward (4 rows of loads ahead)   320 x 33 x 1024 (270 packs) 18.2 and 24.6, x 48 0.95 of the tiles' time, x 64 1.12, x 256 113.7 and
+//     75.4;  512 x 33 x 1024 (431 packs) 21.4 and 37.4, x 100 56.4 and 61.5, x 128 70.9 and 65.3;  256 x 64 x 1024 (215 packs) 1.27
+//   gradient (none ahead)   320 x 33 x 1024 35.2 and 31.6, x 256 248 and 149;  400 x 33 x 1024 (337 packs) 0.97, x 40 44.9 and 40.3;
+//     512 x 33 x 1024 41.8 and 47.8, x 40 50.1 and 49.9, x 64 77.5 and 58.8, x 256 296 and 236;  700 x 48 x 1024 (589 packs) 1.01;
+//     1024 x 48 x 1024 (862 packs) 0.91, x 64 1.05, x 65 121.7 and 131.4, x 80 0.98, x 128 1.02;  in single elements 300 x 17 x 1025
+//     (253 packs) 27.9 and 38.9, x 40 58.8 and 58.5, 320 x 48 x 1025 70.4 and 63.2
+// That is where columns fill at least three quarters of their tiles; else any length is walked from kWalkPacks on: 45,600 x 300 x 8
+// (an eighth, 300 packs) 183 and 679, gradient 418 and 1,111;  27,000 x 300 x 40 (0.62) 330 and 425, 723 and 724;  23,000 x 300 x 48 (0.75)
+// 358 and 359, 757 and 604.
 constexpr int64_t kWalkRows = 16, kWalkPacks = 256;
 struct WalkRule {
     int64_t packs, rows;  // from so many packs an SM, up to so many rows
